@@ -550,6 +550,109 @@ int32_t kv_recompute_layer(kv_recompute_t* rc, const kv_shape_t* shape, const kv
                            void* kv, void* x_out, void* workspace, uint64_t workspace_bytes,
                            void* stream);
 
+/* ------------------------------------------------ decoding on the packed records */
+
+/* Between two switches a context decodes.  The calls below do that on the records themselves, in the pool in which
+ * they lie: new tokens are appended to them, attention reads them as they are packed, and the tokens that
+ * attention has hardly used make room.  A context that was switched out packed continues without a Load.
+ *
+ * A SEQUENCE is a context's chunks as a table of pages: page i holds the tokens (slots) [i*chunk_tokens,
+ * (i+1)*chunk_tokens) of the sequence in the record at byte off[i] of the pool, at width bits[i] (a record as
+ * kv_compress_chunks writes it, all layers; the off and bits of kv_plan_chunks_dev or kv_chunk_offsets are such a
+ * table).  Several sequences are run together, each with a table of its own; two of them may share pages that
+ * neither writes.
+ * Requirements on the shape (else KV_ESHAPE): format 0 or 3, head_dim in {64, 128, 256}, chunk_tokens % 16 == 0;
+ * n_tokens is the most tokens a sequence may have.
+ *
+ * The table is on the device, where another kernel may have written it, and a call cannot look at it.  The kernels
+ * keep to it as far as it is sound: a page whose width is not one of 16, 8, 4, 2, whose offset is not a multiple
+ * of 16 or whose record does not end within pool_bytes is ABSENT (so is a page of bits 0, the way to leave out
+ * a page that has been reclaimed): it is not read, its tokens are not attended to, nothing is written to it.
+ * A length is cut to [0, n_tokens]. */
+typedef struct {
+    void*           pool;        /* dev, 16-byte aligned                                           */
+    uint64_t        pool_bytes;
+    const uint64_t* off;         /* dev [n_seqs][stride] byte offsets of the records in the pool   */
+    const uint8_t*  bits;        /* dev [n_seqs][stride] their widths                              */
+    const int32_t*  len;         /* dev [n_seqs] tokens of each sequence, the new ones included    */
+    int32_t         n_seqs;      /* 1 .. 65535                                                     */
+    int32_t         stride;      /* table entries from one sequence to the next, >= n_chunks       */
+} kv_pages_t;
+
+/* The NEW ROWS of a step are the rows of its newest tokens, sequence after sequence: sequence s has the rows
+ * [row_start[s], row_start[s+1]) of n_rows (row_start: dev i32 [n_seqs+1], ascending; NULL: one row per sequence,
+ * n_rows == n_seqs).  Its j-th of c rows is its token len[s] - c + j.  A sequence may have none; a row whose token
+ * would be negative has no place and sees nothing; rows in front of row_start[0] or behind row_start[n_seqs] belong
+ * to no sequence: nothing of theirs is read or written. */
+
+/* Append (Claim with contents, Sec. 3.1 primitive 1): writes the K and V rows of the new tokens to their places in
+ * one layer of their pages, each at the width of its page: fp16 copied, 8 / 4 / 2 bits quantised by the rule above
+ * (a group never spans two tokens, so the bytes are those kv_compress_chunks gives the same values).
+ *   k, v   dev fp16 [n_rows][n_kv_heads][head_dim]; row_stride elements from one row to the next (>= n_kv_heads *
+ *          head_dim, a multiple of 8: k and v may be parts of one projection's output);
+ *   seen   dev i32 [n_seqs], tokens the sequence has had in all, the new ones included: its j-th of c rows is at
+ *          position seen[s] - c + j (len[s] and seen[s] differ once tokens have been evicted); NULL: len;
+ *   mass   dev fp32 [n_seqs][n_kv_heads][n_tokens] of this layer, may be NULL: 0 at the slots of the new tokens;
+ *   pos    dev i32, same shape, may be NULL: their positions there.
+ * n_rows == 0 is a no-op. */
+int32_t kv_append_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                         const void* k, const void* v, int64_t row_stride, int32_t n_rows,
+                         const int32_t* row_start, const int32_t* seen,
+                         float* mass, int32_t* pos, void* stream);
+
+/* Bytes of device workspace kv_attend_tokens needs; 0 on invalid arguments. */
+uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int32_t max_rows, int32_t with_mass);
+
+/* Attention of the new rows to one layer's pages as they are packed:
+ *   out = softmax(q K^T / sqrt(head_dim), tokens up to the row's own, absent pages left out) V
+ * per query head, query head h reading kv head h / (n_q_heads / n_kv_heads).  K counts with the values code * scale + mn
+ * its codes stand for, V with these rounded to fp16; logits, softmax and sums are fp32, probabilities enter the product
+ * with V as fp16.  A row that sees no token gives zeros.
+ *   q        dev fp16 [n_rows][n_q_heads][head_dim], q_stride elements from row to row (>= n_q_heads * head_dim, a
+ *            multiple of 8);
+ *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others'
+ *            output is left as it was);
+ *   mass     dev fp32 [n_seqs][n_kv_heads][n_tokens] of this layer, may be NULL: for every slot below len[s] of a
+ *            sequence that has new rows
+ *              mass = mass_in + sum over its rows and the query heads of the kv head of the softmax weights
+ *            (0 in absent pages); other entries are untouched.  mass_in: same shape, may equal mass (the weights
+ *            accumulate in place) or be NULL (zeros), but not overlap it otherwise;
+ *   out      dev fp16 [n_rows][n_q_heads][head_dim], 16-byte aligned;
+ *   workspace dev, >= kv_attend_workspace_bytes(), 256-byte aligned, contents scratch.
+ * The rows and pages of the sequences must not alias out, mass or the workspace.  n_rows == 0 is a no-op. */
+int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                         const void* q, int64_t q_stride, int32_t n_rows, const int32_t* row_start, int32_t max_rows,
+                         const float* mass_in, float* mass, void* workspace, uint64_t workspace_bytes,
+                         void* out, void* stream);
+
+/* Bytes of device workspace kv_evict_tokens needs; 0 on invalid arguments. */
+uint64_t kv_evict_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int32_t n_layers, int32_t keep);
+
+/* Eviction by accumulated attention weight: every kv head of the layers [layer_begin, layer_end) keeps `keep` of its
+ * sequence's tokens, and they come to lie in the slots [0, keep), so that the pages behind them are free once every layer
+ * has been treated (the caller lowers len to keep and takes the pages from the table).  Sequences of at most `keep` tokens
+ * are left as they are.
+ *   Kept are, in this order of preference: tokens at positions below `sink` or at or above seen[s] - recent; then the
+ *   others by mass_in, heaviest first (NaN counts as less than everything); of equal ones the lowest slots.
+ *   Kept tokens below `keep` stay where they are.  The i-th slot below `keep` whose token goes is taken by the i-th kept
+ *   token at or above `keep`, in ascending order of slots: only rows that have to move are moved, and slots no longer
+ *   ascend with positions (attention does not ask for that; pos tells which token a slot holds).
+ *   A row that moves between pages of one width keeps its bytes; between two widths it is dequantised to fp16 and
+ *   quantised at the width it comes to.  A row is not moved from or to an absent page (the tokens of an absent page can
+ *   be kept like others: present pages are the caller's care).
+ *   mass_in, pos_in  dev fp32 / i32 [layer_end - layer_begin][n_seqs][n_kv_heads][n_tokens];
+ *   seen             as for kv_append_tokens;
+ *   mass, pos        same shape: entries of the slots [0, min(len, keep)) get those of the tokens that now lie there, the
+ *                    others are untouched.  mass may equal mass_in, pos may equal pos_in; no other overlap;
+ *   keep >= 1, sink, recent >= 0, sink + recent <= keep (else KV_EINVAL).
+ *   workspace        dev, >= kv_evict_workspace_bytes(), 256-byte aligned, contents scratch.
+ * Two sequences of one call must not share pages in which rows move.  An empty layer range is a no-op. */
+int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_t layer_begin, int32_t layer_end,
+                        const float* mass_in, const int32_t* pos_in, const int32_t* seen,
+                        int32_t keep, int32_t sink, int32_t recent,
+                        void* workspace, uint64_t workspace_bytes,
+                        float* mass, int32_t* pos, void* stream);
+
 /* -------------------------------------------- host lifecycle (Sec. 3.4 ii) */
 
 /* LCTRU queue: concatenated sub-queues, one per bit-width, least compressed

@@ -65,7 +65,7 @@ class Shape(NamedTuple):
 
 
 _lib = None
-_vp, _i32, _u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64
+_vp, _i32, _u64, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_int64
 
 _SIGNATURES = {
     "kv_last_error": (ctypes.c_char_p, []),
@@ -98,6 +98,11 @@ _SIGNATURES = {
     "kv_recompute_workspace_bytes": (_u64, [_vp, _vp, _i32]),
     "kv_recompute_tune": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _u64, _vp, _vp]),
     "kv_recompute_layer": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _u64, _vp]),
+    "kv_append_tokens": (_i32, [_vp, _vp, _i32, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "kv_attend_workspace_bytes": (_u64, [_vp, _i32, _i32, _i32]),
+    "kv_attend_tokens": (_i32, [_vp, _vp, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _vp, _vp, _u64, _vp, _vp]),
+    "kv_evict_workspace_bytes": (_u64, [_vp, _i32, _i32, _i32]),
+    "kv_evict_tokens": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _u64, _vp, _vp, _vp]),
     "kv_lctru_create": (_vp, []),
     "kv_lctru_destroy": (None, [_vp]),
     "kv_lctru_insert": (_i32, [_vp, _i32, _i32, _i32, _u64, _u64]),
@@ -603,6 +608,119 @@ def kv_swapout_aot(packed_dev: torch.Tensor, packed_pinned: torch.Tensor, begin:
         raise ValueError("range exceeds a buffer")
     _check(lib().kv_swapout_aot(_dev(packed_dev), packed_pinned.data_ptr(), begin, end,
                                 _stream(producer_stream), _stream(copy_stream)))
+
+
+# ------------------------------------------------------------------ decoding on the packed records
+
+class kv_pages_t(ctypes.Structure):
+    _fields_ = [("pool", _vp), ("pool_bytes", _u64), ("off", _vp), ("bits", _vp), ("len", _vp),
+                ("n_seqs", _i32), ("stride", _i32)]
+
+
+class Pages:
+    """Paged sequences (kv_pages_t) of one shape: the record pool, the page tables off and bits [n_seqs][stride] and the
+    lengths [n_seqs].  Holds the tensors and the two C structures, so that a step marshals them once; what the tensors
+    hold may change from call to call."""
+
+    def __init__(self, shape: Shape, pool: torch.Tensor, off: torch.Tensor, bits: torch.Tensor, length: torch.Tensor):
+        if off.dim() != 2 or tuple(bits.shape) != tuple(off.shape) or tuple(length.shape) != (off.shape[0],):
+            raise ValueError("off and bits must be [n_seqs][stride], length [n_seqs]")
+        for t in (off, bits, length):
+            if t.device != pool.device:
+                raise ValueError("the pool and its tables must be on one device")
+        self.shape, self.pool, self.off, self.bits, self.length = shape, pool, off, bits, length
+        self.device = pool.device
+        self._shape = shape.c()
+        self._c = kv_pages_t(_dev(pool), pool.numel() * pool.element_size(), _dev(off, torch.int64), _dev(bits, torch.uint8),
+                             _dev(length, torch.int32), off.shape[0], off.shape[1])
+        self._refs = ctypes.byref(self._shape), ctypes.byref(self._c)
+
+    @property
+    def n_seqs(self) -> int:
+        return self._c.n_seqs
+
+    def _on_device(self, stream):
+        """The stream's address; the pages' device has to be the current one."""
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError(f"the pages are on {self.device}, which is not the current device")
+        return _stream(stream)
+
+    def _arg(self, t, dtype, shape, name):
+        """Address of an optional contiguous tensor of this dtype and shape on the pages' device."""
+        if t is None:
+            return None
+        if tuple(t.shape) != shape or t.device != self.device:
+            raise ValueError(f"{name} must be {list(shape)} on {self.device}, got {list(t.shape)} on {t.device}")
+        return _dev(t, dtype)
+
+    def _rows(self, t, heads, name):
+        """Address and row stride of fp16 rows [n_rows][heads][head_dim], whose rows may lie apart."""
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.shape.head_dim or t.device != self.device:
+            raise ValueError(f"{name} must be [n_rows][{heads}][{self.shape.head_dim}] on {self.device}")
+        if t.dtype != torch.float16:
+            raise TypeError(f"expected dtype torch.float16, got {t.dtype}")
+        stride = t.stride()
+        if stride[2] != 1 or (heads > 1 and stride[1] != t.shape[2]):
+            raise TypeError(f"the heads of a row of {name} must be contiguous")
+        return t.data_ptr(), (stride[0] if t.shape[0] > 1 else heads * t.shape[2])
+
+    def _book(self, t, dtype, name, layers=None):
+        s = self.shape
+        shape = (self.n_seqs, s.n_kv_heads, s.n_tokens)
+        return self._arg(t, dtype, shape if layers is None else (layers,) + shape, name)
+
+
+def kv_append_tokens(pages: Pages, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor = None,
+                     seen: torch.Tensor = None, mass: torch.Tensor = None, pos: torch.Tensor = None, stream=None) -> None:
+    k_at, stride = pages._rows(k, pages.shape.n_kv_heads, "k")
+    v_at, v_stride = pages._rows(v, pages.shape.n_kv_heads, "v")
+    if v.shape != k.shape or v_stride != stride:
+        raise ValueError("k and v must have the same shape and row stride")
+    _check(lib().kv_append_tokens(*pages._refs, layer, k_at, v_at, stride, k.shape[0],
+                                  pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"),
+                                  pages._arg(seen, torch.int32, (pages.n_seqs,), "seen"),
+                                  pages._book(mass, torch.float32, "mass"), pages._book(pos, torch.int32, "pos"),
+                                  pages._on_device(stream)))
+
+
+def kv_attend_workspace_bytes(shape: Shape, n_seqs: int, max_rows: int = 1, with_mass: bool = False) -> int:
+    s = shape.c()
+    n = int(lib().kv_attend_workspace_bytes(ctypes.byref(s), n_seqs, max_rows, int(with_mass)))
+    if n == 0:
+        raise KvError(KV_EINVAL, kv_last_error())
+    return n
+
+
+def kv_attend_tokens(pages: Pages, layer: int, q: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor,
+                     row_start: torch.Tensor = None, max_rows: int = 1, mass_in: torch.Tensor = None,
+                     mass: torch.Tensor = None, stream=None) -> None:
+    q_at, stride = pages._rows(q, pages.shape.n_q_heads, "q")
+    _check(lib().kv_attend_tokens(*pages._refs, layer, q_at, stride, q.shape[0],
+                                  pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"), max_rows,
+                                  pages._book(mass_in, torch.float32, "mass_in"), pages._book(mass, torch.float32, "mass"),
+                                  _dev(workspace), workspace.numel() * workspace.element_size(),
+                                  pages._arg(out, torch.float16, tuple(q.shape), "out"), pages._on_device(stream)))
+
+
+def kv_evict_workspace_bytes(shape: Shape, n_seqs: int, n_layers: int, keep: int) -> int:
+    s = shape.c()
+    n = int(lib().kv_evict_workspace_bytes(ctypes.byref(s), n_seqs, n_layers, keep))
+    if n == 0:
+        raise KvError(KV_EINVAL, kv_last_error())
+    return n
+
+
+def kv_evict_tokens(pages: Pages, layer_begin: int, layer_end: int, mass_in: torch.Tensor, pos_in: torch.Tensor, keep: int,
+                    sink: int, recent: int, workspace: torch.Tensor, mass: torch.Tensor, pos: torch.Tensor,
+                    seen: torch.Tensor = None, stream=None) -> None:
+    layers = layer_end - layer_begin
+    _check(lib().kv_evict_tokens(*pages._refs, layer_begin, layer_end,
+                                 pages._book(mass_in, torch.float32, "mass_in", layers),
+                                 pages._book(pos_in, torch.int32, "pos_in", layers),
+                                 pages._arg(seen, torch.int32, (pages.n_seqs,), "seen"), keep, sink, recent,
+                                 _dev(workspace), workspace.numel() * workspace.element_size(),
+                                 pages._book(mass, torch.float32, "mass", layers), pages._book(pos, torch.int32, "pos", layers),
+                                 pages._on_device(stream)))
 
 
 # ------------------------------------------------------------------ host lifecycle

@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libkvswitch.so")
-SOURCES = ("kv_host.cpp", "kv_lctru.cpp", "kv_device.hip", "kv_recompute.hip")
+SOURCES = ("kv_host.cpp", "kv_lctru.cpp", "kv_device.hip", "kv_recompute.hip", "kv_decode.hip")
 
 
 def hipcc() -> str:

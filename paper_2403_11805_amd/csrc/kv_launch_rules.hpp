@@ -60,4 +60,19 @@ inline int64_t attention_shares(int64_t pairs, int64_t n_kv_heads, int64_t tiles
     return std::max<int64_t>(shares, 1);
 }
 
+// Append: 16-byte pieces per lane of a wavefront's share of a row's K and V heads.
+inline int append_pieces_per_lane(int64_t n_rows, int pieces) { return n_rows * pieces >= 4 * 64 * 2048 ? 4 : 1; }
+
+// Shares that the tokens of a (sequence, kv head, row tile) are divided among, `groups` of these and at most `tokens` tokens each.
+constexpr int kAttendMinUnits = 4;          // units of 32 tokens of a share: one per wavefront
+inline int64_t attend_splits(int64_t groups, int64_t tokens) {
+    const int64_t units = (tokens + 31) / 32, most = std::max<int64_t>(1, units / kAttendMinUnits);
+    return std::max<int64_t>(1, std::min<int64_t>({most, std::max<int64_t>(1024 / groups, (tokens + 4095) / 4096), 256}));
+}
+
+// Eviction: workgroups that share a pair's moves, `rows` at a time each.
+inline int64_t evict_blocks(int64_t pairs, int64_t list, int64_t rows) {
+    return std::max<int64_t>(1, std::min<int64_t>((list + rows - 1) / rows, std::max<int64_t>(4096 / pairs, 4)));
+}
+
 }  // namespace kvs
