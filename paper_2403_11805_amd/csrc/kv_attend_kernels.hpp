@@ -6,16 +6,18 @@
 // in which a lane keeps one query row (lane % 16) throughout: reference, sum and rescaling of a row need no exchange
 // between lanes, and the four S^T values of a lane (tokens 4 * (lane / 16) + 0..3 of each tile) ARE the operand P^T of the second
 // product, without a move.  The k index of an MFMA is free as long as both operands agree on it:
-//   K: k runs over head dimensions in the order 64*.. + 16 * (lane / 16) + ..: a lane reads one contiguous piece per group, and
-//      within eight dimensions the pairs (0,4) (1,5) (2,6) (3,7), which is how codes of 4 and 2 bits fall out of a word;
+//   K: a lane reads one contiguous piece of its token per group of dimensions; within eight dimensions codes come in the pairs
+//      (0,4) (1,5) (2,6) (3,7), which is how they fall out of a word, and Q is put into that order for them;
 //   V: k runs over the unit's tokens, four per quarter wavefront and tile; a lane reads the rows of its tokens at its own D/16
 //      contiguous dimensions, and one v_perm per register pairs two tokens.
-// Codes are not dequantised for K: a half with the code in the top bits of its mantissa is 2^b + code exactly (1024 + code at 8
-// bits, from a byte), the MFMA sums q * that per group, and scale and minimum enter once per (token, group):
-//     S = sum_g s_g (acc_g - 2^b qsum_g) + mn_g qsum_g.
-// V is dequantised by one v_fma_mix per element, fp16(code * s + mn).
+// A code of b bits in the low bits of a half is the subnormal number code * 2^-24 exactly, so a shift and a mask make an operand
+// of two codes.  K is not dequantised: the MFMAs sum q * code per group, and scale and minimum enter once per (token, group),
+//     S = sum_g (2^24 s_g) acc_g + mn_g qsum_g.
+// V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s.  P enters as the sum of two
+// halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
 #pragma once
 
+#include "kv_launch_rules.hpp"
 #include "kv_pages_kernels.hpp"
 
 namespace kvs {
@@ -25,9 +27,11 @@ typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 h4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kAttendWaves = 4;
+constexpr int kMaxSplits = kAttendMaxSplits;
 constexpr float kTop = 7.0f;         // a row's reference is set 2^7 below its largest logit so far ...
 constexpr float kSlack = 15.0f;      // ... and moves when a logit passes 2^15 above it: probabilities stay in fp16's range, and those
                                      // 2^-31 below the largest still count
+constexpr int kNowhere = 0x7fffff00;     // first token of a tile that no row sees
 
 struct AttendGeom {
     int32_t layer, n_rows, max_rows;
@@ -54,57 +58,40 @@ __device__ __forceinline__ Shares shares_of(const AttendGeom& g, int n) {
 
 __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
 
-// What a code of width W becomes by the bits below: kOffset + code.
-template <int W> struct CodeOffset { static constexpr float value = W == 8 ? 1024.0f : (W == 4 ? 16.0f : 4.0f); };
-
-// Shift by a signed constant.
-template <int S> __device__ __forceinline__ uint32_t shift(uint32_t x) {
-    if constexpr (S >= 0) return x << S;
-    else return x >> -S;
+// Eight halves in the order (0,4) (1,5) (2,6) (3,7).
+__device__ __forceinline__ u4_t paired(const uint32_t* w) {
+    return u4_t{perm(w[2], w[0], 0x05040100u), perm(w[2], w[0], 0x07060302u), perm(w[3], w[1], 0x05040100u), perm(w[3], w[1], 0x07060302u)};
 }
 
-// Eight dimensions of K, in the order (0,4) (1,5) (2,6) (3,7), from their 8 * W bits.
+constexpr float kCode = 16777216.0f;       // 2^24: what a code as a subnormal half has to be multiplied by
+
+// Eight dimensions of K from their 8 * W bits: fp16 as they are, codes in the order of paired().  (W = 2: the bits of dimensions 0-3
+// in the low half, those of 4-7 in the high one.)
 template <int W> __device__ __forceinline__ u4_t k_operand(const uint32_t* w) {
-    u4_t r;
-    if constexpr (W == 16) {
-        r.x = perm(w[2], w[0], 0x05040100u);
-        r.y = perm(w[2], w[0], 0x07060302u);
-        r.z = perm(w[3], w[1], 0x05040100u);
-        r.w = perm(w[3], w[1], 0x07060302u);
-    } else if constexpr (W == 8) {
-        r.x = perm(w[1], w[0], 0x0c040c00u) | 0x64006400u;
-        r.y = perm(w[1], w[0], 0x0c050c01u) | 0x64006400u;
-        r.z = perm(w[1], w[0], 0x0c060c02u) | 0x64006400u;
-        r.w = perm(w[1], w[0], 0x0c070c03u) | 0x64006400u;
-    } else if constexpr (W == 4) {
-        r.x = (shift<6>(w[0]) & 0x03c003c0u) | 0x4c004c00u;
-        r.y = (shift<2>(w[0]) & 0x03c003c0u) | 0x4c004c00u;
-        r.z = (shift<-2>(w[0]) & 0x03c003c0u) | 0x4c004c00u;
-        r.w = (shift<-6>(w[0]) & 0x03c003c0u) | 0x4c004c00u;
-    } else {                                                // the bytes of dimensions 0-3 and 4-7, one in each half
-        r.x = (shift<8>(w[0]) & 0x03000300u) | 0x44004400u;
-        r.y = (shift<6>(w[0]) & 0x03000300u) | 0x44004400u;
-        r.z = (shift<4>(w[0]) & 0x03000300u) | 0x44004400u;
-        r.w = (shift<2>(w[0]) & 0x03000300u) | 0x44004400u;
-    }
-    return r;
+    if constexpr (W == 16) return u4_t{w[0], w[1], w[2], w[3]};
+    else if constexpr (W == 8)
+        return u4_t{perm(w[1], w[0], 0x0c040c00u), perm(w[1], w[0], 0x0c050c01u), perm(w[1], w[0], 0x0c060c02u), perm(w[1], w[0], 0x0c070c03u)};
+    else if constexpr (W == 4)
+        return u4_t{w[0] & 0x000f000fu, (w[0] >> 4) & 0x000f000fu, (w[0] >> 8) & 0x000f000fu, (w[0] >> 12) & 0x000f000fu};
+    else return u4_t{w[0] & 0x00030003u, (w[0] >> 2) & 0x00030003u, (w[0] >> 4) & 0x00030003u, (w[0] >> 6) & 0x00030003u};
 }
 
 __device__ __forceinline__ h8_t as_h8(u4_t v) { return __builtin_bit_cast(h8_t, v); }
 
-// Codes of two tokens for one dimension, as halves 2^b + code, from the words that hold them (dimension d of the word).
+// Codes of two tokens for dimension d of the words a and b that hold them, as a pair of subnormal halves; those of odd dimensions of
+// widths 4 and 2 are left 2^W times as large (their scale makes up for it).
 template <int W, int d> __device__ __forceinline__ uint32_t v_codes(uint32_t a, uint32_t b) {
-    if constexpr (W == 8) return perm(b, a, 0x0c040c00u + 0x00010001u * d) | 0x64006400u;
+    if constexpr (W == 8) return perm(b, a, 0x0c040c00u + 0x00010001u * d);
     else if constexpr (W == 4) {
         const uint32_t x = perm(b, a, d < 4 ? 0x05040100u : 0x07060302u);
-        return (shift<6 - 4 * (d & 3)>(x) & 0x03c003c0u) | 0x4c004c00u;
+        return (x >> (4 * (d & 2))) & (d & 1 ? 0x00f000f0u : 0x000f000fu);
     } else {
         const uint32_t x = perm(b, a, d < 8 ? 0x05040100u : 0x07060302u);
-        return (shift<8 - 2 * (d & 7)>(x) & 0x03000300u) | 0x44004400u;
+        return (x >> (2 * (d & 6))) & (d & 1 ? 0x000c000cu : 0x00030003u);
     }
 }
 
-// Loads n contiguous 32-bit words (n a power of two; less than one: BYTES bytes into the low end of one).
+// BYTES contiguous bytes as 32-bit words (less than four: the low end of one).
 template <int BYTES> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
     if constexpr (BYTES >= 16) {
 #pragma unroll
@@ -126,86 +113,64 @@ template <int D> struct RowState {
     float ref, sum;                  // the row's reference (same in its four lanes), the lane's own share of the sum
 };
 
-// A tile whose loads are issued: raw words of K and V, parameters of K for the lane's four tokens and every group, of V for its four
-// tokens and the group of its dimensions.
-template <int D, int G, int W> struct TileRegs {
-    static constexpr int NG = D / G, DL = D / 16;
-    static constexpr int kK = D * W / 128;                              // words of a lane's share of a K tile
-    static constexpr int kV = DL * W / 32 > 0 ? DL * W / 32 : 1;        // words of one token's row at the lane's dimensions
-    uint32_t k[kK];
-    uint32_t v[4][kV];
-    float ks[W == 16 ? 1 : 4 * NG], km[W == 16 ? 1 : 4 * NG];
-    float vs[W == 16 ? 1 : 4], vm[W == 16 ? 1 : 4];
+// What is loaded of a tile, as it lies in memory: K at the lane's token with the parameters of the lane's four tokens 4q .. 4q+3 in
+// every group; V of these four tokens at the lane's dimensions, with their parameters (HP: parameters in binary16).
+template <int D, int G, int W, bool HP> struct KRegs {
+    static constexpr int kWords = D * W / 128, kParams = W == 16 ? 1 : 4 * (D / G) / (HP ? 2 : 1);
+    uint32_t k[kWords], s[kParams], m[kParams];
+};
+template <int D, int G, int W, bool HP> struct VRegs {
+    static constexpr int kWords = D / 16 * W / 32 > 0 ? D / 16 * W / 32 : 1, kParams = KRegs<D, G, W, HP>::kParams;
+    uint32_t v[4][kWords], s[kParams], m[kParams];
 };
 
-// Parameters of the tokens 4q .. 4q+3 of the tile: 4 * NG values that lie side by side.
-template <int N> __device__ __forceinline__ void load_params(const uint8_t* p, int half_params, int first, float* out) {
-    if (half_params) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const h4_t x = reinterpret_cast<const h4_t*>(reinterpret_cast<const _Float16*>(p) + first)[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) out[4 * i + j] = static_cast<float>(x[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const f4_t x = reinterpret_cast<const f4_t*>(reinterpret_cast<const float*>(p) + first)[i];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) out[4 * i + j] = x[j];
-        }
-    }
+// Parameter i of those loaded.
+template <bool HP> __device__ __forceinline__ float param(const uint32_t* w, int i) {
+    if constexpr (HP) return static_cast<float>(__builtin_bit_cast(h2_t, w[i / 2])[i % 2]);
+    else return __builtin_bit_cast(float, w[i]);
 }
 
-// Issues the loads of a tile: `record` its page's record, `in_page` its first token's row, `valid` how many of its 16 tokens there
-// are (what lies behind them may be anything: V rows of missing tokens are replaced by the last one there is, their parameters by 0).
-template <int D, int G, int W>
-__device__ __forceinline__ void tile_load(TileRegs<D, G, W>& t, const uint8_t* __restrict__ record, const PagesView& v, int k_slab,
-                                          int in_page, int valid, int lane) {
-    constexpr int NG = D / G, DL = D / 16, kRowBytes = D * W / 8;
+// Where a tile lies: its page's record, its first token's row there, its first token, and how many of its 16 tokens there are.
+struct Tile {
+    const uint8_t* record;
+    int in_page, first, valid;
+};
+
+// Issues the loads of a tile; ka, va: the layer's K and V slabs in records of this width.
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabAt& ka, int lane) {
+    constexpr int NG = D / G, kRowBytes = D * W / 8, kPiece = G / 4 * W / 8;     // bytes of a token's row, of a lane's piece per group
     const int l16 = lane & 15, q4 = lane >> 4;
-    const SlabAt ka = slab_at<D>(v, W, k_slab), va = slab_at<D>(v, W, k_slab + v.Hkv);
-    const uint8_t* kb = record + ka.codes + static_cast<uint32_t>(in_page) * kRowBytes;
-    const uint8_t* vb = record + va.codes + static_cast<uint32_t>(in_page) * kRowBytes;
-    constexpr int kPiece = G / 4 * W / 8;                               // bytes of a lane's piece per group
+    const uint8_t* kb = tile.record + ka.codes + static_cast<uint32_t>(tile.in_page) * kRowBytes;
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi)
         load_words<kPiece>(kb + static_cast<uint32_t>(l16 * kRowBytes + gi * (G * W / 8) + q4 * kPiece), &t.k[gi * kPiece / 4]);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int row = min(4 * q4 + r, valid - 1);
-        load_words<DL * W / 8>(vb + static_cast<uint32_t>(row * kRowBytes + l16 * (DL * W / 8)), t.v[r]);
-    }
     if constexpr (W != 16) {
-        const int first = (in_page + 4 * q4) * NG;
-        load_params<4 * NG>(record + ka.scale, v.half_params, first, t.ks);
-        load_params<4 * NG>(record + ka.mn, v.half_params, first, t.km);
-        float s[4 * NG], m[4 * NG];
-        load_params<4 * NG>(record + va.scale, v.half_params, first, s);
-        load_params<4 * NG>(record + va.mn, v.half_params, first, m);
-        const int mine = l16 * DL / G;
+        const uint32_t at = static_cast<uint32_t>((tile.in_page + 4 * q4) * NG * (HP ? 2 : 4));
+        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + ka.scale + at, t.s);
+        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + ka.mn + at, t.m);
+    }
+}
+// (What lies behind a sequence's tokens may be anything: V rows of missing tokens are replaced by the last one there is, and their
+// parameters are not used.)
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabAt& va, int lane) {
+    constexpr int NG = D / G, kRowBytes = D * W / 8, kMine = D / 16 * W / 8;
+    const int l16 = lane & 15, q4 = lane >> 4;
+    const uint8_t* vb = tile.record + va.codes + static_cast<uint32_t>(tile.in_page) * kRowBytes;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float a = s[r * NG], b = m[r * NG];
-#pragma unroll
-            for (int gi = 1; gi < NG; ++gi) {
-                a = mine == gi ? s[r * NG + gi] : a;
-                b = mine == gi ? m[r * NG + gi] : b;
-            }
-            if (valid < 16) {                                           // (uniform)
-                const bool there = 4 * q4 + r < valid;
-                a = there ? a : 0.0f;
-                b = there ? b : 0.0f;
-            }
-            t.vs[r] = a;
-            t.vm[r] = b - a * CodeOffset<W>::value;
-        }
+    for (int r = 0; r < 4; ++r)
+        load_words<kMine>(vb + static_cast<uint32_t>(min(4 * q4 + r, tile.valid - 1) * kRowBytes + l16 * kMine), t.v[r]);
+    if constexpr (W != 16) {
+        const uint32_t at = static_cast<uint32_t>((tile.in_page + 4 * q4) * NG * (HP ? 2 : 4));
+        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + va.scale + at, t.s);
+        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + va.mn + at, t.m);
     }
 }
 
 // S^T of a tile, scaled to logits in units of log2.
-template <int D, int G, int W>
-__device__ __forceinline__ f4_t tile_logits(const TileRegs<D, G, W>& t, const u4_t* q, const float* qsum, float scale) {
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u4_t* q, const float* qsum, float scale) {
     constexpr int NG = D / G, kPer = G / 32;
     f4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -216,121 +181,210 @@ __device__ __forceinline__ f4_t tile_logits(const TileRegs<D, G, W>& t, const u4
             const int j = gi * kPer + i;
             u4_t a;
             if constexpr (W == 2) {
-                const uint32_t both = t.k[j / 2];
-                const uint32_t one = perm(0u, both, (j & 1) ? 0x0c030c02u : 0x0c010c00u);
+                const uint32_t one = perm(0u, t.k[j / 2], (j & 1) ? 0x0c030c02u : 0x0c010c00u);
                 a = k_operand<2>(&one);
             } else a = k_operand<W>(&t.k[j * (W / 4)]);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), as_h8(q[j]), acc, 0, 0, 0);
         }
         if constexpr (W == 16) s = acc;
         else {
-            const float off = CodeOffset<W>::value * qsum[gi];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                s[r] += __builtin_fmaf(t.ks[r * NG + gi], acc[r] - off, t.km[r * NG + gi] * qsum[gi]);
+            for (int r = 0; r < 4; ++r) {
+                s[r] = __builtin_fmaf(param<HP>(t.s, r * NG + gi) * kCode, acc[r], s[r]);
+                s[r] = __builtin_fmaf(param<HP>(t.m, r * NG + gi), qsum[gi], s[r]);
+            }
         }
     }
     return s * scale;
 }
 
+// Scales and minima of a lane's four tokens in the group of its dimensions; `odd` for codes that v_codes leaves larger.
+template <int W> struct VScale {
+    float s[4], odd[4], m[4];
+};
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t, int valid, int lane) {
+    constexpr int NG = D / G;
+    const int q4 = lane >> 4, mine = (lane & 15) * (D / 16) / G;
+    VScale<W> x;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float a = param<HP>(t.s, r * NG), b = param<HP>(t.m, r * NG);
+#pragma unroll
+        for (int gi = 1; gi < NG; ++gi) {
+            a = mine == gi ? param<HP>(t.s, r * NG + gi) : a;
+            b = mine == gi ? param<HP>(t.m, r * NG + gi) : b;
+        }
+        x.s[r] = a;
+        x.m[r] = b;
+    }
+    if (valid < 16) {                                                   // (uniform) missing tokens: 0
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            x.s[r] = 4 * q4 + r < valid ? x.s[r] : 0.0f;
+            x.m[r] = 4 * q4 + r < valid ? x.m[r] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        x.s[r] *= kCode;
+        x.odd[r] = x.s[r] * (W == 4 ? 1.0f / 16 : 1.0f / 4);            // (unused at width 8)
+    }
+    return x;
+}
+
 // V^T of one dimension for tokens (4q + 2j, 4q + 2j + 1) of a tile, as a pair of halves.
-template <int D, int G, int W, int i>
-__device__ __forceinline__ uint32_t v_pair(const TileRegs<D, G, W>& t, int j) {
+template <int D, int G, int W, bool HP, int i>
+__device__ __forceinline__ uint32_t v_pair(const VRegs<D, G, W, HP>& t, const VScale<W>& x, int j) {
     if constexpr (W == 16) return perm(t.v[2 * j + 1][i / 2], t.v[2 * j][i / 2], (i & 1) ? 0x07060302u : 0x05040100u);
     else {
         constexpr int kIn = 32 / W;                                     // dimensions of a word
-        const uint32_t c = v_codes<W, i % kIn>(t.v[2 * j][i / kIn], t.v[2 * j + 1][i / kIn]);
-        const h2_t h = __builtin_bit_cast(h2_t, c);
-        h2_t x;
-        x[0] = static_cast<_Float16>(__builtin_fmaf(static_cast<float>(h[0]), t.vs[2 * j], t.vm[2 * j]));
-        x[1] = static_cast<_Float16>(__builtin_fmaf(static_cast<float>(h[1]), t.vs[2 * j + 1], t.vm[2 * j + 1]));
-        return __builtin_bit_cast(uint32_t, x);
+        constexpr bool odd = W != 8 && (i & 1);
+        const h2_t h = __builtin_bit_cast(h2_t, v_codes<W, i % kIn>(t.v[2 * j][i / kIn], t.v[2 * j + 1][i / kIn]));
+        h2_t y;
+        y[0] = static_cast<_Float16>(__builtin_fmaf(static_cast<float>(h[0]), odd ? x.odd[2 * j] : x.s[2 * j], x.m[2 * j]));
+        y[1] = static_cast<_Float16>(__builtin_fmaf(static_cast<float>(h[1]), odd ? x.odd[2 * j + 1] : x.s[2 * j + 1], x.m[2 * j + 1]));
+        return __builtin_bit_cast(uint32_t, y);
     }
 }
 
-template <int D, int G, int W, int NT, int i = 0>
-__device__ __forceinline__ void tile_values(const TileRegs<D, G, W>* t, u4_t p, RowState<D>& st) {
-    u4_t a;
-    a.x = v_pair<D, G, W, i>(t[0], 0);
-    a.y = v_pair<D, G, W, i>(t[0], 1);
-    a.z = NT == 2 ? v_pair<D, G, W, i>(t[NT - 1], 0) : 0u;
-    a.w = NT == 2 ? v_pair<D, G, W, i>(t[NT - 1], 1) : 0u;
-    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), as_h8(p), st.o[i], 0, 0, 0);
-    if constexpr (i + 1 < D / 16) tile_values<D, G, W, NT, i + 1>(t, p, st);
+// O^T += V^T P^T of a unit, dimension by dimension; P as the sum of two halves.
+template <int D, int G, int W, bool HP, int i = 0>
+__device__ __forceinline__ void unit_values(const VRegs<D, G, W, HP>* t, const VScale<W>* x, const h8_t& hi, const h8_t& lo, RowState<D>& st) {
+    const u4_t a = {v_pair<D, G, W, HP, i>(t[0], x[0], 0), v_pair<D, G, W, HP, i>(t[0], x[0], 1),
+                    v_pair<D, G, W, HP, i>(t[1], x[1], 0), v_pair<D, G, W, HP, i>(t[1], x[1], 1)};
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), lo, st.o[i], 0, 0, 0);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), hi, st.o[i], 0, 0, 0);
+    if constexpr (i + 1 < D / 16) unit_values<D, G, W, HP, i + 1>(t, x, hi, lo, st);
 }
 
 // What a wavefront knows of its rows.
-template <int D> struct RowsOfWave {
-    u4_t q[D / 32];
-    float qsum[D / 64 > 0 ? D / 64 : 1];       // of every group, the row's sum of q (as many groups as there are at most)
+template <int D, int G> struct RowsOfWave {
+    u4_t q[D / 32];                            // the lane's pieces, dimensions in memory order
+    float qsum[D / G];                         // of every group, the row's sum of q
     int last;                                  // the last token the lane's row sees (-1: none)
     int all_see;                               // tokens up to this one are seen by every row
     float* logits;                             // where the row's logits go (NULL: nowhere)
+    float scale;
 };
 
-// One or two tiles of one width.  first[]: the tiles' first tokens.
-template <int D, int G, int W, int NT>
-__device__ __forceinline__ void unit(const uint8_t* const* record, const int* in_page, const int* first, int n, const PagesView& v, int k_slab,
-                                     float scale, const RowsOfWave<D>& rw, RowState<D>& st, int lane) {
-    const int q4 = lane >> 4;
-    TileRegs<D, G, W> t[NT];
+// A wavefront's batch of up to 64 tiles, one per lane.
+struct TileBatch {
+    uint32_t off_lo, off_hi;                   // the page's offset
+    int in_page;                               // the tile's first row there
+    int unit0;                                 // tile of lane l: 2 * (unit0 + kAttendWaves * (l / 2)) + l % 2
+};
+
+__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// The next two of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time behind every row's last
+// token.
+__device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, int n, uint8_t* pool, Tile* tile) {
+    int at = __builtin_ctzll(tiles);
 #pragma unroll
-    for (int k = 0; k < NT; ++k) tile_load<D, G, W>(t[k], record[k], v, k_slab, in_page[k], min(16, n - first[k]), lane);
-    f4_t s[NT];
-    float top = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < NT; ++k) {
-        s[k] = tile_logits<D, G, W>(t[k], rw.q, rw.qsum, scale);
-        if (first[k] + 15 > rw.all_see) {                                // (uniform)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[k][r] = first[k] + 4 * q4 + r <= rw.last ? s[k][r] : -INFINITY;
-        }
-        if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + first[k] + 4 * q4) = s[k];
-        top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
+    for (int k = 0; k < 2; ++k) {
+        if (k) at = tiles ? __builtin_ctzll(tiles) : at;
+        const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(lane_value(static_cast<int>(tb.off_hi), at))) << 32 |
+                             static_cast<uint32_t>(lane_value(static_cast<int>(tb.off_lo), at));
+        tile[k].record = pool + off;
+        tile[k].in_page = lane_value(tb.in_page, at);
+        const int first = 16 * (2 * (tb.unit0 + kAttendWaves * (at >> 1)) + (at & 1));
+        tile[k].valid = min(16, n - first);
+        tile[k].first = k && !tiles ? kNowhere : first;
+        tiles &= tiles - 1;                                              // (0 stays 0)
     }
-    if (__ballot(top > st.ref + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        if (top > st.ref + kSlack) {
-            const float to = top - kTop, f = __builtin_amdgcn_exp2f(st.ref - to);
-            st.ref = to;
-            st.sum *= f;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
-        }
-    }
-    const float ref = st.ref == -INFINITY ? 0.0f : st.ref;               // (a row that has seen nothing: every logit is -inf)
-    h8_t p = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < NT; ++k)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float e = __builtin_amdgcn_exp2f(s[k][r] - ref);
-            st.sum += e;
-            p[4 * k + r] = static_cast<_Float16>(e);
-        }
-    tile_values<D, G, W, NT>(t, __builtin_bit_cast(u4_t, p), st);
 }
 
-template <int D, int G, int NT>
-__device__ __forceinline__ void unit_of_width(int b, const uint8_t* const* record, const int* in_page, const int* first, int n, const PagesView& v,
-                                              int k_slab, float scale, const RowsOfWave<D>& rw, RowState<D>& st, int lane) {
-    if (b == 16) unit<D, G, 16, NT>(record, in_page, first, n, v, k_slab, scale, rw, st, lane);
-    else if (b == 8) unit<D, G, 8, NT>(record, in_page, first, n, v, k_slab, scale, rw, st, lane);
-    else if (b == 4) unit<D, G, 4, NT>(record, in_page, first, n, v, k_slab, scale, rw, st, lane);
-    else unit<D, G, 2, NT>(record, in_page, first, n, v, k_slab, scale, rw, st, lane);
+// The tiles of width W among a batch, two at a time.  The order of tokens does not matter to attention, so tiles are paired by width,
+// whatever the order of the pages.  K of the next pair is loaded once K of this one has been used, and V likewise: the loads are in
+// flight during the other half of the arithmetic, without a second set of registers.
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, int k_slab,
+                                     const RowsOfWave<D, G>& rw, RowState<D>& st, int lane) {
+    if (!tiles) return;
+    const int q4 = lane >> 4;
+    const SlabAt ka = slab_at<D>(v, W, k_slab), va = slab_at<D>(v, W, k_slab + v.Hkv);
+    u4_t q[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        const uint32_t ws[4] = {rw.q[i].x, rw.q[i].y, rw.q[i].z, rw.q[i].w};
+        q[i] = W == 16 ? rw.q[i] : paired(ws);
+    }
+    KRegs<D, G, W, HP> kr[2];
+    VRegs<D, G, W, HP> vr[2];
+    Tile tile[2], next[2];
+    next_pair(tiles, tb, n, v.pool, next);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], va, lane);
+    bool more = true;
+    while (more) {
+        f4_t s[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            tile[k] = next[k];
+            s[k] = tile_logits<D, G, W, HP>(kr[k], q, rw.qsum, rw.scale);
+            if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[k][r] = tile[k].first + 4 * q4 + r <= rw.last ? s[k][r] : -INFINITY;
+            }
+            if (rw.logits && tile[k].first != kNowhere) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k];
+            top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
+        }
+        more = tiles != 0;
+        if (more) {
+            next_pair(tiles, tb, n, v.pool, next);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
+        }
+        if (__ballot(top > st.ref + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (top > st.ref + kSlack) {
+                const float to = top - kTop, f = __builtin_amdgcn_exp2f(st.ref - to);
+                st.ref = to;
+                st.sum *= f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
+            }
+        }
+        const float ref = st.ref == -INFINITY ? 0.0f : st.ref;           // (a row that has seen nothing: every logit is -inf)
+        h8_t hi, lo;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float e = __builtin_amdgcn_exp2f(s[k][r] - ref);
+                st.sum += e;
+                hi[4 * k + r] = static_cast<_Float16>(e);
+                lo[4 * k + r] = static_cast<_Float16>(e - static_cast<float>(hi[4 * k + r]));
+            }
+        VScale<W> x[2];
+        if constexpr (W != 16) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) x[k] = v_scale<D, G, W, HP>(vr[k], tile[k].valid, lane);
+        }
+        unit_values<D, G, W, HP>(vr, x, hi, lo, st);
+        if (more) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], va, lane);
+        }
+    }
 }
 
 // One share of a (sequence, kv head, row tile): grid splits * row_tiles * kv heads * sequences, the shares of a pair side by side.
 // The wavefronts of a workgroup take the share's units in turn, each with a state of its own; the four states meet in LDS.
-template <int D, int G>
-__global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
+template <int D, int G, bool HP>
+__global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                    float* __restrict__ logits) {
     constexpr int DL = D / 16, NG = D / G;
-    __shared__ float o_lds[kAttendWaves][16][D];
+    extern __shared__ float o_lds[];                 // [kAttendWaves][min(16, rows of a pair)][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
+    const int tile_rows = min(16, g.rows);
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     uint32_t id = blockIdx.x;
@@ -347,7 +401,8 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
     // this lane's query row
     const int j = rt * 16 + l16, nth = j / g.per, head = h * g.per + j % g.per;
     const bool ok = j < count * g.per;
-    RowsOfWave<D> rw;
+    RowsOfWave<D, G> rw;
+    rw.scale = g.scale_log2e;
     rw.last = ok ? n - rows.count + nth : -1;
     rw.all_see = n - rows.count + rt * 16 / g.per;
     const int64_t pair = static_cast<int64_t>(s) * v.Hkv + h;
@@ -364,8 +419,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
                 const h8_t x = as_h8(w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += static_cast<float>(x[e]);
-                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-                rw.q[gi * (G / 32) + i] = k_operand<16>(ws);
+                rw.q[gi * (G / 32) + i] = w;
             }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
@@ -382,48 +436,28 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
     const int u_end = min((n + 31) >> 5, (share + 1) * sh.units);          // (none for an empty sequence)
     const uint64_t* offs = v.off + static_cast<int64_t>(s) * v.stride;
     const uint8_t* bits = v.bits + static_cast<int64_t>(s) * v.stride;
-    const int tiles_per_page = v.T >> 4;
-    // the pages of the wavefront's next 32 units, a tile per lane: offset, and width (0: absent or behind the end)
-    uint32_t off_lo = 0, off_hi = 0, width = 0;
-    auto look_up = [&](int u) {
-        const int tile = min(2 * (u + kAttendWaves * (lane >> 1)) + (lane & 1), (n - 1) >> 4);
-        const int page = v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile;
+    for (int u = share * sh.units + wave; u < u_end; u += 32 * kAttendWaves) {
+        // the pages of the wavefront's next 32 units, a tile per lane
+        TileBatch tb;
+        tb.unit0 = u;
+        const int unit = u + kAttendWaves * (lane >> 1), tile = 2 * unit + (lane & 1);
+        const bool in = unit < u_end && tile * 16 < n;
+        const int page = !in ? 0 : (v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile);
         const uint64_t off = offs[page];
         const uint32_t b = bits[page];
-        off_lo = static_cast<uint32_t>(off);
-        off_hi = static_cast<uint32_t>(off >> 32);
-        width = page_present(v, off, b) ? b : 0u;
-    };
-    int ahead = 0;                                    // units looked up and not yet walked
-    for (int u = share * sh.units + wave; u < u_end; u += kAttendWaves) {
-        if (ahead == 0) {
-            look_up(u);
-            ahead = 32;
-        }
-        const uint8_t* record[2];
-        int in_page[2], first[2], b[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = 2 * (32 - ahead) + k, tile = 2 * u + k;
-            const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off_hi), at))) << 32 |
-                                 static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(off_lo), at));
-            const int page = v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile;
-            first[k] = tile * 16;
-            b[k] = first[k] < n ? __builtin_amdgcn_readlane(static_cast<int>(width), at) : 0;
-            record[k] = v.pool + off;
-            in_page[k] = (tile - page * tiles_per_page) * 16;
-        }
-        --ahead;
-        if (b[0] == b[1]) {
-            if (b[0]) unit_of_width<D, G, 2>(b[0], record, in_page, first, n, v, k_slab, g.scale_log2e, rw, st, lane);
-        } else {
-            if (b[0]) unit_of_width<D, G, 1>(b[0], record, in_page, first, n, v, k_slab, g.scale_log2e, rw, st, lane);
-            if (b[1]) unit_of_width<D, G, 1>(b[1], record + 1, in_page + 1, first + 1, n, v, k_slab, g.scale_log2e, rw, st, lane);
-        }
-        if (rw.logits) {                             // what an absent tile would have had
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-                if (!b[k] && first[k] < n) *reinterpret_cast<f4_t*>(rw.logits + first[k] + 4 * q4) = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        const uint32_t width = in && page_present(v, off, b) ? b : 0u;
+        tb.off_lo = static_cast<uint32_t>(off);
+        tb.off_hi = static_cast<uint32_t>(off >> 32);
+        tb.in_page = tile * 16 - page * v.T;
+        walk<D, G, 16, HP>(__ballot(width == 16), tb, n, v, k_slab, rw, st, lane);
+        walk<D, G, 8, HP>(__ballot(width == 8), tb, n, v, k_slab, rw, st, lane);
+        walk<D, G, 4, HP>(__ballot(width == 4), tb, n, v, k_slab, rw, st, lane);
+        walk<D, G, 2, HP>(__ballot(width == 2), tb, n, v, k_slab, rw, st, lane);
+        if (logits) {                                // what the tokens of absent tiles would have had
+            for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
+                const int at = __builtin_ctzll(none), first = 16 * (2 * (u + kAttendWaves * (at >> 1)) + (at & 1));
+                if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + first + 4 * q4) = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            }
         }
     }
     // the four states against one reference per row
@@ -438,7 +472,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < DL; i += 4)
-                *reinterpret_cast<f4_t*>(&o_lds[wave][l16][DL * (4 * q4 + r) + i]) = f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
+                *reinterpret_cast<f4_t*>(o_lds + (wave * tile_rows + l16) * D + DL * (4 * q4 + r) + i) = f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
     }
     __syncthreads();
     const int here = min(16, count * g.per - rt * 16);                   // rows of this tile
@@ -452,7 +486,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
         for (int k = 0; k < kAttendWaves; ++k) {
             const float m = ml_lds[k][0][row], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
             sum += f * ml_lds[k][1][row];
-            o += *reinterpret_cast<const f4_t*>(&o_lds[k][row][d]) * f;
+            o += *reinterpret_cast<const f4_t*>(o_lds + (k * tile_rows + row) * D + d) * f;
         }
         const int jr = rt * 16 + row;
         if (part_ml && d == 0) {
@@ -473,48 +507,78 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
     }
 }
 
-// Reference and sum of a row over its shares, taken in ascending order.
-__device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int64_t first, int used, int rows, float& ref, float& sum) {
+// Reference and sum of a row over its shares, by all lanes of a wavefront together; weight[k] the factor of share k.
+__device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int64_t first, int used, int rows, int lane, float* weight,
+                                          float& ref, float& sum) {
+    float m[kMaxSplits / 64], l[kMaxSplits / 64];
     ref = -INFINITY;
-    sum = 0.0f;
-    for (int k = 0; k < used; ++k) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * rows) * 2]);
-    for (int k = 0; k < used; ++k) {
-        const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * rows) * 2);
-        sum += ml.x == -INFINITY ? 0.0f : ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+        const int k = i * 64 + lane;
+        m[i] = -INFINITY;
+        l[i] = 0.0f;
+        if (k < used) {
+            const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * rows) * 2);
+            m[i] = ml.x;
+            l[i] = ml.y;
+        }
+        ref = fmaxf(ref, m[i]);
     }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / 64; ++i) {
+        const int k = i * 64 + lane;
+        const float f = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - ref);
+        if (weight && k < used) weight[k] = f;
+        sum += f * l[i];
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
 }
 
-// Joins the shares of the pairs whose tokens were divided: one thread per four channels of a row.
+// Joins the shares of a row whose tokens were divided: one workgroup per row, its threads four channels and every
+// (1024 / D)-th share each.
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(PagesView v, AttendGeom g, const int32_t* __restrict__ row_start,
                                                           const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                           _Float16* __restrict__ out) {
-    constexpr int kQuads = D / 4;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int d = static_cast<int>(i % kQuads) * 4;
-    const int64_t row = i / kQuads;
-    const int64_t pair = row / g.rows;
-    const int j = static_cast<int>(row - pair * g.rows);
+    constexpr int kQuads = D / 4, kParts = 256 / kQuads;
+    __shared__ float weight[kMaxSplits];
+    __shared__ float total;
+    __shared__ f4_t o_lds[kParts][kQuads];
+    const int lane = threadIdx.x & 63;
+    const int64_t pair = blockIdx.x / g.rows;
+    const int j = static_cast<int>(blockIdx.x - pair * g.rows);
     const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair - static_cast<int64_t>(s) * v.Hkv);
-    if (s >= v.n_seqs) return;
     const SeqRows rows = seq_rows(row_start, s, g.n_rows);
     const int n = seq_len(v, s), count = min(rows.count, g.max_rows);
     const Shares sh = shares_of(g, n);
     if (sh.used <= 1 || j >= count * g.per) return;
     const int64_t first = pair * g.splits * g.rows + j;
-    float ref, sum;
-    row_total(part_ml, first, sh.used, g.rows, ref, sum);
-    f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < sh.used; ++k) {
-        const int64_t at = first + static_cast<int64_t>(k) * g.rows;
-        const float m = part_ml[at * 2], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
-        o += *reinterpret_cast<const f4_t*>(part_o + at * D + d) * f;
+    const int quad = threadIdx.x % kQuads, part = threadIdx.x / kQuads;
+    if (threadIdx.x < 64) {
+        float ref, sum;
+        row_total(part_ml, first, sh.used, g.rows, lane, weight, ref, sum);
+        if (lane == 0) total = sum;
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    __syncthreads();
+    f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f4_t* src = reinterpret_cast<const f4_t*>(part_o + first * D) + quad;
+    const int64_t step = static_cast<int64_t>(g.rows) * kQuads;
+#pragma unroll 4
+    for (int k = part; k < sh.used; k += kParts) o += src[k * step] * weight[k];
+    o_lds[part][quad] = o;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int k = 1; k < kParts; ++k) o += o_lds[k][quad];
+    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
     h4_t x;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
-    *reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(rows.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D + d) = x;
+    reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(rows.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D)[quad] = x;
 }
 
 // The weights of a pair's keys, from the logits its rows left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
@@ -532,11 +596,14 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(PagesView v, AttendGeo
     const int count = min(rows.count, g.max_rows) * g.per;
     if (count == 0) return;
     const Shares sh = shares_of(g, n);
-    for (int j = threadIdx.x; j < count; j += 256) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    for (int j = wave; j < count; j += 4) {
         float ref, sum;
-        row_total(part_ml, pair * g.splits * g.rows + j, sh.used, g.rows, ref, sum);
-        refs[j] = sum > 0.0f ? ref : 0.0f;                       // (a row that sees nothing weighs nothing: its logits are -inf)
-        invs[j] = sum > 0.0f ? 1.0f / sum : 0.0f;
+        row_total(part_ml, pair * g.splits * g.rows + j, sh.used, g.rows, lane, nullptr, ref, sum);
+        if (lane == 0) {
+            refs[j] = sum > 0.0f ? ref : 0.0f;                   // (a row that sees nothing weighs nothing: its logits are -inf)
+            invs[j] = sum > 0.0f ? 1.0f / sum : 0.0f;
+        }
     }
     __syncthreads();
     const int t = t0 + static_cast<int>(threadIdx.x) * 4;

@@ -203,9 +203,9 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
         return fail(KV_ENOMEM, "workspace of %llu bytes, %llu needed", static_cast<unsigned long long>(workspace_bytes),
                     static_cast<unsigned long long>(w.all));
     const int64_t pairs = static_cast<int64_t>(pages->n_seqs) * shape->n_kv_heads;
-    const int64_t groups = pairs * g.row_tiles * g.splits, quads = pairs * g.rows * (shape->head_dim / 4);
+    const int64_t groups = pairs * g.row_tiles * g.splits;
     const int32_t blocks = (shape->n_tokens + 1023) / 1024;
-    if (groups > 0x7fffffffLL || (quads + 255) / 256 > 0x7fffffffLL || pairs * blocks > 0x7fffffffLL)
+    if (groups > 0x7fffffffLL || pairs * g.rows > 0x7fffffffLL || pairs * blocks > 0x7fffffffLL)
         return fail(KV_ESHAPE, "attention grid exceeds 2^31 workgroups");
     const PagesView view = pages_view(*shape, *pages);
     uint8_t* space = static_cast<uint8_t*>(workspace);
@@ -216,7 +216,14 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     const _Float16* q16 = static_cast<const _Float16*>(q);
     _Float16* o16 = static_cast<_Float16*>(out);
     const dim3 grid(static_cast<uint32_t>(groups)), block(64 * kAttendWaves);
-#define KV_LAUNCH(D, G) hipLaunchKernelGGL((attend_kernel<D, G>), grid, block, 0, st, view, g, q16, row_start, o16, part_o, part_ml, logits)
+    const uint32_t lds = static_cast<uint32_t>(kAttendWaves * std::min(16, g.rows) * shape->head_dim) * 4;   // at most 64 KB
+#define KV_LAUNCH(D, G)                                                                                                                       \
+    do {                                                                                                                                      \
+        if (view.half_params)                                                                                                                 \
+            hipLaunchKernelGGL((attend_kernel<D, G, true>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits);     \
+        else                                                                                                                                  \
+            hipLaunchKernelGGL((attend_kernel<D, G, false>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits);    \
+    } while (0)
     switch (shape->head_dim * 1024 + shape->group) {
         case 64 * 1024 + 64: KV_LAUNCH(64, 64); break;
         case 128 * 1024 + 64: KV_LAUNCH(128, 64); break;
@@ -228,7 +235,7 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
 #undef KV_LAUNCH
     if (int rc = launch_status("attend_kernel launch")) return rc;
     if (g.splits > 1) {
-        const dim3 join(static_cast<uint32_t>((quads + 255) / 256));
+        const dim3 join(static_cast<uint32_t>(pairs * g.rows));
 #define KV_LAUNCH(D) hipLaunchKernelGGL((attend_join_kernel<D>), join, dim3(256), 0, st, view, g, row_start, part_o, part_ml, o16)
         KV_BY_HEAD_DIM(shape->head_dim, KV_LAUNCH);
 #undef KV_LAUNCH

@@ -65,9 +65,10 @@ inline int append_pieces_per_lane(int64_t n_rows, int pieces) { return n_rows * 
 
 // Shares that the tokens of a (sequence, kv head, row tile) are divided among, `groups` of these and at most `tokens` tokens each.
 constexpr int kAttendMinUnits = 4;          // units of 32 tokens of a share: one per wavefront
+constexpr int kAttendMaxSplits = 256;
 inline int64_t attend_splits(int64_t groups, int64_t tokens) {
     const int64_t units = (tokens + 31) / 32, most = std::max<int64_t>(1, units / kAttendMinUnits);
-    return std::max<int64_t>(1, std::min<int64_t>({most, std::max<int64_t>(1024 / groups, (tokens + 4095) / 4096), 256}));
+    return std::max<int64_t>(1, std::min<int64_t>({most, std::max<int64_t>(1024 / groups, (tokens + 4095) / 4096), kAttendMaxSplits}));
 }
 
 // Eviction: workgroups that share a pair's moves, `rows` at a time each.
