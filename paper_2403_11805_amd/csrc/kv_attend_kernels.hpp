@@ -27,7 +27,6 @@ typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 h4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kAttendWaves = 4;
-constexpr int kMaxSplits = kAttendMaxSplits;
 constexpr float kTop = 7.0f;         // a row's reference is set 2^7 below its largest logit so far ...
 constexpr float kSlack = 15.0f;      // ... and moves when a logit passes 2^15 above it: probabilities stay in fp16's range, and those
                                      // 2^-31 below the largest still count
@@ -38,22 +37,102 @@ struct AttendGeom {
     int32_t per;                     // query heads per kv head
     int32_t rows;                    // per * max_rows: query rows of a (sequence, kv head) pair
     int32_t row_tiles;               // ceil(rows / 16)
-    int32_t splits;                  // shares a pair's tokens are divided among at most
-    int32_t min_units;               // units of a share at least
+    int32_t tile_rows;               // min(16, rows)
+    int32_t groups;                  // workgroups that the work of all sequences is divided among
     int64_t q_stride;
     float scale_log2e;               // log2(e) / sqrt(D)
 };
 
-// Shares of a sequence of n tokens: `units` units each, `used` of them.
-struct Shares {
-    int units, used;
+// How the work is divided.  The units of all sequences, kv heads and row tiles stand in one line (sequence by sequence, head by head),
+// and every workgroup takes an equal run of it, whatever the lengths are: all run at once and end together, and a run goes on
+// through the next head or sequence where one ends.  In front of the units of every (kv head, row tile) pair the line has kPieceCost
+// places for what beginning and ending a piece takes, so that runs through many short ones are shorter.  The lengths are on the
+// device, so a workgroup finds its run itself, a lane per sequence, 64 sequences a step.
+constexpr int kPieceCost = 8;
+struct SeqWork {
+    int n, first, count;             // tokens; its new rows
+    int units, pairs;                // units of 32 tokens; (kv head, row tile) pairs, none without rows
+    __device__ __forceinline__ int each() const { return units ? units + kPieceCost : 0; }     // places of a pair
 };
-__device__ __forceinline__ Shares shares_of(const AttendGeom& g, int n) {
-    const int all = (n + 31) >> 5;
-    Shares s;
-    s.units = max((all + g.splits - 1) / g.splits, g.min_units);
-    s.used = (all + s.units - 1) / s.units;
-    return s;
+__device__ __forceinline__ SeqWork work_of(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int s) {
+    SeqWork w = {0, 0, 0, 0, 0};
+    if (s < v.n_seqs) {
+        w.n = seq_len(v, s);
+        const SeqRows rows = seq_rows(row_start, s, g.n_rows);
+        w.first = rows.first;
+        w.count = rows.count;
+        w.units = (w.n + 31) >> 5;
+        w.pairs = v.Hkv * ((min(w.count, g.max_rows) * g.per + 15) >> 4);
+    }
+    return w;
+}
+__device__ __forceinline__ SeqWork of_lane(const SeqWork& w, int l) {
+    return {__builtin_amdgcn_readlane(w.n, l), __builtin_amdgcn_readlane(w.first, l), __builtin_amdgcn_readlane(w.count, l),
+            __builtin_amdgcn_readlane(w.units, l), __builtin_amdgcn_readlane(w.pairs, l)};
+}
+
+// Where the lanes' sequences lie in the line.
+struct Line {
+    SeqWork mine;                    // of sequence s0 + lane
+    int s0, end;                     // end: of the lane's sequence
+    int run;                         // units of a workgroup's run
+
+    __device__ __forceinline__ void step(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane, int before) {
+        end = mine.each() * mine.pairs;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int x = __shfl_up(end, d);
+            end += lane >= d ? x : 0;
+        }
+        end += before;
+    }
+    __device__ __forceinline__ void start(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
+        s0 = 0;
+        mine = work_of(v, g, row_start, lane);
+        step(v, g, row_start, lane, 0);
+        int total = __builtin_amdgcn_readlane(end, 63);
+        for (int s = 64; s < v.n_seqs; s += 64) {
+            const SeqWork w = work_of(v, g, row_start, s + lane);
+            int x = w.each() * w.pairs;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+            total += x;
+        }
+        run = __builtin_amdgcn_readfirstlane(max(kAttendMinUnits + kPieceCost, (total + g.groups - 1) / g.groups));
+    }
+    __device__ __forceinline__ void next(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
+        const int before = __builtin_amdgcn_readlane(end, 63);
+        s0 += 64;
+        mine = work_of(v, g, row_start, s0 + lane);
+        step(v, g, row_start, lane, before);
+    }
+};
+
+// Partial results: a workgroup leaves those of pair p (numbered over all sequences) at slot workgroup + p, which no other has: from one
+// piece of the line to the next the workgroup, the pair or both go up.
+__device__ __forceinline__ int64_t pair_number(const PagesView& v, const AttendGeom& g, int s, int pair) {
+    return static_cast<int64_t>(s) * v.Hkv * g.row_tiles + pair;
+}
+
+// The shares of row j of (sequence s, kv head h): `used` slots from `first` on.
+struct RowShares {
+    SeqWork w;
+    int used;
+    int64_t first;
+};
+__device__ __forceinline__ RowShares row_shares(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane, int s,
+                                                int h, int j) {
+    Line line;
+    line.start(v, g, row_start, lane);
+    while (s >= line.s0 + 64) line.next(v, g, row_start, lane);
+    const int l = s - line.s0;
+    RowShares x;
+    x.w = of_lane(line.mine, l);
+    const int row_tiles = x.w.pairs / v.Hkv, pair = h * row_tiles + j / 16;
+    const int begin = __builtin_amdgcn_readlane(line.end, l) - x.w.each() * (x.w.pairs - pair) + kPieceCost, wg = begin / line.run;
+    x.used = x.w.units ? (begin + x.w.units - 1) / line.run - wg + 1 : 0;
+    x.first = wg + pair_number(v, g, s, pair);
+    return x;
 }
 
 __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
@@ -248,14 +327,21 @@ __device__ __forceinline__ uint32_t v_pair(const VRegs<D, G, W, HP>& t, const VS
     }
 }
 
-// O^T += V^T P^T of a unit, dimension by dimension; P as the sum of two halves.
+// O^T += V^T P^T of a unit, two dimensions at a time (an MFMA that adds to the sum of the one right before it would wait for it); P as
+// the sum of two halves.
+template <int D, int G, int W, bool HP, int i>
+__device__ __forceinline__ h8_t v_operand(const VRegs<D, G, W, HP>* t, const VScale<W>* x) {
+    return as_h8(u4_t{v_pair<D, G, W, HP, i>(t[0], x[0], 0), v_pair<D, G, W, HP, i>(t[0], x[0], 1),
+                      v_pair<D, G, W, HP, i>(t[1], x[1], 0), v_pair<D, G, W, HP, i>(t[1], x[1], 1)});
+}
 template <int D, int G, int W, bool HP, int i = 0>
 __device__ __forceinline__ void unit_values(const VRegs<D, G, W, HP>* t, const VScale<W>* x, const h8_t& hi, const h8_t& lo, RowState<D>& st) {
-    const u4_t a = {v_pair<D, G, W, HP, i>(t[0], x[0], 0), v_pair<D, G, W, HP, i>(t[0], x[0], 1),
-                    v_pair<D, G, W, HP, i>(t[1], x[1], 0), v_pair<D, G, W, HP, i>(t[1], x[1], 1)};
-    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), lo, st.o[i], 0, 0, 0);
-    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), hi, st.o[i], 0, 0, 0);
-    if constexpr (i + 1 < D / 16) unit_values<D, G, W, HP, i + 1>(t, x, hi, lo, st);
+    const h8_t a = v_operand<D, G, W, HP, i>(t, x), b = v_operand<D, G, W, HP, i + 1>(t, x);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, lo, st.o[i], 0, 0, 0);
+    st.o[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, lo, st.o[i + 1], 0, 0, 0);
+    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, hi, st.o[i], 0, 0, 0);
+    st.o[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hi, st.o[i + 1], 0, 0, 0);
+    if constexpr (i + 2 < D / 16) unit_values<D, G, W, HP, i + 2>(t, x, hi, lo, st);
 }
 
 // What a wavefront knows of its rows.
@@ -268,11 +354,11 @@ template <int D, int G> struct RowsOfWave {
     float scale;
 };
 
-// A wavefront's batch of up to 64 tiles, one per lane.
+// A workgroup's batch of up to 64 tiles, one per lane of each of its wavefronts.
 struct TileBatch {
     uint32_t off_lo, off_hi;                   // the page's offset
     int in_page;                               // the tile's first row there
-    int unit0;                                 // tile of lane l: 2 * (unit0 + kAttendWaves * (l / 2)) + l % 2
+    int tile0;                                 // lane l has tile tile0 + l
 };
 
 __device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
@@ -288,7 +374,7 @@ __device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, 
                              static_cast<uint32_t>(lane_value(static_cast<int>(tb.off_lo), at));
         tile[k].record = pool + off;
         tile[k].in_page = lane_value(tb.in_page, at);
-        const int first = 16 * (2 * (tb.unit0 + kAttendWaves * (at >> 1)) + (at & 1));
+        const int first = 16 * (tb.tile0 + at);
         tile[k].valid = min(16, n - first);
         tile[k].first = k && !tiles ? kNowhere : first;
         tiles &= tiles - 1;                                              // (0 stays 0)
@@ -296,11 +382,14 @@ __device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, 
 }
 
 // The tiles of width W among a batch, two at a time.  The order of tokens does not matter to attention, so tiles are paired by width,
-// whatever the order of the pages.  K of the next pair is loaded once K of this one has been used, and V likewise: the loads are in
+// whatever the order of the pages, and the pairs (`dealt` of them of other widths so far) go to the wavefronts in turn.  K of the next pair is loaded once K of this one has been used, and V likewise: the loads are in
 // flight during the other half of the arithmetic, without a second set of registers.
 template <int D, int G, int W, bool HP>
 __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, int k_slab,
-                                     const RowsOfWave<D, G>& rw, RowState<D>& st, int lane) {
+                                     const RowsOfWave<D, G>& rw, RowState<D>& st, int wave, int lane, int& dealt) {
+    const int skip = (wave - dealt) & (kAttendWaves - 1);
+    dealt += (__builtin_popcountll(tiles) + 1) / 2;
+    for (int i = 0; i < 2 * skip; ++i) tiles &= tiles - 1;
     if (!tiles) return;
     const int q4 = lane >> 4;
     const SlabAt ka = slab_at<D>(v, W, k_slab), va = slab_at<D>(v, W, k_slab + v.Hkv);
@@ -313,7 +402,12 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
     KRegs<D, G, W, HP> kr[2];
     VRegs<D, G, W, HP> vr[2];
     Tile tile[2], next[2];
-    next_pair(tiles, tb, n, v.pool, next);
+    auto take = [&] {
+        next_pair(tiles, tb, n, v.pool, next);
+#pragma unroll
+        for (int i = 0; i < 2 * (kAttendWaves - 1); ++i) tiles &= tiles - 1;      // the other wavefronts'
+    };
+    take();
 #pragma unroll
     for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
 #pragma unroll
@@ -335,7 +429,7 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
         }
         more = tiles != 0;
         if (more) {
-            next_pair(tiles, tb, n, v.pool, next);
+            take();
 #pragma unroll
             for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
         }
@@ -374,41 +468,49 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
     }
 }
 
-// One share of a (sequence, kv head, row tile): grid splits * row_tiles * kv heads * sequences, the shares of a pair side by side.
-// The wavefronts of a workgroup take the share's units in turn, each with a state of its own; the four states meet in LDS.
+// Grid: g.groups workgroups, each a run of the line.  The wavefronts of a workgroup take the pairs of tiles of a piece of the run (the part
+// that lies in one sequence, kv head and row tile) in turn, each with a state of its own; the four states meet in LDS.
 template <int D, int G, bool HP>
 __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                    float* __restrict__ logits) {
     constexpr int DL = D / 16, NG = D / G;
-    extern __shared__ float o_lds[];                 // [kAttendWaves][min(16, rows of a pair)][D]
+    extern __shared__ float o_lds[];                 // [kAttendWaves][tile_rows][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
-    const int tile_rows = min(16, g.rows);
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    uint32_t id = blockIdx.x;
-    const int share = static_cast<int>(id % g.splits);
-    id /= g.splits;
-    const int rt = static_cast<int>(id % g.row_tiles);
-    id /= g.row_tiles;
-    const int h = static_cast<int>(id % v.Hkv), s = static_cast<int>(id / v.Hkv);
-    const SeqRows rows = seq_rows(row_start, s, g.n_rows);
-    const int n = seq_len(v, s), count = min(rows.count, g.max_rows);
-    const Shares sh = shares_of(g, n);
-    if (share >= max(sh.used, 1) || rt * 16 >= count * g.per) return;    // (an empty sequence: its first share writes zeros)
+    Line line;
+    line.start(v, g, row_start, lane);
+    int at = static_cast<int>(blockIdx.x) * line.run;
+    const int run_end = at + line.run;
+    while (at < run_end) {
+        // the piece that begins at `at`: its sequence, pair and units
+        uint64_t behind = __ballot(line.end > at);
+        while (!behind && line.s0 + 64 < v.n_seqs) {
+            line.next(v, g, row_start, lane);
+            behind = __ballot(line.end > at);
+        }
+        if (!behind) return;                         // (the end of the line; uniform in the workgroup)
+        const int l = __builtin_ctzll(behind), s = line.s0 + l;
+        const SeqWork sw = of_lane(line.mine, l);
+        const int n = sw.n, local = at - (__builtin_amdgcn_readlane(line.end, l) - sw.each() * sw.pairs);
+        const int pair = local / sw.each(), place = local - pair * sw.each(), places = min(sw.each() - place, run_end - at);
+        const int u_begin = max(place - kPieceCost, 0), u_end = place + places - kPieceCost;
+        const int row_tiles = sw.pairs / v.Hkv, h = pair / row_tiles, rt = pair - h * row_tiles;
+        const int count = min(sw.count, g.max_rows);
+        at += places;
+        if (u_end <= u_begin) continue;              // the run ends in front of the pair's first unit
 
-    // this lane's query row
-    const int j = rt * 16 + l16, nth = j / g.per, head = h * g.per + j % g.per;
-    const bool ok = j < count * g.per;
-    RowsOfWave<D, G> rw;
-    rw.scale = g.scale_log2e;
-    rw.last = ok ? n - rows.count + nth : -1;
-    rw.all_see = n - rows.count + rt * 16 / g.per;
-    const int64_t pair = static_cast<int64_t>(s) * v.Hkv + h;
-    rw.logits = logits && ok ? logits + (pair * g.rows + j) * v.N : nullptr;
-    {
-        const _Float16* qp = q + static_cast<int64_t>(rows.first + (ok ? nth : 0)) * g.q_stride + head * (ok ? 1 : 0) * D;
+        // this lane's query row
+        const int j = rt * 16 + l16, nth = j / g.per, head = h * g.per + j % g.per;
+        const bool ok = j < count * g.per;
+        RowsOfWave<D, G> rw;
+        rw.scale = g.scale_log2e;
+        rw.last = ok ? n - sw.count + nth : -1;
+        rw.all_see = n - sw.count + rt * 16 / g.per;
+        rw.logits = logits && ok ? logits + ((static_cast<int64_t>(s) * v.Hkv + h) * g.rows + j) * v.N : nullptr;
+        const _Float16* qp = q + static_cast<int64_t>(sw.first + (ok ? nth : 0)) * g.q_stride + (ok ? head : 0) * D;
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi) {
             float sum = 0.0f;
@@ -425,148 +527,133 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_ke
             sum += __shfl_xor(sum, 32);
             rw.qsum[gi] = sum;
         }
-    }
-    RowState<D> st;
+        RowState<D> st;
 #pragma unroll
-    for (int i = 0; i < DL; ++i) st.o[i] = f4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    st.ref = -INFINITY;
-    st.sum = 0.0f;
+        for (int i = 0; i < DL; ++i) st.o[i] = f4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        st.ref = -INFINITY;
+        st.sum = 0.0f;
 
-    const int k_slab = (g.layer * 2) * v.Hkv + h;
-    const int u_end = min((n + 31) >> 5, (share + 1) * sh.units);          // (none for an empty sequence)
-    const uint64_t* offs = v.off + static_cast<int64_t>(s) * v.stride;
-    const uint8_t* bits = v.bits + static_cast<int64_t>(s) * v.stride;
-    for (int u = share * sh.units + wave; u < u_end; u += 32 * kAttendWaves) {
-        // the pages of the wavefront's next 32 units, a tile per lane
-        TileBatch tb;
-        tb.unit0 = u;
-        const int unit = u + kAttendWaves * (lane >> 1), tile = 2 * unit + (lane & 1);
-        const bool in = unit < u_end && tile * 16 < n;
-        const int page = !in ? 0 : (v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile);
-        const uint64_t off = offs[page];
-        const uint32_t b = bits[page];
-        const uint32_t width = in && page_present(v, off, b) ? b : 0u;
-        tb.off_lo = static_cast<uint32_t>(off);
-        tb.off_hi = static_cast<uint32_t>(off >> 32);
-        tb.in_page = tile * 16 - page * v.T;
-        walk<D, G, 16, HP>(__ballot(width == 16), tb, n, v, k_slab, rw, st, lane);
-        walk<D, G, 8, HP>(__ballot(width == 8), tb, n, v, k_slab, rw, st, lane);
-        walk<D, G, 4, HP>(__ballot(width == 4), tb, n, v, k_slab, rw, st, lane);
-        walk<D, G, 2, HP>(__ballot(width == 2), tb, n, v, k_slab, rw, st, lane);
-        if (logits) {                                // what the tokens of absent tiles would have had
-            for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
-                const int at = __builtin_ctzll(none), first = 16 * (2 * (u + kAttendWaves * (at >> 1)) + (at & 1));
-                if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + first + 4 * q4) = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        const int k_slab = (g.layer * 2) * v.Hkv + h;
+        const uint64_t* offs = v.off + static_cast<int64_t>(s) * v.stride;
+        const uint8_t* bits = v.bits + static_cast<int64_t>(s) * v.stride;
+        for (int u = u_begin; u < u_end; u += 32) {
+            // the pages of the next 32 units, a tile per lane
+            TileBatch tb;
+            tb.tile0 = 2 * u;
+            const int tile = 2 * u + lane;
+            const bool in = tile < 2 * u_end && tile * 16 < n;
+            const int page = !in ? 0 : (v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile);
+            const uint64_t off = offs[page];
+            const uint32_t b = bits[page];
+            const uint32_t width = in && page_present(v, off, b) ? b : 0u;
+            tb.off_lo = static_cast<uint32_t>(off);
+            tb.off_hi = static_cast<uint32_t>(off >> 32);
+            tb.in_page = tile * 16 - page * v.T;
+            int dealt = 0;
+            walk<D, G, 16, HP>(__ballot(width == 16), tb, n, v, k_slab, rw, st, wave, lane, dealt);
+            walk<D, G, 8, HP>(__ballot(width == 8), tb, n, v, k_slab, rw, st, wave, lane, dealt);
+            walk<D, G, 4, HP>(__ballot(width == 4), tb, n, v, k_slab, rw, st, wave, lane, dealt);
+            walk<D, G, 2, HP>(__ballot(width == 2), tb, n, v, k_slab, rw, st, wave, lane, dealt);
+            if (logits && wave == 0) {               // what the tokens of absent tiles would have had
+                for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
+                    const int t = 16 * (2 * u + __builtin_ctzll(none));
+                    if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + t + 4 * q4) = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                }
             }
         }
-    }
-    // the four states against one reference per row
-    st.sum += __shfl_xor(st.sum, 16);
-    st.sum += __shfl_xor(st.sum, 32);
-    if (q4 == 0) {
-        ml_lds[wave][0][l16] = st.ref;
-        ml_lds[wave][1][l16] = st.sum;
-    }
-    if (ok) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < DL; i += 4)
-                *reinterpret_cast<f4_t*>(o_lds + (wave * tile_rows + l16) * D + DL * (4 * q4 + r) + i) = f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
-    }
-    __syncthreads();
-    const int here = min(16, count * g.per - rt * 16);                   // rows of this tile
-    for (int i = threadIdx.x; i < here * (D / 4); i += 64 * kAttendWaves) {
-        const int row = i / (D / 4), d = i % (D / 4) * 4;
-        float ref = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kAttendWaves; ++k) ref = fmaxf(ref, ml_lds[k][0][row]);
-        f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < kAttendWaves; ++k) {
-            const float m = ml_lds[k][0][row], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
-            sum += f * ml_lds[k][1][row];
-            o += *reinterpret_cast<const f4_t*>(o_lds + (k * tile_rows + row) * D + d) * f;
+        // the four states against one reference per row
+        st.sum += __shfl_xor(st.sum, 16);
+        st.sum += __shfl_xor(st.sum, 32);
+        if (q4 == 0) {
+            ml_lds[wave][0][l16] = st.ref;
+            ml_lds[wave][1][l16] = st.sum;
         }
-        const int jr = rt * 16 + row;
-        if (part_ml && d == 0) {
-            float* ml = part_ml + ((pair * g.splits + share) * g.rows + jr) * 2;
-            ml[0] = ref;
-            ml[1] = sum;
-        }
-        if (sh.used <= 1) {
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;            // a row that sees nothing: zeros
-            h4_t x;
+        if (ok) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
-            const int64_t at = (static_cast<int64_t>(rows.first + jr / g.per) * v.Hq + h * g.per + jr % g.per) * D + d;
-            *reinterpret_cast<h4_t*>(out + at) = x;
-        } else {
-            *reinterpret_cast<f4_t*>(part_o + ((pair * g.splits + share) * g.rows + jr) * D + d) = o;
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < DL; i += 4)
+                    *reinterpret_cast<f4_t*>(o_lds + (wave * g.tile_rows + l16) * D + DL * (4 * q4 + r) + i) =
+                        f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
         }
+        __syncthreads();
+        const bool whole = u_begin == 0 && u_end == sw.units;
+        const int64_t slot0 = (blockIdx.x + pair_number(v, g, s, pair)) * g.tile_rows;
+        const int here = min(16, count * g.per - rt * 16);               // rows of this tile
+        for (int i = threadIdx.x; i < here * (D / 4); i += 64 * kAttendWaves) {
+            const int row = i / (D / 4), d = i % (D / 4) * 4;
+            float ref = -INFINITY, sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kAttendWaves; ++k) ref = fmaxf(ref, ml_lds[k][0][row]);
+            f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kAttendWaves; ++k) {
+                const float m = ml_lds[k][0][row], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
+                sum += f * ml_lds[k][1][row];
+                o += *reinterpret_cast<const f4_t*>(o_lds + (k * g.tile_rows + row) * D + d) * f;
+            }
+            const int64_t slot = slot0 + row;
+            if (d == 0) *reinterpret_cast<float2*>(part_ml + slot * 2) = float2{ref, sum};
+            if (whole) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;        // a row that sees nothing: zeros
+                const int jr = rt * 16 + row;
+                h4_t x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
+                *reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(sw.first + jr / g.per) * v.Hq + h * g.per + jr % g.per) * D + d) = x;
+            } else {
+                *reinterpret_cast<f4_t*>(part_o + slot * D + d) = o;
+            }
+        }
+        if (at < run_end) __syncthreads();           // the next piece writes to LDS again
     }
 }
 
-// Reference and sum of a row over its shares, by all lanes of a wavefront together; weight[k] the factor of share k.
-__device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int64_t first, int used, int rows, int lane, float* weight,
+// Reference and sum of a row over its shares (rows first, first + step, ..), by all lanes of a wavefront together, 64 shares a step;
+// weight[k] the factor of share k against the reference.
+__device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int64_t first, int step, int used, int lane, float* weight,
                                           float& ref, float& sum) {
-    float m[kMaxSplits / 64], l[kMaxSplits / 64];
     ref = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
-        const int k = i * 64 + lane;
-        m[i] = -INFINITY;
-        l[i] = 0.0f;
-        if (k < used) {
-            const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * rows) * 2);
-            m[i] = ml.x;
-            l[i] = ml.y;
-        }
-        ref = fmaxf(ref, m[i]);
-    }
+    for (int k = lane; k < used; k += 64) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * step) * 2]);
 #pragma unroll
     for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
     sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kMaxSplits / 64; ++i) {
-        const int k = i * 64 + lane;
-        const float f = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - ref);
-        if (weight && k < used) weight[k] = f;
-        sum += f * l[i];
+    for (int k = lane; k < used; k += 64) {
+        const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * step) * 2);
+        const float f = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - ref);
+        if (weight) weight[k] = f;
+        sum += f * ml.y;
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
 }
 
-// Joins the shares of a row whose tokens were divided: one workgroup per row, its threads four channels and every
-// (1024 / D)-th share each.
+// Joins the shares of a row that several workgroups have had a part of (and writes the zeros of an empty sequence): one workgroup per
+// row, its threads four channels and every (1024 / D)-th share each.  `weight` holds as many floats as there are workgroups.
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(PagesView v, AttendGeom g, const int32_t* __restrict__ row_start,
                                                           const float* __restrict__ part_o, const float* __restrict__ part_ml,
                                                           _Float16* __restrict__ out) {
     constexpr int kQuads = D / 4, kParts = 256 / kQuads;
-    __shared__ float weight[kMaxSplits];
+    extern __shared__ float weight[];
     __shared__ float total;
     __shared__ f4_t o_lds[kParts][kQuads];
     const int lane = threadIdx.x & 63;
-    const int64_t pair = blockIdx.x / g.rows;
-    const int j = static_cast<int>(blockIdx.x - pair * g.rows);
-    const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair - static_cast<int64_t>(s) * v.Hkv);
-    const SeqRows rows = seq_rows(row_start, s, g.n_rows);
-    const int n = seq_len(v, s), count = min(rows.count, g.max_rows);
-    const Shares sh = shares_of(g, n);
-    if (sh.used <= 1 || j >= count * g.per) return;
-    const int64_t first = pair * g.splits * g.rows + j;
+    const int seq_head = static_cast<int>(blockIdx.x) / g.rows, j = static_cast<int>(blockIdx.x) - seq_head * g.rows;
+    const int s = seq_head / v.Hkv, h = seq_head - s * v.Hkv;
+    const RowShares sh = row_shares(v, g, row_start, lane, s, h, j);
+    if (sh.used == 1 || j >= min(sh.w.count, g.max_rows) * g.per) return;
+    const int64_t first = sh.first * g.tile_rows + j % 16;
     const int quad = threadIdx.x % kQuads, part = threadIdx.x / kQuads;
     if (threadIdx.x < 64) {
         float ref, sum;
-        row_total(part_ml, first, sh.used, g.rows, lane, weight, ref, sum);
+        row_total(part_ml, first, g.tile_rows, sh.used, lane, weight, ref, sum);
         if (lane == 0) total = sum;
     }
     __syncthreads();
     f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
     const f4_t* src = reinterpret_cast<const f4_t*>(part_o + first * D) + quad;
-    const int64_t step = static_cast<int64_t>(g.rows) * kQuads;
+    const int64_t step = static_cast<int64_t>(g.tile_rows) * kQuads;
 #pragma unroll 4
     for (int k = part; k < sh.used; k += kParts) o += src[k * step] * weight[k];
     o_lds[part][quad] = o;
@@ -578,7 +665,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(PagesView v, AttendGeo
     h4_t x;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
-    reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(rows.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D)[quad] = x;
+    reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(sh.w.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D)[quad] = x;
 }
 
 // The weights of a pair's keys, from the logits its rows left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
@@ -589,17 +676,15 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(PagesView v, AttendGeo
                                                           const float* mass_in, float* mass) {
     __shared__ float refs[kMaxPairRows], invs[kMaxPairRows];
     const int64_t pair = blockIdx.x / blocks;
-    const int s = static_cast<int>(pair / v.Hkv), t0 = static_cast<int>(blockIdx.x % blocks) * 1024;
-    const int n = seq_len(v, s);
-    if (t0 >= n) return;
-    const SeqRows rows = seq_rows(row_start, s, g.n_rows);
-    const int count = min(rows.count, g.max_rows) * g.per;
-    if (count == 0) return;
-    const Shares sh = shares_of(g, n);
+    const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair % v.Hkv), t0 = static_cast<int>(blockIdx.x % blocks) * 1024;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const RowShares sh = row_shares(v, g, row_start, lane, s, h, 0);
+    const int n = sh.w.n, count = min(sh.w.count, g.max_rows) * g.per;
+    if (t0 >= n || count == 0) return;
     for (int j = wave; j < count; j += 4) {
+        const RowShares of = j < 16 ? sh : row_shares(v, g, row_start, lane, s, h, j);
         float ref, sum;
-        row_total(part_ml, pair * g.splits * g.rows + j, sh.used, g.rows, lane, nullptr, ref, sum);
+        row_total(part_ml, of.first * g.tile_rows + j % 16, g.tile_rows, of.used, lane, nullptr, ref, sum);
         if (lane == 0) {
             refs[j] = sum > 0.0f ? ref : 0.0f;                   // (a row that sees nothing weighs nothing: its logits are -inf)
             invs[j] = sum > 0.0f ? 1.0f / sum : 0.0f;

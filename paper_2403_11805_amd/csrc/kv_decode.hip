@@ -107,9 +107,8 @@ AttendGeom attend_geom(const kv_shape_t& s, int32_t n_seqs, int32_t max_rows) {
     g.per = s.n_q_heads / s.n_kv_heads;
     g.rows = g.per * max_rows;
     g.row_tiles = (g.rows + 15) / 16;
-    const int64_t groups = static_cast<int64_t>(n_seqs) * s.n_kv_heads * g.row_tiles;
-    g.splits = static_cast<int32_t>(attend_splits(groups, s.n_tokens));
-    g.min_units = kAttendMinUnits;
+    g.tile_rows = std::min(16, g.rows);
+    g.groups = static_cast<int32_t>(attend_groups(static_cast<int64_t>(n_seqs) * s.n_kv_heads * g.row_tiles, s.n_tokens, s.head_dim));
     g.scale_log2e = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim)));
     return g;
 }
@@ -118,20 +117,24 @@ struct AttendSpace {
     uint64_t part_o, part_ml, logits, all;      // byte offsets and the size of the workspace
 };
 AttendSpace attend_space(const kv_shape_t& s, int32_t n_seqs, const AttendGeom& g, bool with_mass) {
-    const uint64_t pairs = static_cast<uint64_t>(n_seqs) * s.n_kv_heads, rows = pairs * g.splits * g.rows;
     auto up = [](uint64_t x) { return (x + 255) & ~255ull; };
+    const uint64_t rows = (g.groups + static_cast<uint64_t>(n_seqs) * s.n_kv_heads * g.row_tiles) * g.tile_rows;
     AttendSpace w;
     w.part_o = 0;
-    w.part_ml = w.part_o + (g.splits > 1 ? up(rows * s.head_dim * 4) : 0);
+    w.part_ml = w.part_o + up(rows * s.head_dim * 4);
     w.logits = w.part_ml + up(rows * 8);
-    w.all = w.logits + (with_mass ? up(pairs * g.rows * s.n_tokens * 4) : 0);
+    w.all = w.logits + (with_mass ? up(static_cast<uint64_t>(n_seqs) * s.n_kv_heads * g.rows * s.n_tokens * 4) : 0);
     return w;
 }
 
-int check_max_rows(const kv_shape_t* shape, int32_t max_rows) {
+// The rows of a step and the work they make: units of 32 tokens of every (sequence, kv head, row tile) are counted in 31 bits.
+int check_attend(const kv_shape_t* shape, int32_t n_seqs, int32_t max_rows) {
     if (max_rows < 1 || max_rows > 16) return fail(KV_EINVAL, "max_rows %d outside [1,16]", max_rows);
-    if (static_cast<int64_t>(shape->n_q_heads / shape->n_kv_heads) * max_rows > kMaxPairRows)
-        return fail(KV_ESHAPE, "more than %d query rows per kv head", kMaxPairRows);
+    const int64_t rows = static_cast<int64_t>(shape->n_q_heads / shape->n_kv_heads) * max_rows;
+    if (rows > kMaxPairRows) return fail(KV_ESHAPE, "more than %d query rows per kv head", kMaxPairRows);
+    const int64_t pairs = static_cast<int64_t>(n_seqs) * shape->n_kv_heads;
+    if (pairs * ((rows + 15) / 16) > 0x7fffffffLL / ((shape->n_tokens + 2047) / 32) || pairs * rows > 0x7fffffffLL)
+        return fail(KV_ESHAPE, "n_seqs * n_kv_heads * n_tokens too large for one call");
     return KV_OK;
 }
 
@@ -178,7 +181,7 @@ int32_t kv_append_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
 }
 
 uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int32_t max_rows, int32_t with_mass) {
-    if (check_paged_shape(shape) || check_seqs(n_seqs) || check_max_rows(shape, max_rows)) return 0;
+    if (check_paged_shape(shape) || check_seqs(n_seqs) || check_attend(shape, n_seqs, max_rows)) return 0;
     return attend_space(*shape, n_seqs, attend_geom(*shape, n_seqs, max_rows), with_mass != 0).all;
 }
 
@@ -187,7 +190,7 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
                          void* workspace, uint64_t workspace_bytes, void* out, void* stream) {
     if (int rc = check_pages(shape, pages)) return rc;
     if (int rc = check_layer(shape, layer)) return rc;
-    if (int rc = check_max_rows(shape, max_rows)) return rc;
+    if (int rc = check_attend(shape, pages->n_seqs, max_rows)) return rc;
     if (int rc = check_rows(pages, n_rows, row_start, q_stride, static_cast<int64_t>(shape->n_q_heads) * shape->head_dim)) return rc;
     if (mass_in && !mass) return fail(KV_EINVAL, "mass_in without mass");
     if (n_rows == 0) return KV_OK;
@@ -203,10 +206,7 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
         return fail(KV_ENOMEM, "workspace of %llu bytes, %llu needed", static_cast<unsigned long long>(workspace_bytes),
                     static_cast<unsigned long long>(w.all));
     const int64_t pairs = static_cast<int64_t>(pages->n_seqs) * shape->n_kv_heads;
-    const int64_t groups = pairs * g.row_tiles * g.splits;
     const int32_t blocks = (shape->n_tokens + 1023) / 1024;
-    if (groups > 0x7fffffffLL || pairs * g.rows > 0x7fffffffLL || pairs * blocks > 0x7fffffffLL)
-        return fail(KV_ESHAPE, "attention grid exceeds 2^31 workgroups");
     const PagesView view = pages_view(*shape, *pages);
     uint8_t* space = static_cast<uint8_t*>(workspace);
     float* part_o = reinterpret_cast<float*>(space + w.part_o);
@@ -215,8 +215,8 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     hipStream_t st = static_cast<hipStream_t>(stream);
     const _Float16* q16 = static_cast<const _Float16*>(q);
     _Float16* o16 = static_cast<_Float16*>(out);
-    const dim3 grid(static_cast<uint32_t>(groups)), block(64 * kAttendWaves);
-    const uint32_t lds = static_cast<uint32_t>(kAttendWaves * std::min(16, g.rows) * shape->head_dim) * 4;   // at most 64 KB
+    const dim3 grid(static_cast<uint32_t>(g.groups)), block(64 * kAttendWaves);
+    const uint32_t lds = static_cast<uint32_t>(kAttendWaves * g.tile_rows * shape->head_dim) * 4;   // at most 64 KB
 #define KV_LAUNCH(D, G)                                                                                                                       \
     do {                                                                                                                                      \
         if (view.half_params)                                                                                                                 \
@@ -234,13 +234,12 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     }
 #undef KV_LAUNCH
     if (int rc = launch_status("attend_kernel launch")) return rc;
-    if (g.splits > 1) {
-        const dim3 join(static_cast<uint32_t>(pairs * g.rows));
-#define KV_LAUNCH(D) hipLaunchKernelGGL((attend_join_kernel<D>), join, dim3(256), 0, st, view, g, row_start, part_o, part_ml, o16)
-        KV_BY_HEAD_DIM(shape->head_dim, KV_LAUNCH);
+    const dim3 join(static_cast<uint32_t>(pairs * g.rows));
+#define KV_LAUNCH(D) \
+    hipLaunchKernelGGL((attend_join_kernel<D>), join, dim3(256), static_cast<uint32_t>(g.groups) * 4, st, view, g, row_start, part_o, part_ml, o16)
+    KV_BY_HEAD_DIM(shape->head_dim, KV_LAUNCH);
 #undef KV_LAUNCH
-        if (int rc = launch_status("attend_join_kernel launch")) return rc;
-    }
+    if (int rc = launch_status("attend_join_kernel launch")) return rc;
     if (mass) {
         hipLaunchKernelGGL(attend_mass_kernel, dim3(static_cast<uint32_t>(pairs * blocks)), dim3(256), 0, st, view, g, blocks, row_start,
                            part_ml, logits, mass_in, mass);
