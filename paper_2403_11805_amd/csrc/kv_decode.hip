@@ -282,14 +282,19 @@ int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_
         return fail(KV_ENOMEM, "workspace of %llu bytes, %llu needed", static_cast<unsigned long long>(workspace_bytes),
                     static_cast<unsigned long long>(need));
     const int32_t rows_per_group = 256 / (shape->head_dim / 8);
-    const int32_t blocks = static_cast<int32_t>(evict_blocks(pairs, g.list, rows_per_group));
+    const int32_t blocks = static_cast<int32_t>(evict_blocks(pairs, g.list, rows_per_group * kAtOnce));
     if (pairs * std::max(blocks, 1) > 0x7fffffffLL) return fail(KV_ESHAPE, "eviction grid exceeds 2^31 workgroups");
     const PagesView view = pages_view(*shape, *pages);
     int32_t* n_moves = static_cast<int32_t*>(workspace);
     int32_t* moves = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + ((static_cast<uint64_t>(pairs) * 4 + 255) & ~255ull));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(evict_select_kernel, dim3(static_cast<uint32_t>(pairs)), dim3(kSelectThreads), 0, st, view, g, mass_in, pos_in, seen,
-                       moves, n_moves, mass, pos);
+#define KV_LAUNCH(KEYS)                                                                                                                 \
+    hipLaunchKernelGGL((evict_select_kernel<KEYS>), dim3(static_cast<uint32_t>(pairs)), dim3(kSelectThreads), 0, st, view, g, mass_in, \
+                       pos_in, seen, moves, n_moves, mass, pos)
+    if (shape->n_tokens <= 4 * kSelectThreads) KV_LAUNCH(4);
+    else if (shape->n_tokens <= 32 * kSelectThreads) KV_LAUNCH(32);
+    else KV_LAUNCH(0);
+#undef KV_LAUNCH
     if (int rc = launch_status("evict_select_kernel launch")) return rc;
     if (g.list == 0) return KV_OK;                          // no sequence can have more than `keep` tokens
     const dim3 grid(static_cast<uint32_t>(pairs * blocks));

@@ -23,13 +23,17 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int sink, int
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
 
-// One workgroup per pair = (layer, sequence, kv head).  The key of the keep-th token is found digit by digit (11, 11 and 10 bits)
-// from histograms in LDS; of the tokens that have exactly that key the lowest slots are kept, as many as there is room for.
-// Every wavefront then owns a contiguous range of slots and walks it in steps of 64: ballots count, so that kept tokens above
-// `keep` and evicted ones below come out in ascending order without a sort.
+// One workgroup per pair = (layer, sequence, kv head).  A wavefront owns a contiguous range of slots and a lane every 64th of them; up to
+// KEYS keys of a lane are read once and kept in registers (KEYS = 0: the range is longer, and every pass reads it again).  The key of
+// the keep-th token is found digit by digit (11, 11 and 10 bits) from histograms in LDS; of the tokens that have exactly that key the
+// lowest slots are kept, as many as there is room for.  Kept tokens above `keep` and evicted ones below come out in ascending order
+// without a sort: ballots count within 64 slots, and one pass counts for the wavefronts behind.
+// Latency bounds it: a workgroup reads a few hundred KB at most.
+template <int KEYS>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView v, EvictGeom g, const float* mass_in, const int32_t* pos_in,
                                                                       const int32_t* __restrict__ seen, int32_t* __restrict__ moves,
                                                                       int32_t* __restrict__ n_moves, float* mass, int32_t* pos) {
+    constexpr int kKeys = KEYS ? KEYS : 1;
     __shared__ uint32_t hist[2048];
     __shared__ uint32_t found[2];                                 // digit, tokens still wanted within it
     __shared__ uint32_t wave_total[kSelectWaves];
@@ -52,17 +56,47 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView 
         return;
     }
     const int from = (seen ? seen[s] : n) - g.recent;
-    auto key_at = [&](int i) { return evict_key(mass_in[i], pos_in[i], g.sink, from); };
+    const int steps = (n + kSelectThreads - 1) / kSelectThreads;                 // of 64 slots, of a wavefront's range
+    const int begin = wave * steps * 64 + lane;                                  // the lane's first slot
+    auto key_at = [&](int i) { return i < n ? evict_key(mass_in[i], pos_in[i], g.sink, from) : 0u; };
+    // (a lane's slots behind n have the lowest key, and `here` keeps them out of every count)
+    uint32_t keys[kKeys];
+    if constexpr (KEYS > 0) {
+        float m[kKeys];
+        int p[kKeys];
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int at = min(begin + i * 64, n - 1);
+            m[i] = mass_in[at];
+            p[i] = pos_in[at];
+        }
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) keys[i] = evict_key(m[i], p[i], g.sink, from);
+    }
+    // visits the lane's slots: f(slot, key, whether there is one); every lane of the wavefront together
+    auto each = [&](auto&& f) {
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const int at = begin + i * 64;
+                if (i < steps) f(at, keys[i], at < n);
+            }
+        } else {
+            for (int i = 0; i < steps; ++i) {
+                const int at = begin + i * 64;
+                f(at, key_at(at), at < n);
+            }
+        }
+    };
     uint32_t prefix = 0, want = static_cast<uint32_t>(keep);      // the want-th largest of the keys that begin with prefix
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
         const int low = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
         for (int i = tid; i < bins; i += kSelectThreads) hist[i] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += kSelectThreads) {
-            const uint32_t k = key_at(i);
-            if (pass == 0 || (k >> (low + (pass == 2 ? 10 : 11))) == prefix) atomicAdd(&hist[(k >> low) & (bins - 1)], 1u);
-        }
+        each([&](int, uint32_t k, bool here) {
+            if (here && (pass == 0 || (k >> (low + (pass == 2 ? 10 : 11))) == prefix)) atomicAdd(&hist[(k >> low) & (bins - 1)], 1u);
+        });
         __syncthreads();
         // from the highest bin down: thread t has the bins below bins - t * per
         const int per = bins / kSelectThreads;
@@ -95,31 +129,27 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView 
         want = found[1];
         __syncthreads();
     }
-    // kept: keys above `prefix`, and the first `want` slots whose key it is
-    const int range = ((n + kSelectThreads - 1) / kSelectThreads) * 64;          // slots of a wavefront
-    const int begin = min(wave * range, n), end = min(begin + range, n);
+    // kept: keys above `prefix`, and the first `want` slots whose key it is.  A wavefront needs the number of such ties in front of it,
+    // then of holes (evicted, below keep) and movers (kept, at or above it).
     int eq = 0;
-    for (int i = begin + lane; i - lane < end; i += 64)
-        eq += __builtin_popcountll(__ballot(i < end && key_at(i) == prefix));
+    each([&](int, uint32_t k, bool here) { eq += __builtin_popcountll(__ballot(here && k == prefix)); });
     if (lane == 0) wave_eq[wave] = eq;
     __syncthreads();
     int eq_before = 0;
     for (int k = 0; k < wave; ++k) eq_before += wave_eq[k];
     const uint64_t below_lane = (1ull << lane) - 1;
-    auto walk = [&](auto&& visit) {                                // visit(slot, in range, kept)
+    auto walk = [&](auto&& visit) {                                // visit(slot, whether there is one, kept)
         int seen_eq = eq_before;
-        for (int i = begin + lane; i - lane < end; i += 64) {
-            const bool in = i < end;
-            const uint32_t k = in ? key_at(i) : 0u;
-            const uint64_t ties = __ballot(in && k == prefix);
-            const bool kept = in && (k > prefix || (k == prefix && seen_eq + __builtin_popcountll(ties & below_lane) < static_cast<int>(want)));
+        each([&](int i, uint32_t k, bool here) {
+            const uint64_t ties = __ballot(here && k == prefix);
+            const bool kept = here && (k > prefix || (k == prefix && seen_eq + __builtin_popcountll(ties & below_lane) < static_cast<int>(want)));
             seen_eq += __builtin_popcountll(ties);
-            visit(i, in, kept);
-        }
+            visit(i, here, kept);
+        });
     };
     int holes = 0, movers = 0;
-    walk([&](int i, bool in, bool kept) {
-        holes += __builtin_popcountll(__ballot(in && !kept && i < keep));
+    walk([&](int i, bool here, bool kept) {
+        holes += __builtin_popcountll(__ballot(here && !kept && i < keep));
         movers += __builtin_popcountll(__ballot(kept && i >= keep));
     });
     if (lane == 0) {
@@ -136,8 +166,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView 
     if (tid == 0) n_moves[pair] = all;
     int32_t* to = moves + pair * 2 * g.list;
     int32_t* from_slot = to + g.list;
-    walk([&](int i, bool in, bool kept) {
-        const bool hole = in && !kept && i < keep, mover = kept && i >= keep;
+    walk([&](int i, bool here, bool kept) {
+        const bool hole = here && !kept && i < keep, mover = kept && i >= keep;
         const uint64_t hb = __ballot(hole), mb = __ballot(mover);
         if (hole) to[hole_at + __builtin_popcountll(hb & below_lane)] = i;
         if (mover) from_slot[mover_at + __builtin_popcountll(mb & below_lane)] = i;
@@ -228,8 +258,10 @@ __device__ __forceinline__ void piece_store(const PagesView& v, uint8_t* record,
     }
 }
 
-// The moves of a pair's list, `blocks` workgroups per pair: D/8 neighbouring lanes carry one row, its K and its V, and its weight
-// and position.  Rows come from slots at or above `keep` and go to slots below it, so no move reads what another has written.
+// The moves of a pair's list, `blocks` workgroups per pair: D/8 neighbouring lanes carry kAtOnce rows, their K and their V, with their
+// weight and position.  Rows come from slots at or above `keep` and go to slots below it, so no move reads what another has written.
+// A row's way is list entry - page entry - row - store: the four steps of the kAtOnce rows are taken together.
+constexpr int kAtOnce = 4;
 template <int D>
 __global__ __launch_bounds__(256) void evict_move_kernel(PagesView v, EvictGeom g, int32_t blocks, int32_t lpg_log2,
                                                          const int32_t* __restrict__ moves, const int32_t* __restrict__ n_moves,
@@ -240,27 +272,76 @@ __global__ __launch_bounds__(256) void evict_move_kernel(PagesView v, EvictGeom 
     const int block = static_cast<int>(blockIdx.x % blocks);
     const int layer = g.layer0 + static_cast<int>(pair / v.Hkv / v.n_seqs), s = static_cast<int>(pair / v.Hkv % v.n_seqs);
     const int h = static_cast<int>(pair % v.Hkv);
-    const int count = n_moves[pair], in_row = threadIdx.x % kRow;
+    const int count = n_moves[pair], in_row = threadIdx.x % kRow, row = threadIdx.x / kRow;
     const int32_t* to_list = moves + pair * 2 * g.list;
     const int32_t* from_list = to_list + g.list;
     const uint64_t* offs = v.off + static_cast<int64_t>(s) * v.stride;
     const uint8_t* bits = v.bits + static_cast<int64_t>(s) * v.stride;
     const int k_slab = layer * 2 * v.Hkv + h;
-    for (int i = block * kRows + static_cast<int>(threadIdx.x) / kRow; i < count; i += blocks * kRows) {
-        const int to = to_list[i], from = from_list[i];
-        if (in_row == 0) {
-            mass[pair * v.N + to] = mass_in[pair * v.N + from];
-            pos[pair * v.N + to] = pos_in[pair * v.N + from];
+    for (int i0 = block * kRows * kAtOnce; i0 < count; i0 += blocks * kRows * kAtOnce) {
+        int to[kAtOnce], from[kAtOnce], to_b[kAtOnce], from_b[kAtOnce];
+        uint64_t to_off[kAtOnce], from_off[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {                       // (behind the list: the last move again, not stored)
+            const int i = min(i0 + k * kRows + row, count - 1);
+            to[k] = to_list[i];
+            from[k] = from_list[i];
         }
-        const int to_page = to / v.T, from_page = from / v.T;
-        const uint64_t to_off = offs[to_page], from_off = offs[from_page];
-        const int to_b = bits[to_page], from_b = bits[from_page];
-        if (!page_present(v, to_off, to_b) || !page_present(v, from_off, from_b)) continue;
-        const int to_piece = (to - to_page * v.T) * kRow + in_row, from_piece = (from - from_page * v.T) * kRow + in_row;
-        const Piece k = piece_load<D>(v, v.pool + from_off, from_b, k_slab, from_piece, lpg_log2);
-        const Piece x = piece_load<D>(v, v.pool + from_off, from_b, k_slab + v.Hkv, from_piece, lpg_log2);
-        piece_store<D>(v, v.pool + to_off, to_b, from_b, k_slab, to_piece, lpg_log2, lane, k);
-        piece_store<D>(v, v.pool + to_off, to_b, from_b, k_slab + v.Hkv, to_piece, lpg_log2, lane, x);
+        float m[kAtOnce];
+        int p[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int a = to[k] / v.T, b = from[k] / v.T;
+            to_off[k] = offs[a];
+            from_off[k] = offs[b];
+            to_b[k] = bits[a];
+            from_b[k] = bits[b];
+            m[k] = mass_in[pair * v.N + from[k]];
+            p[k] = pos_in[pair * v.N + from[k]];
+        }
+        bool fp16 = true;                                         // every row between fp16 pages: the common case, without branches
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            fp16 = fp16 && to_b[k] == 16 && from_b[k] == 16 && page_present(v, to_off[k], 16) && page_present(v, from_off[k], 16);
+        if (__all(fp16)) {
+            u4_t x[kAtOnce], y[kAtOnce];
+            const int64_t slab = static_cast<int64_t>(k_slab) * v.T * kRow, v_step = static_cast<int64_t>(v.Hkv) * v.T * kRow;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const u4_t* src = reinterpret_cast<const u4_t*>(v.pool + from_off[k]) + slab + from[k] % v.T * kRow + in_row;
+                x[k] = stream_load<true>(src);
+                y[k] = stream_load<true>(src + v_step);
+            }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                u4_t* dst = reinterpret_cast<u4_t*>(v.pool + to_off[k]) + slab + to[k] % v.T * kRow + in_row;
+                if (i0 + k * kRows + row < count) {
+                    stream_store<true>(x[k], dst);
+                    stream_store<true>(y[k], dst + v_step);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int i = i0 + row; i < min(i0 + kRows * kAtOnce, count); i += kRows) {
+                const int a = to_list[i], b = from_list[i];
+                const uint64_t a_off = offs[a / v.T], b_off = offs[b / v.T];
+                const int a_bits = bits[a / v.T], b_bits = bits[b / v.T];
+                if (!page_present(v, a_off, a_bits) || !page_present(v, b_off, b_bits)) continue;
+                const int a_piece = a % v.T * kRow + in_row, b_piece = b % v.T * kRow + in_row;
+#pragma unroll 1
+                for (int slab = k_slab; slab <= k_slab + v.Hkv; slab += v.Hkv)                 // K, then V
+                    piece_store<D>(v, v.pool + a_off, a_bits, b_bits, slab, a_piece, lpg_log2, lane,
+                                   piece_load<D>(v, v.pool + b_off, b_bits, slab, b_piece, lpg_log2));
+            }
+        }
+        if (in_row == 0) {
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (i0 + k * kRows + row < count) {
+                    mass[pair * v.N + to[k]] = m[k];
+                    pos[pair * v.N + to[k]] = p[k];
+                }
+        }
     }
 }
 

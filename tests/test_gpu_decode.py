@@ -246,6 +246,26 @@ def test_evict(geom, lens, widths, keep, sink, recent, fmt, in_place):
             assert np.array_equal(m[0, s, :, c:], mass[0, s, :, c:], equal_nan=True)
 
 
+@pytest.mark.parametrize("N,lens,keep,sink,recent", [(4112, [4112, 4100], 1500, 4, 200), (8192, [8192, 70], 8000, 0, 0),
+                                                     (32784, [32784, 32769], 9000, 16, 1000)])
+@pytest.mark.parametrize("kind", ["ties", "all equal", "distinct"])
+def test_evict_of_long_sequences(N, lens, keep, sink, recent, kind):
+    """Ranges of slots that take a lane more than 4 and more than 32 keys."""
+    p = Paged((1, 1, 1, 64, N, 16, 64), lens, (16,), 17)
+    mass, pos = p.book(1)
+    if kind == "all equal":
+        mass[:] = 0.25
+    elif kind == "distinct":
+        mass = p.rng.permutation(mass.size).reshape(mass.shape).astype(np.float32) - 1000
+    pool, m, q = run_evict(p, (0, 1), mass, pos, keep, sink, recent)
+    want = p.pool.copy()
+    wm, wp = od.evict(p.os, want, *p.table(), (0, 1), mass, pos, keep, sink, recent)
+    assert np.array_equal(pool, want)
+    for s, n in enumerate(lens):
+        c = min(n, keep)
+        assert np.array_equal(m[0, s, :, :c], wm[0, s, :, :c]) and np.array_equal(q[0, s, :, :c], wp[0, s, :, :c])
+
+
 def test_evict_again_and_again():
     """Two evictions in a row with other weights, positions carried along, all layers: the newest tokens stay by position although
     they lie anywhere."""
