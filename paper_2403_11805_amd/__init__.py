@@ -17,6 +17,9 @@ def __getattr__(name):
         return importlib.import_module(f"{__name__}.{name}")
     binding = importlib.import_module(f"{__name__}.binding")
     try:
-        return getattr(binding, name)
+        found = getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
+    if name.startswith("kv_"):           # an entry point: the next access finds it here (3 us less per call)
+        globals()[name] = found
+    return found

@@ -183,6 +183,7 @@ def _dev_or_pinned(t: torch.Tensor, dtype=None) -> int:
 
 # not part of torch's documented interface: where it is absent the documented call takes its place
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> int:
@@ -629,56 +630,64 @@ class Pages:
             if t.device != pool.device:
                 raise ValueError("the pool and its tables must be on one device")
         self.shape, self.pool, self.off, self.bits, self.length = shape, pool, off, bits, length
-        self.device = pool.device
+        self.n_seqs = off.shape[0]
+        self._index = pool.get_device()
+        self._book_shape = (self.n_seqs, shape.n_kv_heads, shape.n_tokens)
         self._shape = shape.c()
         self._c = kv_pages_t(_dev(pool), pool.numel() * pool.element_size(), _dev(off, torch.int64), _dev(bits, torch.uint8),
                              _dev(length, torch.int32), off.shape[0], off.shape[1])
         self._refs = ctypes.byref(self._shape), ctypes.byref(self._c)
 
-    @property
-    def n_seqs(self) -> int:
-        return self._c.n_seqs
-
     def _on_device(self, stream):
         """The stream's address; the pages' device has to be the current one."""
-        if self.device.index != torch.cuda.current_device():
-            raise ValueError(f"the pages are on {self.device}, which is not the current device")
+        if self._index != _current_device():
+            raise ValueError(f"the pages are on cuda:{self._index}, which is not the current device")
         return _stream(stream)
 
+    # (a decode step makes several of these calls per layer: one comparison decides, and what is wrong is found out afterwards)
     def _arg(self, t, dtype, shape, name):
         """Address of an optional contiguous tensor of this dtype and shape on the pages' device."""
         if t is None:
             return None
-        if tuple(t.shape) != shape or t.device != self.device:
-            raise ValueError(f"{name} must be {list(shape)} on {self.device}, got {list(t.shape)} on {t.device}")
-        return _dev(t, dtype)
+        if t.shape == shape and t.dtype is dtype and t.get_device() == self._index and t.is_contiguous():
+            return t.data_ptr()
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        _dev(t, dtype)
+        raise ValueError(f"{name} must be on cuda:{self._index}, got {t.device}")
 
     def _rows(self, t, heads, name):
         """Address and row stride of fp16 rows [n_rows][heads][head_dim], whose rows may lie apart."""
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.shape.head_dim or t.device != self.device:
-            raise ValueError(f"{name} must be [n_rows][{heads}][{self.shape.head_dim}] on {self.device}")
-        if t.dtype != torch.float16:
-            raise TypeError(f"expected dtype torch.float16, got {t.dtype}")
-        stride = t.stride()
-        if stride[2] != 1 or (heads > 1 and stride[1] != t.shape[2]):
+        d, size, stride = self.shape.head_dim, t.shape, t.stride()
+        if len(size) != 3 or size[1] != heads or size[2] != d:
+            raise ValueError(f"{name} must be [n_rows][{heads}][{d}], got {list(size)}")
+        if t.dtype is not torch.float16 or t.get_device() != self._index:
+            raise TypeError(f"{name} must be torch.float16 on cuda:{self._index}, got {t.dtype} on {t.device}")
+        if stride[2] != 1 or (stride[1] != d and heads > 1):
             raise TypeError(f"the heads of a row of {name} must be contiguous")
-        return t.data_ptr(), (stride[0] if t.shape[0] > 1 else heads * t.shape[2])
+        return t.data_ptr(), (stride[0] if size[0] > 1 else heads * d)
+
+    def _space(self, t):
+        """Address and bytes of a workspace."""
+        if t.get_device() != self._index:
+            raise ValueError(f"the workspace must be on cuda:{self._index}, got {t.device}")
+        return _dev(t), t.numel() * t.element_size()
 
     def _book(self, t, dtype, name, layers=None):
-        s = self.shape
-        shape = (self.n_seqs, s.n_kv_heads, s.n_tokens)
-        return self._arg(t, dtype, shape if layers is None else (layers,) + shape, name)
+        return self._arg(t, dtype, self._book_shape if layers is None else (layers,) + self._book_shape, name)
 
 
 def kv_append_tokens(pages: Pages, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor = None,
                      seen: torch.Tensor = None, mass: torch.Tensor = None, pos: torch.Tensor = None, stream=None) -> None:
-    k_at, stride = pages._rows(k, pages.shape.n_kv_heads, "k")
-    v_at, v_stride = pages._rows(v, pages.shape.n_kv_heads, "v")
+    heads = pages.shape.n_kv_heads
+    k_at, stride = pages._rows(k, heads, "k")
+    v_at, v_stride = pages._rows(v, heads, "v")
     if v.shape != k.shape or v_stride != stride:
         raise ValueError("k and v must have the same shape and row stride")
+    n = pages.n_seqs
     _check(lib().kv_append_tokens(*pages._refs, layer, k_at, v_at, stride, k.shape[0],
-                                  pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"),
-                                  pages._arg(seen, torch.int32, (pages.n_seqs,), "seen"),
+                                  pages._arg(row_start, torch.int32, (n + 1,), "row_start"),
+                                  pages._arg(seen, torch.int32, (n,), "seen"),
                                   pages._book(mass, torch.float32, "mass"), pages._book(pos, torch.int32, "pos"),
                                   pages._on_device(stream)))
 
@@ -698,8 +707,8 @@ def kv_attend_tokens(pages: Pages, layer: int, q: torch.Tensor, workspace: torch
     _check(lib().kv_attend_tokens(*pages._refs, layer, q_at, stride, q.shape[0],
                                   pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"), max_rows,
                                   pages._book(mass_in, torch.float32, "mass_in"), pages._book(mass, torch.float32, "mass"),
-                                  _dev(workspace), workspace.numel() * workspace.element_size(),
-                                  pages._arg(out, torch.float16, tuple(q.shape), "out"), pages._on_device(stream)))
+                                  *pages._space(workspace), pages._arg(out, torch.float16, q.shape, "out"),
+                                  pages._on_device(stream)))
 
 
 def kv_evict_workspace_bytes(shape: Shape, n_seqs: int, n_layers: int, keep: int) -> int:
@@ -718,7 +727,7 @@ def kv_evict_tokens(pages: Pages, layer_begin: int, layer_end: int, mass_in: tor
                                  pages._book(mass_in, torch.float32, "mass_in", layers),
                                  pages._book(pos_in, torch.int32, "pos_in", layers),
                                  pages._arg(seen, torch.int32, (pages.n_seqs,), "seen"), keep, sink, recent,
-                                 _dev(workspace), workspace.numel() * workspace.element_size(),
+                                 *pages._space(workspace),
                                  pages._book(mass, torch.float32, "mass", layers), pages._book(pos, torch.int32, "pos", layers),
                                  pages._on_device(stream)))
 

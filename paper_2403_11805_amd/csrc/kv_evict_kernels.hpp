@@ -22,6 +22,15 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int sink, int
 
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kCopies = 4;
+
+// The sum of x over the lanes 0 .. count - 1 (of at most kSelectWaves), in every lane.
+__device__ __forceinline__ int sum_of_first(int x, int count, int lane) {
+    x = lane < count ? x : 0;
+#pragma unroll
+    for (int d = 1; d < kSelectWaves; d <<= 1) x += __shfl_xor(x, d);
+    return __builtin_amdgcn_readfirstlane(x);
+}
 
 // One workgroup per pair = (layer, sequence, kv head).  A wavefront owns a contiguous range of slots and a lane every 64th of them; up to
 // KEYS keys of a lane are read once and kept in registers (KEYS = 0: the range is longer, and every pass reads it again).  The key of
@@ -30,14 +39,16 @@ constexpr int kSelectWaves = kSelectThreads / 64;
 // without a sort: ballots count within 64 slots, and one pass counts for the wavefronts behind.
 // Latency bounds it: a workgroup reads a few hundred KB at most.
 template <int KEYS>
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView v, EvictGeom g, const float* mass_in, const int32_t* pos_in,
+__global__ __launch_bounds__(kSelectThreads, KEYS == 32 ? 4 : 8) void evict_select_kernel(PagesView v, EvictGeom g, const float* mass_in, const int32_t* pos_in,
                                                                       const int32_t* __restrict__ seen, int32_t* __restrict__ moves,
                                                                       int32_t* __restrict__ n_moves, float* mass, int32_t* pos) {
     constexpr int kKeys = KEYS ? KEYS : 1;
-    __shared__ uint32_t hist[2048];
-    __shared__ uint32_t found[2];                                 // digit, tokens still wanted within it
-    __shared__ uint32_t wave_total[kSelectWaves];
-    __shared__ int32_t wave_eq[kSelectWaves], wave_hole[kSelectWaves], wave_mover[kSelectWaves];
+    // one histogram per digit, cleared together; the first digit, where most keys meet in few bins (sign, exponent and two bits),
+    // has kCopies, so that fewer lanes of an LDS atomic hit one address
+    __shared__ uint32_t hist[2048 * kCopies + 2048 + 1024];
+    __shared__ uint32_t found[3][2];                              // digit, tokens still wanted within it
+    __shared__ uint32_t wave_total[3][kSelectWaves];
+    __shared__ int32_t wave_count[4][kSelectWaves];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int64_t pair = blockIdx.x;
@@ -89,80 +100,100 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(PagesView 
         }
     };
     uint32_t prefix = 0, want = static_cast<uint32_t>(keep);      // the want-th largest of the keys that begin with prefix
+    for (int i = tid; i < 2048 * kCopies + 2048 + 1024; i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        const int low = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048;
-        for (int i = tid; i < bins; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
+        const int low = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bins = pass == 2 ? 1024 : 2048, copies = pass == 0 ? kCopies : 1;
+        uint32_t* h = hist + (pass == 0 ? 0 : 2048 * kCopies + (pass == 1 ? 0 : 2048));
         each([&](int, uint32_t k, bool here) {
-            if (here && (pass == 0 || (k >> (low + (pass == 2 ? 10 : 11))) == prefix)) atomicAdd(&hist[(k >> low) & (bins - 1)], 1u);
+            if (here && (pass == 0 || (k >> (low + (pass == 2 ? 10 : 11))) == prefix))
+                atomicAdd(&h[((k >> low) & (bins - 1)) * copies + (lane & (copies - 1))], 1u);
         });
         __syncthreads();
         // from the highest bin down: thread t has the bins below bins - t * per
+        constexpr int kMostPer = 2048 / kSelectThreads;
         const int per = bins / kSelectThreads;
-        uint32_t mine = 0;
-        for (int e = 0; e < per; ++e) mine += hist[bins - 1 - (tid * per + e)];
+        uint32_t own[kMostPer], mine = 0;
+#pragma unroll
+        for (int e = 0; e < kMostPer; ++e) {
+            own[e] = 0;
+            if (e < per)
+                for (int c = 0; c < copies; ++c) own[e] += h[(bins - 1 - (tid * per + e)) * copies + c];
+            mine += own[e];
+        }
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t x = __shfl_up(upto, d);
             upto += lane >= d ? x : 0;
         }
-        if (lane == 63) wave_total[wave] = upto;
+        if (lane == 63) wave_total[pass][wave] = upto;
         __syncthreads();
-        for (int k = 0; k < wave; ++k) upto += wave_total[k];
+        upto += sum_of_first(wave_total[pass][lane & (kSelectWaves - 1)], wave, lane);
         const uint32_t before = upto - mine;
         if (before < want && want <= upto) {                      // exactly one thread: some n > keep tokens are counted
-            uint32_t left = want - before;
-            for (int e = 0; e < per; ++e) {
-                const int bin = bins - 1 - (tid * per + e);
-                if (left <= hist[bin]) {
-                    found[0] = static_cast<uint32_t>(bin);
-                    found[1] = left;
-                    break;
+            uint32_t left = want - before, bin = bins - 1 - tid * per;
+#pragma unroll
+            for (int e = 0; e + 1 < kMostPer; ++e) {
+                if (e + 1 < per && left > own[e]) {
+                    left -= own[e];
+                    --bin;
                 }
-                left -= hist[bin];
             }
+            found[pass][0] = bin;
+            found[pass][1] = left;
         }
         __syncthreads();
-        prefix = (prefix << (pass == 2 ? 10 : 11)) | found[0];
-        want = found[1];
-        __syncthreads();
+        prefix = (prefix << (pass == 2 ? 10 : 11)) | found[pass][0];
+        want = found[pass][1];
     }
-    // kept: keys above `prefix`, and the first `want` slots whose key it is.  A wavefront needs the number of such ties in front of it,
-    // then of holes (evicted, below keep) and movers (kept, at or above it).
-    int eq = 0;
-    each([&](int, uint32_t k, bool here) { eq += __builtin_popcountll(__ballot(here && k == prefix)); });
-    if (lane == 0) wave_eq[wave] = eq;
+    // Kept: keys above `prefix`, and the first `want` slots whose key it is.  A wavefront needs the number of such ties in front of it, and
+    // of holes (evicted, below keep) and movers (kept, at or above it): all follow from four counts of every wavefront.
+    int above[2] = {0, 0}, ties[2] = {0, 0};                       // [slots below keep, others]
+    each([&](int i, uint32_t k, bool here) {
+        const uint64_t gt = __ballot(here && k > prefix), eq = __ballot(here && k == prefix), low = __ballot(i < keep);
+        above[0] += __builtin_popcountll(gt & low);
+        above[1] += __builtin_popcountll(gt & ~low);
+        ties[0] += __builtin_popcountll(eq & low);
+        ties[1] += __builtin_popcountll(eq & ~low);
+    });
+    if (lane == 0) {
+        wave_count[0][wave] = above[0];
+        wave_count[1][wave] = above[1];
+        wave_count[2][wave] = ties[0];
+        wave_count[3][wave] = ties[1];
+    }
     __syncthreads();
-    int eq_before = 0;
-    for (int k = 0; k < wave; ++k) eq_before += wave_eq[k];
+    int eq_before, hole_at, mover_at, all;
+    {                                                              // lane k: the counts of wavefront k
+        const int k = lane & (kSelectWaves - 1);
+        const int eq_low = wave_count[2][k], eq_high = wave_count[3][k];
+        int eq = eq_low + eq_high;                                 // up to wavefront k
+#pragma unroll
+        for (int d = 1; d < kSelectWaves; d <<= 1) {
+            const int x = __shfl_up(eq, d);
+            eq += k >= d ? x : 0;
+        }
+        const int left = max(static_cast<int>(want) - (eq - eq_low - eq_high), 0);
+        const int first = min(k * steps * 64, n), slots_low = max(0, min(min(first + steps * 64, n), keep) - first);
+        const int holes = slots_low - wave_count[0][k] - min(left, eq_low);
+        const int movers = wave_count[1][k] + min(max(left - eq_low, 0), eq_high);
+        eq_before = sum_of_first(eq_low + eq_high, wave, lane);
+        hole_at = sum_of_first(holes, wave, lane);
+        mover_at = sum_of_first(movers, wave, lane);
+        all = sum_of_first(holes, kSelectWaves, lane);
+    }
     const uint64_t below_lane = (1ull << lane) - 1;
     auto walk = [&](auto&& visit) {                                // visit(slot, whether there is one, kept)
         int seen_eq = eq_before;
         each([&](int i, uint32_t k, bool here) {
-            const uint64_t ties = __ballot(here && k == prefix);
-            const bool kept = here && (k > prefix || (k == prefix && seen_eq + __builtin_popcountll(ties & below_lane) < static_cast<int>(want)));
-            seen_eq += __builtin_popcountll(ties);
+            const uint64_t eq = __ballot(here && k == prefix);
+            const bool kept = here && (k > prefix || (k == prefix && seen_eq + __builtin_popcountll(eq & below_lane) < static_cast<int>(want)));
+            seen_eq += __builtin_popcountll(eq);
             visit(i, here, kept);
         });
     };
-    int holes = 0, movers = 0;
-    walk([&](int i, bool here, bool kept) {
-        holes += __builtin_popcountll(__ballot(here && !kept && i < keep));
-        movers += __builtin_popcountll(__ballot(kept && i >= keep));
-    });
-    if (lane == 0) {
-        wave_hole[wave] = holes;
-        wave_mover[wave] = movers;
-    }
-    __syncthreads();
-    int hole_at = 0, mover_at = 0, all = 0;
-    for (int k = 0; k < kSelectWaves; ++k) {
-        hole_at += k < wave ? wave_hole[k] : 0;
-        mover_at += k < wave ? wave_mover[k] : 0;
-        all += wave_hole[k];
-    }
     if (tid == 0) n_moves[pair] = all;
     int32_t* to = moves + pair * 2 * g.list;
     int32_t* from_slot = to + g.list;

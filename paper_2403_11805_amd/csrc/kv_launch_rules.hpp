@@ -73,7 +73,7 @@ inline int64_t attend_groups(int64_t pairs, int64_t tokens, int head_dim) {
 
 // Eviction: workgroups that share a pair's moves, `rows` at a time each.
 inline int64_t evict_blocks(int64_t pairs, int64_t list, int64_t rows) {
-    return std::max<int64_t>(1, std::min<int64_t>((list + rows - 1) / rows, std::max<int64_t>(4096 / pairs, 4)));
+    return std::max<int64_t>(1, std::min<int64_t>((list + rows - 1) / rows, std::max<int64_t>(2048 / pairs, 4)));
 }
 
 }  // namespace kvs
