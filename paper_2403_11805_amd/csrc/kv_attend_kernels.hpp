@@ -209,47 +209,58 @@ template <bool HP> __device__ __forceinline__ float param(const uint32_t* w, int
     else return __builtin_bit_cast(float, w[i]);
 }
 
-// Where a tile lies: its page's record, its first token's row there, its first token, and how many of its 16 tokens there are.
+// Where a tile lies (all wave-uniform): its K codes and the K scales of its first token, its first token, and how many of its 16 tokens
+// there are.
 struct Tile {
-    const uint8_t* record;
-    int in_page, first, valid;
+    const uint8_t *codes, *scales;
+    int first, valid;
+};
+// From there to the minima (any width), and to the same of V.
+struct SlabSteps {
+    uint64_t mn, v_codes, v_scales;
 };
 
-// Issues the loads of a tile; ka, va: the layer's K and V slabs in records of this width.
+// Issues the loads of a tile.  Addresses are a wave-uniform base and a lane's offset that is the same for every tile.
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabAt& ka, int lane) {
+__device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, int lane) {
     constexpr int NG = D / G, kRowBytes = D * W / 8, kPiece = G / 4 * W / 8;     // bytes of a token's row, of a lane's piece per group
-    const int l16 = lane & 15, q4 = lane >> 4;
-    const uint8_t* kb = tile.record + ka.codes + static_cast<uint32_t>(tile.in_page) * kRowBytes;
+    const uint32_t at = static_cast<uint32_t>((lane & 15) * kRowBytes + (lane >> 4) * kPiece);
 #pragma unroll
-    for (int gi = 0; gi < NG; ++gi)
-        load_words<kPiece>(kb + static_cast<uint32_t>(l16 * kRowBytes + gi * (G * W / 8) + q4 * kPiece), &t.k[gi * kPiece / 4]);
+    for (int gi = 0; gi < NG; ++gi) load_words<kPiece>(tile.codes + at + gi * (G * W / 8), &t.k[gi * kPiece / 4]);
     if constexpr (W != 16) {
-        const uint32_t at = static_cast<uint32_t>((tile.in_page + 4 * q4) * NG * (HP ? 2 : 4));
-        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + ka.scale + at, t.s);
-        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + ka.mn + at, t.m);
+        constexpr int kBytes = 4 * NG * (HP ? 2 : 4);
+        const uint32_t p = static_cast<uint32_t>((lane >> 4) * kBytes);
+        load_words<kBytes>(tile.scales + p, t.s);
+        load_words<kBytes>(tile.scales + step.mn + p, t.m);
     }
 }
 // (What lies behind a sequence's tokens may be anything: V rows of missing tokens are replaced by the last one there is, and their
 // parameters are not used.)
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabAt& va, int lane) {
+__device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, int lane) {
     constexpr int NG = D / G, kRowBytes = D * W / 8, kMine = D / 16 * W / 8;
-    const int l16 = lane & 15, q4 = lane >> 4;
-    const uint8_t* vb = tile.record + va.codes + static_cast<uint32_t>(tile.in_page) * kRowBytes;
+    const uint8_t* vb = tile.codes + step.v_codes;
+    const uint32_t mine = static_cast<uint32_t>((lane & 15) * kMine);
+    if (tile.valid == 16) {                                             // (uniform)
+        const uint32_t at = static_cast<uint32_t>((lane >> 4) * 4 * kRowBytes) + mine;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        load_words<kMine>(vb + static_cast<uint32_t>(min(4 * q4 + r, tile.valid - 1) * kRowBytes + l16 * kMine), t.v[r]);
+        for (int r = 0; r < 4; ++r) load_words<kMine>(vb + at + r * kRowBytes, t.v[r]);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            load_words<kMine>(vb + (static_cast<uint32_t>(min((lane >> 4) * 4 + r, tile.valid - 1) * kRowBytes) + mine), t.v[r]);
+    }
     if constexpr (W != 16) {
-        const uint32_t at = static_cast<uint32_t>((tile.in_page + 4 * q4) * NG * (HP ? 2 : 4));
-        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + va.scale + at, t.s);
-        load_words<4 * NG * (HP ? 2 : 4)>(tile.record + va.mn + at, t.m);
+        constexpr int kBytes = 4 * NG * (HP ? 2 : 4);
+        const uint32_t p = static_cast<uint32_t>((lane >> 4) * kBytes);
+        load_words<kBytes>(tile.scales + step.v_scales + p, t.s);
+        load_words<kBytes>(tile.scales + step.v_scales + step.mn + p, t.m);
     }
 }
 
-// S^T of a tile, scaled to logits in units of log2.
+// q K^T of a tile; for codes 2^-24 times that (qsum is, too).
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u4_t* q, const float* qsum, float scale) {
+__device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u4_t* q, const float* qsum) {
     constexpr int NG = D / G, kPer = G / 32;
     f4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -269,12 +280,12 @@ __device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u
         else {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[r] = __builtin_fmaf(param<HP>(t.s, r * NG + gi) * kCode, acc[r], s[r]);
-                s[r] = __builtin_fmaf(param<HP>(t.m, r * NG + gi), qsum[gi], s[r]);
+                const float m = param<HP>(t.m, r * NG + gi);
+                s[r] = __builtin_fmaf(param<HP>(t.s, r * NG + gi), acc[r], gi ? __builtin_fmaf(m, qsum[gi], s[r]) : m * qsum[gi]);
             }
         }
     }
-    return s * scale;
+    return s;
 }
 
 // Scales and minima of a lane's four tokens in the group of its dimensions; `odd` for codes that v_codes leaves larger.
@@ -354,14 +365,17 @@ template <int D, int G> struct RowsOfWave {
     float scale;
 };
 
-// A workgroup's batch of up to 64 tiles, one per lane of each of its wavefronts.
+// A workgroup's batch of up to 64 tiles, one per lane of each of its wavefronts: what a Tile says.
 struct TileBatch {
-    uint32_t off_lo, off_hi;                   // the page's offset
-    int in_page;                               // the tile's first row there
+    uint64_t codes, scales;
     int tile0;                                 // lane l has tile tile0 + l
 };
 
-__device__ __forceinline__ int lane_value(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), lane));
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), lane));
+    return static_cast<uint64_t>(hi) << 32 | lo;
+}
 
 // The next two of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time behind every row's last
 // token.
@@ -370,10 +384,8 @@ __device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, 
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         if (k) at = tiles ? __builtin_ctzll(tiles) : at;
-        const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(lane_value(static_cast<int>(tb.off_hi), at))) << 32 |
-                             static_cast<uint32_t>(lane_value(static_cast<int>(tb.off_lo), at));
-        tile[k].record = pool + off;
-        tile[k].in_page = lane_value(tb.in_page, at);
+        tile[k].codes = pool + lane_value(tb.codes, at);
+        tile[k].scales = pool + lane_value(tb.scales, at);
         const int first = 16 * (tb.tile0 + at);
         tile[k].valid = min(16, n - first);
         tile[k].first = k && !tiles ? kNowhere : first;
@@ -381,37 +393,43 @@ __device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, 
     }
 }
 
-// The tiles of width W among a batch, two at a time.  The order of tokens does not matter to attention, so tiles are paired by width,
-// whatever the order of the pages, and the pairs (`dealt` of them of other widths so far) go to the wavefronts in turn.  K of the next pair is loaded once K of this one has been used, and V likewise: the loads are in
-// flight during the other half of the arithmetic, without a second set of registers.
+// The wavefront's share of a batch's tiles of one width: tiles are paired within their width, whatever the order of the pages (the
+// order of tokens does not matter to attention), and the pairs, counted over all widths, go to the wavefronts in turn.
+__device__ __forceinline__ uint64_t own_tiles(bool of_width, int wave, int& pairs) {
+    const uint64_t all = __ballot(of_width);
+    const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
+    const bool own = of_width && ((pairs + (rank >> 1)) & (kAttendWaves - 1)) == wave;
+    pairs += (__builtin_popcountll(all) + 1) / 2;
+    return __ballot(own);
+}
+
+// A wavefront's tiles of width W, two at a time.  K of the next pair is loaded once K of this one has been used, and V likewise: the
+// loads are in flight during the other half of the arithmetic, without a second set of registers.
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, int k_slab,
-                                     const RowsOfWave<D, G>& rw, RowState<D>& st, int wave, int lane, int& dealt) {
-    const int skip = (wave - dealt) & (kAttendWaves - 1);
-    dealt += (__builtin_popcountll(tiles) + 1) / 2;
-    for (int i = 0; i < 2 * skip; ++i) tiles &= tiles - 1;
+__device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, const RowsOfWave<D, G>& rw,
+                                     RowState<D>& st, int lane) {
     if (!tiles) return;
     const int q4 = lane >> 4;
-    const SlabAt ka = slab_at<D>(v, W, k_slab), va = slab_at<D>(v, W, k_slab + v.Hkv);
+    const uint64_t rows = static_cast<uint64_t>(v.T) * static_cast<uint32_t>(v.Hkv), params = static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
+    const SlabSteps step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
     u4_t q[D / 32];
+    float qsum[D / G];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
         const uint32_t ws[4] = {rw.q[i].x, rw.q[i].y, rw.q[i].z, rw.q[i].w};
         q[i] = W == 16 ? rw.q[i] : paired(ws);
     }
+#pragma unroll
+    for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / kCode);
+    const float scale = W == 16 ? rw.scale : rw.scale * kCode;           // of what tile_logits gives: logits in units of log2
     KRegs<D, G, W, HP> kr[2];
     VRegs<D, G, W, HP> vr[2];
     Tile tile[2], next[2];
-    auto take = [&] {
-        next_pair(tiles, tb, n, v.pool, next);
+    next_pair(tiles, tb, n, v.pool, next);
 #pragma unroll
-        for (int i = 0; i < 2 * (kAttendWaves - 1); ++i) tiles &= tiles - 1;      // the other wavefronts'
-    };
-    take();
+    for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, lane);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], va, lane);
+    for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, lane);
     bool more = true;
     while (more) {
         f4_t s[2];
@@ -419,20 +437,21 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             tile[k] = next[k];
-            s[k] = tile_logits<D, G, W, HP>(kr[k], q, rw.qsum, rw.scale);
+            s[k] = tile_logits<D, G, W, HP>(kr[k], q, qsum);
             if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[k][r] = tile[k].first + 4 * q4 + r <= rw.last ? s[k][r] : -INFINITY;
             }
-            if (rw.logits && tile[k].first != kNowhere) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k];
+            if (rw.logits && tile[k].first != kNowhere) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k] * scale;
             top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
         }
         more = tiles != 0;
         if (more) {
-            take();
+            next_pair(tiles, tb, n, v.pool, next);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], ka, lane);
+            for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, lane);
         }
+        top *= scale;
         if (__ballot(top > st.ref + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -445,15 +464,17 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
             }
         }
         const float ref = st.ref == -INFINITY ? 0.0f : st.ref;           // (a row that has seen nothing: every logit is -inf)
+        // P = hi + lo: hi has the leading 11 bits of e, so that both conversions are exact (but for what lies below 2^-24)
         h8_t hi, lo;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(s[k][r] - ref);
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], scale, -ref));
+                const float lead = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e) & 0xffffe000u);
                 st.sum += e;
-                hi[4 * k + r] = static_cast<_Float16>(e);
-                lo[4 * k + r] = static_cast<_Float16>(e - static_cast<float>(hi[4 * k + r]));
+                hi[4 * k + r] = static_cast<_Float16>(lead);
+                lo[4 * k + r] = static_cast<_Float16>(e - lead);
             }
         VScale<W> x[2];
         if constexpr (W != 16) {
@@ -463,7 +484,7 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
         unit_values<D, G, W, HP>(vr, x, hi, lo, st);
         if (more) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], va, lane);
+            for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, lane);
         }
     }
 }
@@ -546,14 +567,16 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_ke
             const uint64_t off = offs[page];
             const uint32_t b = bits[page];
             const uint32_t width = in && page_present(v, off, b) ? b : 0u;
-            tb.off_lo = static_cast<uint32_t>(off);
-            tb.off_hi = static_cast<uint32_t>(off >> 32);
-            tb.in_page = tile * 16 - page * v.T;
-            int dealt = 0;
-            walk<D, G, 16, HP>(__ballot(width == 16), tb, n, v, k_slab, rw, st, wave, lane, dealt);
-            walk<D, G, 8, HP>(__ballot(width == 8), tb, n, v, k_slab, rw, st, wave, lane, dealt);
-            walk<D, G, 4, HP>(__ballot(width == 4), tb, n, v, k_slab, rw, st, wave, lane, dealt);
-            walk<D, G, 2, HP>(__ballot(width == 2), tb, n, v, k_slab, rw, st, wave, lane, dealt);
+            const uint32_t row = static_cast<uint32_t>(k_slab * v.T + tile * 16 - page * v.T);     // of the record's rows
+            tb.codes = off + static_cast<uint64_t>(row) * (D / 8 * b);
+            tb.scales = off + v.bit_bytes * b + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
+            int pairs = 0;
+            const uint64_t tiles16 = own_tiles(width == 16, wave, pairs), tiles8 = own_tiles(width == 8, wave, pairs);
+            const uint64_t tiles4 = own_tiles(width == 4, wave, pairs), tiles2 = own_tiles(width == 2, wave, pairs);
+            walk<D, G, 16, HP>(tiles16, tb, n, v, rw, st, lane);
+            walk<D, G, 8, HP>(tiles8, tb, n, v, rw, st, lane);
+            walk<D, G, 4, HP>(tiles4, tb, n, v, rw, st, lane);
+            walk<D, G, 2, HP>(tiles2, tb, n, v, rw, st, lane);
             if (logits && wave == 0) {               // what the tokens of absent tiles would have had
                 for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
                     const int t = 16 * (2 * u + __builtin_ctzll(none));
