@@ -6,8 +6,8 @@
 // in which a lane keeps one query row (lane % 16) throughout: reference, sum and rescaling of a row need no exchange
 // between lanes, and the four S^T values of a lane (tokens 4 * (lane / 16) + 0..3 of each tile) ARE the operand P^T of the second
 // product, without a move.  The k index of an MFMA is free as long as both operands agree on it:
-//   K: a lane reads one contiguous piece of its token per group of dimensions; within eight dimensions codes come in the pairs
-//      (0,4) (1,5) (2,6) (3,7), which is how they fall out of a word, and Q is put into that order for them;
+//   K: a lane reads one contiguous piece of its token per group of dimensions; within eight dimensions Q is held in the pairs (0,4) (1,5)
+//      (2,6) (3,7), which is how codes of 8, 4 and 2 bits fall out of their words (fp16 is put into that order);
 //   V: k runs over the unit's tokens, four per quarter wavefront and tile; a lane reads the rows of its tokens at its own D/16
 //      contiguous dimensions, and one v_perm per register pairs two tokens.
 // A code of b bits in the low bits of a half is the subnormal number code * 2^-24 exactly, so a shift and a mask make an operand
@@ -144,10 +144,10 @@ __device__ __forceinline__ u4_t paired(const uint32_t* w) {
 
 constexpr float kCode = 16777216.0f;       // 2^24: what a code as a subnormal half has to be multiplied by
 
-// Eight dimensions of K from their 8 * W bits: fp16 as they are, codes in the order of paired().  (W = 2: the bits of dimensions 0-3
-// in the low half, those of 4-7 in the high one.)
+// Eight dimensions of K from their 8 * W bits, in the order of paired().  (W = 2: the bits of dimensions 0-3 in the low half, those of
+// 4-7 in the high one.)
 template <int W> __device__ __forceinline__ u4_t k_operand(const uint32_t* w) {
-    if constexpr (W == 16) return u4_t{w[0], w[1], w[2], w[3]};
+    if constexpr (W == 16) return paired(w);
     else if constexpr (W == 8)
         return u4_t{perm(w[1], w[0], 0x0c040c00u), perm(w[1], w[0], 0x0c050c01u), perm(w[1], w[0], 0x0c060c02u), perm(w[1], w[0], 0x0c070c03u)};
     else if constexpr (W == 4)
@@ -193,14 +193,20 @@ template <int D> struct RowState {
 };
 
 // What is loaded of a tile, as it lies in memory: K at the lane's token with the parameters of the lane's four tokens 4q .. 4q+3 in
-// every group; V of these four tokens at the lane's dimensions, with their parameters (HP: parameters in binary16).
+// every group; V of these four tokens at the lane's dimensions, with the parameters of the group of these (side by side where there
+// is one group, else each in a word of its own).  HP: parameters in binary16.
 template <int D, int G, int W, bool HP> struct KRegs {
     static constexpr int kWords = D * W / 128, kParams = W == 16 ? 1 : 4 * (D / G) / (HP ? 2 : 1);
     uint32_t k[kWords], s[kParams], m[kParams];
 };
 template <int D, int G, int W, bool HP> struct VRegs {
-    static constexpr int kWords = D / 16 * W / 32 > 0 ? D / 16 * W / 32 : 1, kParams = KRegs<D, G, W, HP>::kParams;
+    static constexpr int kWords = D / 16 * W / 32 > 0 ? D / 16 * W / 32 : 1, kParams = W == 16 ? 1 : (D == G && HP ? 2 : 4);
     uint32_t v[4][kWords], s[kParams], m[kParams];
+    __device__ __forceinline__ static float param(const uint32_t* w, int r) {
+        if constexpr (!HP) return __builtin_bit_cast(float, w[r]);
+        else if constexpr (D == G) return static_cast<float>(__builtin_bit_cast(h2_t, w[r / 2])[r % 2]);
+        else return static_cast<float>(__builtin_bit_cast(h2_t, w[r])[0]);
+    }
 };
 
 // Parameter i of those loaded.
@@ -220,41 +226,58 @@ struct SlabSteps {
     uint64_t mn, v_codes, v_scales;
 };
 
-// Issues the loads of a tile.  Addresses are a wave-uniform base and a lane's offset that is the same for every tile.
+// A lane's byte offsets from a tile's K codes, V codes, parameters, and parameters of the group of its V dimensions: the same for every tile of a width, so that an address is a
+// wave-uniform base and one of these.
+template <int D, int G, int W, bool HP> struct LaneAt {
+    static constexpr int kRowBytes = D * W / 8, kPiece = G / 4 * W / 8;       // bytes of a token's row, of a lane's piece of K per group
+    static constexpr int kMine = D / 16 * W / 8, kParam = HP ? 2 : 4, kParams = 4 * (D / G) * kParam;
+    uint32_t k, v, p, vp;
+    __device__ __forceinline__ explicit LaneAt(int lane)
+        : k(static_cast<uint32_t>((lane & 15) * kRowBytes + (lane >> 4) * kPiece)),
+          v(static_cast<uint32_t>((lane >> 4) * 4 * kRowBytes + (lane & 15) * kMine)), p(static_cast<uint32_t>((lane >> 4) * kParams)),
+          vp(static_cast<uint32_t>((lane >> 4) * kParams + (lane & 15) * (D / 16) / G * kParam)) {}
+    // Where loads are issued the offsets have to be 32-bit numbers made there (not 64-bit ones made in front of the loop) for the loads to
+    // take base and offset as they are: an instruction less per load.
+    __device__ __forceinline__ void here() { asm volatile("" : "+v"(k), "+v"(v), "+v"(p), "+v"(vp)); }
+};
+
+// Issues the loads of a tile.
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, int lane) {
-    constexpr int NG = D / G, kRowBytes = D * W / 8, kPiece = G / 4 * W / 8;     // bytes of a token's row, of a lane's piece per group
-    const uint32_t at = static_cast<uint32_t>((lane & 15) * kRowBytes + (lane >> 4) * kPiece);
+__device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, const LaneAt<D, G, W, HP>& at) {
+    using A = LaneAt<D, G, W, HP>;
 #pragma unroll
-    for (int gi = 0; gi < NG; ++gi) load_words<kPiece>(tile.codes + at + gi * (G * W / 8), &t.k[gi * kPiece / 4]);
+    for (int gi = 0; gi < D / G; ++gi) load_words<A::kPiece>(tile.codes + at.k + gi * (G * W / 8), &t.k[gi * A::kPiece / 4]);
     if constexpr (W != 16) {
-        constexpr int kBytes = 4 * NG * (HP ? 2 : 4);
-        const uint32_t p = static_cast<uint32_t>((lane >> 4) * kBytes);
-        load_words<kBytes>(tile.scales + p, t.s);
-        load_words<kBytes>(tile.scales + step.mn + p, t.m);
+        load_words<A::kParams>(tile.scales + at.p, t.s);
+        load_words<A::kParams>(tile.scales + step.mn + at.p, t.m);
     }
 }
 // (What lies behind a sequence's tokens may be anything: V rows of missing tokens are replaced by the last one there is, and their
 // parameters are not used.)
 template <int D, int G, int W, bool HP>
-__device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, int lane) {
-    constexpr int NG = D / G, kRowBytes = D * W / 8, kMine = D / 16 * W / 8;
+__device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, const LaneAt<D, G, W, HP>& at, int lane) {
+    using A = LaneAt<D, G, W, HP>;
     const uint8_t* vb = tile.codes + step.v_codes;
-    const uint32_t mine = static_cast<uint32_t>((lane & 15) * kMine);
     if (tile.valid == 16) {                                             // (uniform)
-        const uint32_t at = static_cast<uint32_t>((lane >> 4) * 4 * kRowBytes) + mine;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) load_words<kMine>(vb + at + r * kRowBytes, t.v[r]);
+        for (int r = 0; r < 4; ++r) load_words<A::kMine>(vb + at.v + r * A::kRowBytes, t.v[r]);
     } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            load_words<kMine>(vb + (static_cast<uint32_t>(min((lane >> 4) * 4 + r, tile.valid - 1) * kRowBytes) + mine), t.v[r]);
+            load_words<A::kMine>(vb + static_cast<uint32_t>(min((lane >> 4) * 4 + r, tile.valid - 1) * A::kRowBytes + (lane & 15) * A::kMine), t.v[r]);
     }
     if constexpr (W != 16) {
-        constexpr int kBytes = 4 * NG * (HP ? 2 : 4);
-        const uint32_t p = static_cast<uint32_t>((lane >> 4) * kBytes);
-        load_words<kBytes>(tile.scales + step.v_scales + p, t.s);
-        load_words<kBytes>(tile.scales + step.v_scales + step.mn + p, t.m);
+        const uint8_t *sb = tile.scales + step.v_scales, *mb = sb + step.mn;
+        if constexpr (D == G) {
+            load_words<A::kParams>(sb + at.vp, t.s);
+            load_words<A::kParams>(mb + at.vp, t.m);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                load_words<A::kParam>(sb + at.vp + r * (D / G) * A::kParam, t.s + r);
+                load_words<A::kParam>(mb + at.vp + r * (D / G) * A::kParam, t.m + r);
+            }
+        }
     }
 }
 
@@ -294,19 +317,12 @@ template <int W> struct VScale {
 };
 template <int D, int G, int W, bool HP>
 __device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t, int valid, int lane) {
-    constexpr int NG = D / G;
-    const int q4 = lane >> 4, mine = (lane & 15) * (D / 16) / G;
+    const int q4 = lane >> 4;
     VScale<W> x;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        float a = param<HP>(t.s, r * NG), b = param<HP>(t.m, r * NG);
-#pragma unroll
-        for (int gi = 1; gi < NG; ++gi) {
-            a = mine == gi ? param<HP>(t.s, r * NG + gi) : a;
-            b = mine == gi ? param<HP>(t.m, r * NG + gi) : b;
-        }
-        x.s[r] = a;
-        x.m[r] = b;
+        x.s[r] = t.param(t.s, r);
+        x.m[r] = t.param(t.m, r);
     }
     if (valid < 16) {                                                   // (uniform) missing tokens: 0
 #pragma unroll
@@ -317,7 +333,7 @@ __device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t, int va
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        x.s[r] *= kCode;
+        x.s[r] = __builtin_fmaf(x.s[r], kCode, 0.0f);
         x.odd[r] = x.s[r] * (W == 4 ? 1.0f / 16 : 1.0f / 4);            // (unused at width 8)
     }
     return x;
@@ -338,26 +354,33 @@ __device__ __forceinline__ uint32_t v_pair(const VRegs<D, G, W, HP>& t, const VS
     }
 }
 
-// O^T += V^T P^T of a unit, two dimensions at a time (an MFMA that adds to the sum of the one right before it would wait for it); P as
-// the sum of two halves.
-template <int D, int G, int W, bool HP, int i>
-__device__ __forceinline__ h8_t v_operand(const VRegs<D, G, W, HP>* t, const VScale<W>* x) {
-    return as_h8(u4_t{v_pair<D, G, W, HP, i>(t[0], x[0], 0), v_pair<D, G, W, HP, i>(t[0], x[0], 1),
-                      v_pair<D, G, W, HP, i>(t[1], x[1], 0), v_pair<D, G, W, HP, i>(t[1], x[1], 1)});
+// O^T += V^T P^T of a unit of NT tiles, two dimensions at a time (an MFMA that adds to the sum of the one right before it would wait for
+// it); P as the sum of two halves.
+template <int NT> struct Halves;
+template <> struct Halves<1> { typedef h4_t type; };
+template <> struct Halves<2> { typedef h8_t type; };
+__device__ __forceinline__ f4_t mfma(h8_t a, h8_t b, f4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4_t mfma(h4_t a, h4_t b, f4_t c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
+template <int D, int G, int W, bool HP, int NT, int i>
+__device__ __forceinline__ typename Halves<NT>::type v_operand(const VRegs<D, G, W, HP>* t, const VScale<W>* x) {
+    const u2_t a = {v_pair<D, G, W, HP, i>(t[0], x[0], 0), v_pair<D, G, W, HP, i>(t[0], x[0], 1)};
+    if constexpr (NT == 1) return __builtin_bit_cast(h4_t, a);
+    else return as_h8(u4_t{a.x, a.y, v_pair<D, G, W, HP, i>(t[1], x[1], 0), v_pair<D, G, W, HP, i>(t[1], x[1], 1)});
 }
-template <int D, int G, int W, bool HP, int i = 0>
-__device__ __forceinline__ void unit_values(const VRegs<D, G, W, HP>* t, const VScale<W>* x, const h8_t& hi, const h8_t& lo, RowState<D>& st) {
-    const h8_t a = v_operand<D, G, W, HP, i>(t, x), b = v_operand<D, G, W, HP, i + 1>(t, x);
-    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, lo, st.o[i], 0, 0, 0);
-    st.o[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, lo, st.o[i + 1], 0, 0, 0);
-    st.o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, hi, st.o[i], 0, 0, 0);
-    st.o[i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, hi, st.o[i + 1], 0, 0, 0);
-    if constexpr (i + 2 < D / 16) unit_values<D, G, W, HP, i + 2>(t, x, hi, lo, st);
+template <int D, int G, int W, bool HP, int NT, int i = 0>
+__device__ __forceinline__ void unit_values(const VRegs<D, G, W, HP>* t, const VScale<W>* x, const typename Halves<NT>::type& hi,
+                                            const typename Halves<NT>::type& lo, RowState<D>& st) {
+    const auto a = v_operand<D, G, W, HP, NT, i>(t, x), b = v_operand<D, G, W, HP, NT, i + 1>(t, x);
+    st.o[i] = mfma(a, lo, st.o[i]);
+    st.o[i + 1] = mfma(b, lo, st.o[i + 1]);
+    st.o[i] = mfma(a, hi, st.o[i]);
+    st.o[i + 1] = mfma(b, hi, st.o[i + 1]);
+    if constexpr (i + 2 < D / 16) unit_values<D, G, W, HP, NT, i + 2>(t, x, hi, lo, st);
 }
 
 // What a wavefront knows of its rows.
 template <int D, int G> struct RowsOfWave {
-    u4_t q[D / 32];                            // the lane's pieces, dimensions in memory order
+    u4_t q[D / 32];                            // the lane's pieces, in the order of paired()
     float qsum[D / G];                         // of every group, the row's sum of q
     int last;                                  // the last token the lane's row sees (-1: none)
     int all_see;                               // tokens up to this one are seen by every row
@@ -377,12 +400,12 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
     return static_cast<uint64_t>(hi) << 32 | lo;
 }
 
-// The next two of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time behind every row's last
+// The next NT of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time behind every row's last
 // token.
-__device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, int n, uint8_t* pool, Tile* tile) {
+template <int NT> __device__ __forceinline__ void next_tiles(uint64_t& tiles, const TileBatch& tb, int n, uint8_t* pool, Tile* tile) {
     int at = __builtin_ctzll(tiles);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < NT; ++k) {
         if (k) at = tiles ? __builtin_ctzll(tiles) : at;
         tile[k].codes = pool + lane_value(tb.codes, at);
         tile[k].scales = pool + lane_value(tb.scales, at);
@@ -393,51 +416,59 @@ __device__ __forceinline__ void next_pair(uint64_t& tiles, const TileBatch& tb, 
     }
 }
 
-// The wavefront's share of a batch's tiles of one width: tiles are paired within their width, whatever the order of the pages (the
-// order of tokens does not matter to attention), and the pairs, counted over all widths, go to the wavefronts in turn.
-__device__ __forceinline__ uint64_t own_tiles(bool of_width, int wave, int& pairs) {
+// The wavefront's share of a batch's tiles of one width: tiles are put together within their width, whatever the order of the pages
+// (the order of tokens does not matter to attention), and the units of NT, counted over all widths, go to the wavefronts in turn.
+// (Without a branch: copies that the compiler makes of registers where a branch of some lanes ends have gone wrong here.)
+template <int NT> __device__ __forceinline__ uint64_t own_tiles(bool of_width, int wave, int& units) {
     const uint64_t all = __ballot(of_width);
     const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
-    const bool own = of_width && ((pairs + (rank >> 1)) & (kAttendWaves - 1)) == wave;
-    pairs += (__builtin_popcountll(all) + 1) / 2;
-    return __ballot(own);
+    const int turn = (units + rank / NT) & (kAttendWaves - 1);
+    units += (__builtin_popcountll(all) + NT - 1) / NT;
+    return all & __ballot(turn == wave);
 }
 
-// A wavefront's tiles of width W, two at a time.  K of the next pair is loaded once K of this one has been used, and V likewise: the
+// A wavefront's tiles of width W, NT at a time.  K of the next unit is loaded once K of this one has been used, and V likewise: the
 // loads are in flight during the other half of the arithmetic, without a second set of registers.
-template <int D, int G, int W, bool HP>
+template <int D, int G, int W, bool HP, int NT>
 __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, const RowsOfWave<D, G>& rw,
                                      RowState<D>& st, int lane) {
     if (!tiles) return;
+    // What depends on the lane is worked out here, width by width: the compiler would keep it in registers for all four.
+    asm volatile("" : "+v"(lane));
     const int q4 = lane >> 4;
     const uint64_t rows = static_cast<uint64_t>(v.T) * static_cast<uint32_t>(v.Hkv), params = static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
     const SlabSteps step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
-    u4_t q[D / 32];
     float qsum[D / G];
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const uint32_t ws[4] = {rw.q[i].x, rw.q[i].y, rw.q[i].z, rw.q[i].w};
-        q[i] = W == 16 ? rw.q[i] : paired(ws);
-    }
 #pragma unroll
     for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / kCode);
     const float scale = W == 16 ? rw.scale : rw.scale * kCode;           // of what tile_logits gives: logits in units of log2
-    KRegs<D, G, W, HP> kr[2];
-    VRegs<D, G, W, HP> vr[2];
-    Tile tile[2], next[2];
-    next_pair(tiles, tb, n, v.pool, next);
+    KRegs<D, G, W, HP> kr[NT];
+    VRegs<D, G, W, HP> vr[NT];
+    Tile tile[NT], next[NT];
+    LaneAt<D, G, W, HP> at(lane);
+    next_tiles<NT>(tiles, tb, n, v.pool, next);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, lane);
+    for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, at);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, lane);
+    for (int k = 0; k < NT; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, at, lane);
     bool more = true;
     while (more) {
-        f4_t s[2];
+        f4_t s[NT];
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            tile[k] = next[k];
+            s[k] = tile_logits<D, G, W, HP>(kr[k], rw.q, qsum);
+        }
+        more = tiles != 0;
+        if (more) {
+            next_tiles<NT>(tiles, tb, n, v.pool, next);
+            at.here();
+#pragma unroll
+            for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, at);
+        }
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            tile[k] = next[k];
-            s[k] = tile_logits<D, G, W, HP>(kr[k], q, qsum);
+        for (int k = 0; k < NT; ++k) {
             if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[k][r] = tile[k].first + 4 * q4 + r <= rw.last ? s[k][r] : -INFINITY;
@@ -445,29 +476,22 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
             if (rw.logits && tile[k].first != kNowhere) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k] * scale;
             top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
         }
-        more = tiles != 0;
-        if (more) {
-            next_pair(tiles, tb, n, v.pool, next);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, lane);
-        }
         top *= scale;
-        if (__ballot(top > st.ref + kSlack)) {
+        if (__ballot(top > st.ref + kSlack)) {                           // (uniform)
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (top > st.ref + kSlack) {
-                const float to = top - kTop, f = __builtin_amdgcn_exp2f(st.ref - to);
-                st.ref = to;
-                st.sum *= f;
+            const bool moves = top > st.ref + kSlack;
+            const float to = moves ? top - kTop : st.ref, f = moves ? __builtin_amdgcn_exp2f(st.ref - to) : 1.0f;
+            st.ref = to;
+            st.sum *= f;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
-            }
+            for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
         }
         const float ref = st.ref == -INFINITY ? 0.0f : st.ref;           // (a row that has seen nothing: every logit is -inf)
         // P = hi + lo: hi has the leading 11 bits of e, so that both conversions are exact (but for what lies below 2^-24)
-        h8_t hi, lo;
+        typename Halves<NT>::type hi, lo;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < NT; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], scale, -ref));
@@ -476,15 +500,16 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
                 hi[4 * k + r] = static_cast<_Float16>(lead);
                 lo[4 * k + r] = static_cast<_Float16>(e - lead);
             }
-        VScale<W> x[2];
+        VScale<W> x[NT];
         if constexpr (W != 16) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) x[k] = v_scale<D, G, W, HP>(vr[k], tile[k].valid, lane);
+            for (int k = 0; k < NT; ++k) x[k] = v_scale<D, G, W, HP>(vr[k], tile[k].valid, lane);
         }
-        unit_values<D, G, W, HP>(vr, x, hi, lo, st);
+        unit_values<D, G, W, HP, NT>(vr, x, hi, lo, st);
         if (more) {
+            at.here();
 #pragma unroll
-            for (int k = 0; k < 2; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, lane);
+            for (int k = 0; k < NT; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, at, lane);
         }
     }
 }
@@ -492,11 +517,11 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
 // Grid: g.groups workgroups, each a run of the line.  The wavefronts of a workgroup take the pairs of tiles of a piece of the run (the part
 // that lies in one sequence, kv head and row tile) in turn, each with a state of its own; the four states meet in LDS.
 template <int D, int G, bool HP>
-__global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
+__global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                    float* __restrict__ logits) {
-    constexpr int DL = D / 16, NG = D / G;
+    constexpr int DL = D / 16, NG = D / G, NT = D == 256 ? 1 : 2;      // (256: the registers of two tiles do not fit)
     extern __shared__ float o_lds[];                 // [kAttendWaves][tile_rows][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
     const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
@@ -531,18 +556,20 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_ke
         rw.last = ok ? n - sw.count + nth : -1;
         rw.all_see = n - sw.count + rt * 16 / g.per;
         rw.logits = logits && ok ? logits + ((static_cast<int64_t>(s) * v.Hkv + h) * g.rows + j) * v.N : nullptr;
-        const _Float16* qp = q + static_cast<int64_t>(sw.first + (ok ? nth : 0)) * g.q_stride + (ok ? head : 0) * D;
+        const _Float16* qp = q + static_cast<int64_t>(sw.first + (ok ? nth : 0)) * g.q_stride + (ok ? head : 0) * D;     // (count >= 1)
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi) {
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < G / 32; ++i) {
-                u4_t w = {0u, 0u, 0u, 0u};
-                if (ok) w = *reinterpret_cast<const u4_t*>(qp + gi * G + q4 * (G / 4) + i * 8);
+                u4_t w = *reinterpret_cast<const u4_t*>(qp + gi * G + q4 * (G / 4) + i * 8);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = ok ? w[e] : 0u;
                 const h8_t x = as_h8(w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum += static_cast<float>(x[e]);
-                rw.q[gi * (G / 32) + i] = w;
+                const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+                rw.q[gi * (G / 32) + i] = paired(ws);
             }
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
@@ -562,21 +589,22 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 256 ? 1 : 2) void attend_ke
             TileBatch tb;
             tb.tile0 = 2 * u;
             const int tile = 2 * u + lane;
-            const bool in = tile < 2 * u_end && tile * 16 < n;
-            const int page = !in ? 0 : (v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile);
+            const bool in = (tile < 2 * u_end) & (tile * 16 < n);
+            const int tile_page = v.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(tile), v.page_of_tile)) : tile;
+            const int page = in ? tile_page : 0;
             const uint64_t off = offs[page];
             const uint32_t b = bits[page];
-            const uint32_t width = in && page_present(v, off, b) ? b : 0u;
+            const uint32_t width = in & page_present(v, off, b) ? b : 0u;
             const uint32_t row = static_cast<uint32_t>(k_slab * v.T + tile * 16 - page * v.T);     // of the record's rows
             tb.codes = off + static_cast<uint64_t>(row) * (D / 8 * b);
             tb.scales = off + v.bit_bytes * b + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
-            int pairs = 0;
-            const uint64_t tiles16 = own_tiles(width == 16, wave, pairs), tiles8 = own_tiles(width == 8, wave, pairs);
-            const uint64_t tiles4 = own_tiles(width == 4, wave, pairs), tiles2 = own_tiles(width == 2, wave, pairs);
-            walk<D, G, 16, HP>(tiles16, tb, n, v, rw, st, lane);
-            walk<D, G, 8, HP>(tiles8, tb, n, v, rw, st, lane);
-            walk<D, G, 4, HP>(tiles4, tb, n, v, rw, st, lane);
-            walk<D, G, 2, HP>(tiles2, tb, n, v, rw, st, lane);
+            int dealt = 0;
+            const uint64_t tiles16 = own_tiles<NT>(width == 16, wave, dealt), tiles8 = own_tiles<NT>(width == 8, wave, dealt);
+            const uint64_t tiles4 = own_tiles<NT>(width == 4, wave, dealt), tiles2 = own_tiles<NT>(width == 2, wave, dealt);
+            walk<D, G, 16, HP, NT>(tiles16, tb, n, v, rw, st, lane);
+            walk<D, G, 8, HP, NT>(tiles8, tb, n, v, rw, st, lane);
+            walk<D, G, 4, HP, NT>(tiles4, tb, n, v, rw, st, lane);
+            walk<D, G, 2, HP, NT>(tiles2, tb, n, v, rw, st, lane);
             if (logits && wave == 0) {               // what the tokens of absent tiles would have had
                 for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
                     const int t = 16 * (2 * u + __builtin_ctzll(none));
