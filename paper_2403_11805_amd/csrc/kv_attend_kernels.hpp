@@ -594,7 +594,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_ker
             const int page = in ? tile_page : 0;
             const uint64_t off = offs[page];
             const uint32_t b = bits[page];
-            const uint32_t width = in & page_present(v, off, b) ? b : 0u;
+            const uint32_t width = (in & page_present(v, off, b)) ? b : 0u;
             const uint32_t row = static_cast<uint32_t>(k_slab * v.T + tile * 16 - page * v.T);     // of the record's rows
             tb.codes = off + static_cast<uint64_t>(row) * (D / 8 * b);
             tb.scales = off + v.bit_bytes * b + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
@@ -679,56 +679,55 @@ __device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
 }
 
-// Joins the shares of a row that several workgroups have had a part of (and writes the zeros of an empty sequence): one workgroup per
-// row, its threads four channels and every (1024 / D)-th share each.  `weight` holds as many floats as there are workgroups.
+// What is left when every workgroup has done its run.  The first `joins` workgroups, one per row of a (sequence, kv head), join the
+// shares of rows that several workgroups have had a part of (and write the zeros of an empty sequence): a thread four channels and
+// every (1024 / D)-th share.  The others, `blocks` of them per (sequence, kv head), make the weights of 1024 keys each from the logits
+// that the rows have left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
+// `weight` holds as many floats as the attention has workgroups.
+constexpr int kMaxPairRows = 1024;
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(PagesView v, AttendGeom g, const int32_t* __restrict__ row_start,
-                                                          const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                          _Float16* __restrict__ out) {
+__global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendGeom g, int32_t joins, int32_t blocks,
+                                                            const int32_t* __restrict__ row_start, const float* __restrict__ part_o,
+                                                            const float* __restrict__ part_ml, const float* __restrict__ logits,
+                                                            const float* mass_in, float* mass, _Float16* __restrict__ out) {
     constexpr int kQuads = D / 4, kParts = 256 / kQuads;
     extern __shared__ float weight[];
     __shared__ float total;
     __shared__ f4_t o_lds[kParts][kQuads];
-    const int lane = threadIdx.x & 63;
-    const int seq_head = static_cast<int>(blockIdx.x) / g.rows, j = static_cast<int>(blockIdx.x) - seq_head * g.rows;
-    const int s = seq_head / v.Hkv, h = seq_head - s * v.Hkv;
-    const RowShares sh = row_shares(v, g, row_start, lane, s, h, j);
-    if (sh.used == 1 || j >= min(sh.w.count, g.max_rows) * g.per) return;
-    const int64_t first = sh.first * g.tile_rows + j % 16;
-    const int quad = threadIdx.x % kQuads, part = threadIdx.x / kQuads;
-    if (threadIdx.x < 64) {
-        float ref, sum;
-        row_total(part_ml, first, g.tile_rows, sh.used, lane, weight, ref, sum);
-        if (lane == 0) total = sum;
-    }
-    __syncthreads();
-    f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-    const f4_t* src = reinterpret_cast<const f4_t*>(part_o + first * D) + quad;
-    const int64_t step = static_cast<int64_t>(g.tile_rows) * kQuads;
-#pragma unroll 4
-    for (int k = part; k < sh.used; k += kParts) o += src[k * step] * weight[k];
-    o_lds[part][quad] = o;
-    __syncthreads();
-    if (part) return;
-#pragma unroll
-    for (int k = 1; k < kParts; ++k) o += o_lds[k][quad];
-    const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-    h4_t x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
-    reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(sh.w.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D)[quad] = x;
-}
-
-// The weights of a pair's keys, from the logits its rows left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
-// One workgroup per pair and 1024 tokens (`blocks` of them per pair).
-constexpr int kMaxPairRows = 1024;
-__global__ __launch_bounds__(256) void attend_mass_kernel(PagesView v, AttendGeom g, int32_t blocks, const int32_t* __restrict__ row_start,
-                                                          const float* __restrict__ part_ml, const float* __restrict__ logits,
-                                                          const float* mass_in, float* mass) {
     __shared__ float refs[kMaxPairRows], invs[kMaxPairRows];
-    const int64_t pair = blockIdx.x / blocks;
-    const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair % v.Hkv), t0 = static_cast<int>(blockIdx.x % blocks) * 1024;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int id = static_cast<int>(blockIdx.x);
+    if (id < joins) {
+        const int pair = id / g.rows, j = id - pair * g.rows, s = pair / v.Hkv, h = pair - s * v.Hkv;
+        const RowShares sh = row_shares(v, g, row_start, lane, s, h, j);
+        if (sh.used == 1 || j >= min(sh.w.count, g.max_rows) * g.per) return;
+        const int64_t first = sh.first * g.tile_rows + j % 16;
+        const int quad = threadIdx.x % kQuads, part = threadIdx.x / kQuads;
+        if (wave == 0) {
+            float ref, sum;
+            row_total(part_ml, first, g.tile_rows, sh.used, lane, weight, ref, sum);
+            if (lane == 0) total = sum;
+        }
+        __syncthreads();
+        f4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+        const f4_t* src = reinterpret_cast<const f4_t*>(part_o + first * D) + quad;
+        const int64_t step = static_cast<int64_t>(g.tile_rows) * kQuads;
+#pragma unroll 4
+        for (int k = part; k < sh.used; k += kParts) o += src[k * step] * weight[k];
+        o_lds[part][quad] = o;
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int k = 1; k < kParts; ++k) o += o_lds[k][quad];
+        const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+        h4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[e] * inv);
+        reinterpret_cast<h4_t*>(out + (static_cast<int64_t>(sh.w.first + j / g.per) * v.Hq + h * g.per + j % g.per) * D)[quad] = x;
+        return;
+    }
+    const int64_t pair = (id - joins) / blocks;
+    const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair % v.Hkv), t0 = (id - joins) % blocks * 1024;
     const RowShares sh = row_shares(v, g, row_start, lane, s, h, 0);
     const int n = sh.w.n, count = min(sh.w.count, g.max_rows) * g.per;
     if (t0 >= n || count == 0) return;
@@ -745,6 +744,7 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(PagesView v, AttendGeo
     const int t = t0 + static_cast<int>(threadIdx.x) * 4;
     if (t >= n) return;
     f4_t w = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int j = 0; j < count; ++j) {
         const f4_t x = *reinterpret_cast<const f4_t*>(logits + (pair * g.rows + j) * v.N + t);
         const float ref = refs[j], inv = invs[j];

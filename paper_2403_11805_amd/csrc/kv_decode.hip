@@ -133,7 +133,7 @@ int check_attend(const kv_shape_t* shape, int32_t n_seqs, int32_t max_rows) {
     const int64_t rows = static_cast<int64_t>(shape->n_q_heads / shape->n_kv_heads) * max_rows;
     if (rows > kMaxPairRows) return fail(KV_ESHAPE, "more than %d query rows per kv head", kMaxPairRows);
     const int64_t pairs = static_cast<int64_t>(n_seqs) * shape->n_kv_heads;
-    if (pairs * ((rows + 15) / 16) > 0x7fffffffLL / ((shape->n_tokens + 2047) / 32) || pairs * rows > 0x7fffffffLL)
+    if (pairs * ((rows + 15) / 16) > 0x7fffffffLL / ((shape->n_tokens + 2047) / 32) || pairs * rows > 0x3fffffffLL)
         return fail(KV_ESHAPE, "n_seqs * n_kv_heads * n_tokens too large for one call");
     return KV_OK;
 }
@@ -234,18 +234,15 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     }
 #undef KV_LAUNCH
     if (int rc = launch_status("attend_kernel launch")) return rc;
-    const dim3 join(static_cast<uint32_t>(pairs * g.rows));
-#define KV_LAUNCH(D) \
-    hipLaunchKernelGGL((attend_join_kernel<D>), join, dim3(256), static_cast<uint32_t>(g.groups) * 4, st, view, g, row_start, part_o, part_ml, o16)
+    const int32_t joins = static_cast<int32_t>(pairs * g.rows);
+    const dim3 finish(static_cast<uint32_t>(joins + (mass ? pairs * blocks : 0)));
+    const uint32_t weights = static_cast<uint32_t>(g.groups) * 4;
+#define KV_LAUNCH(D)                                                                                                                  \
+    hipLaunchKernelGGL((attend_finish_kernel<D>), finish, dim3(256), weights, st, view, g, joins, blocks, row_start, part_o, part_ml, \
+                       logits, mass_in, mass, o16)
     KV_BY_HEAD_DIM(shape->head_dim, KV_LAUNCH);
 #undef KV_LAUNCH
-    if (int rc = launch_status("attend_join_kernel launch")) return rc;
-    if (mass) {
-        hipLaunchKernelGGL(attend_mass_kernel, dim3(static_cast<uint32_t>(pairs * blocks)), dim3(256), 0, st, view, g, blocks, row_start,
-                           part_ml, logits, mass_in, mass);
-        return launch_status("attend_mass_kernel launch");
-    }
-    return KV_OK;
+    return launch_status("attend_finish_kernel launch");
 }
 
 uint64_t kv_evict_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int32_t n_layers, int32_t keep) {
