@@ -10,9 +10,13 @@
 //      (2,6) (3,7), which is how codes of 8, 4 and 2 bits fall out of their words (fp16 is put into that order);
 //   V: k runs over the unit's tokens, four per quarter wavefront and tile; a lane reads the rows of its tokens at its own D/16
 //      contiguous dimensions, and one v_perm per register pairs two tokens.
-// A code of b bits in the low bits of a half is the subnormal number code * 2^-24 exactly, so a shift and a mask make an operand
-// of two codes.  K is not dequantised: the MFMAs sum q * code per group, and scale and minimum enter once per (token, group),
-//     S = sum_g (2^24 s_g) acc_g + mn_g qsum_g.
+// A code of b bits in the mantissa of a half, the other bits 0, is the subnormal number code * 2^-24 (times the power of two of where
+// it stands) exactly, so a shift and a mask make an operand of two codes.  K is not dequantised: the MFMAs sum q * code per group, and
+// scale and minimum enter once per (token, group),
+//     S = sum_g (s_g / 2^-24) acc_g + mn_g qsum_g.
+// An MFMA lines its products up by the exponents without shifting a subnormal's leading zeros out first, and keeps so many bits less of
+// them: K's codes of 4 and 2 bits therefore stand at the mantissa's top (weights of 2-bit pages are off by 8e-7
+// so, by 7e-5 with the codes at its low end); those of 8 bits, which one byte move puts in place, lose 2 bits of 24 (off by 7e-7).
 // V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s.  P enters as the sum of two
 // halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
 #pragma once
@@ -142,17 +146,18 @@ __device__ __forceinline__ u4_t paired(const uint32_t* w) {
     return u4_t{perm(w[2], w[0], 0x05040100u), perm(w[2], w[0], 0x07060302u), perm(w[3], w[1], 0x05040100u), perm(w[3], w[1], 0x07060302u)};
 }
 
-constexpr float kCode = 16777216.0f;       // 2^24: what a code as a subnormal half has to be multiplied by
+constexpr float kCode = 16777216.0f;       // 2^24: what a code in the low bits of a half has to be multiplied by
 
-// Eight dimensions of K from their 8 * W bits, in the order of paired().  (W = 2: the bits of dimensions 0-3 in the low half, those of
-// 4-7 in the high one.)
+// Eight dimensions of K from their 8 * W bits, in the order of paired(); codes come out as code / k_code<W>().  (W = 2: the
+// bits of dimensions 0-3 in the upper byte of the low half, those of 4-7 in that of the high one.)
+template <int W> __device__ __forceinline__ constexpr float k_code() { return W == 4 ? kCode / 64 : W == 2 ? kCode / 256 : kCode; }
 template <int W> __device__ __forceinline__ u4_t k_operand(const uint32_t* w) {
     if constexpr (W == 16) return paired(w);
     else if constexpr (W == 8)
         return u4_t{perm(w[1], w[0], 0x0c040c00u), perm(w[1], w[0], 0x0c050c01u), perm(w[1], w[0], 0x0c060c02u), perm(w[1], w[0], 0x0c070c03u)};
     else if constexpr (W == 4)
-        return u4_t{w[0] & 0x000f000fu, (w[0] >> 4) & 0x000f000fu, (w[0] >> 8) & 0x000f000fu, (w[0] >> 12) & 0x000f000fu};
-    else return u4_t{w[0] & 0x00030003u, (w[0] >> 2) & 0x00030003u, (w[0] >> 4) & 0x00030003u, (w[0] >> 6) & 0x00030003u};
+        return u4_t{(w[0] << 6) & 0x03c003c0u, (w[0] << 2) & 0x03c003c0u, (w[0] >> 2) & 0x03c003c0u, (w[0] >> 6) & 0x03c003c0u};
+    else return u4_t{w[0] & 0x03000300u, (w[0] >> 2) & 0x03000300u, (w[0] >> 4) & 0x03000300u, (w[0] >> 6) & 0x03000300u};
 }
 
 __device__ __forceinline__ h8_t as_h8(u4_t v) { return __builtin_bit_cast(h8_t, v); }
@@ -281,7 +286,7 @@ __device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, 
     }
 }
 
-// q K^T of a tile; for codes 2^-24 times that (qsum is, too).
+// q K^T of a tile; for codes that divided by k_code (qsum is, too).
 template <int D, int G, int W, bool HP>
 __device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u4_t* q, const float* qsum) {
     constexpr int NG = D / G, kPer = G / 32;
@@ -294,7 +299,7 @@ __device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u
             const int j = gi * kPer + i;
             u4_t a;
             if constexpr (W == 2) {
-                const uint32_t one = perm(0u, t.k[j / 2], (j & 1) ? 0x0c030c02u : 0x0c010c00u);
+                const uint32_t one = perm(0u, t.k[j / 2], (j & 1) ? 0x030c020cu : 0x010c000cu);
                 a = k_operand<2>(&one);
             } else a = k_operand<W>(&t.k[j * (W / 4)]);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(a), as_h8(q[j]), acc, 0, 0, 0);
@@ -440,8 +445,8 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
     const SlabSteps step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
     float qsum[D / G];
 #pragma unroll
-    for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / kCode);
-    const float scale = W == 16 ? rw.scale : rw.scale * kCode;           // of what tile_logits gives: logits in units of log2
+    for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / k_code<W>());
+    const float scale = W == 16 ? rw.scale : rw.scale * k_code<W>();     // of what tile_logits gives: logits in units of log2
     KRegs<D, G, W, HP> kr[NT];
     VRegs<D, G, W, HP> vr[NT];
     Tile tile[NT], next[NT];
