@@ -43,20 +43,22 @@ struct AttendGeom {
     int32_t row_tiles;               // ceil(rows / 16)
     int32_t tile_rows;               // min(16, rows)
     int32_t groups;                  // workgroups that the work of all sequences is divided among
+    int32_t step;                    // units that a workgroup's wavefronts take at once
     int64_t q_stride;
     float scale_log2e;               // log2(e) / sqrt(D)
 };
 
 // How the work is divided.  The units of all sequences, kv heads and row tiles stand in one line (sequence by sequence, head by head),
-// and every workgroup takes an equal run of it, whatever the lengths are: all run at once and end together, and a run goes on
-// through the next head or sequence where one ends.  In front of the units of every (kv head, row tile) pair the line has kPieceCost
-// places for what beginning and ending a piece takes, so that runs through many short ones are shorter.  The lengths are on the
+// and every workgroup takes an equal run of it, whatever the lengths are: all run at once and end together.  The lengths are on the
 // device, so a workgroup finds its run itself, a lane per sequence, 64 sequences a step.
+//   Little work: a run is `step` units, one of its wavefronts' steps, or two such, and the units of every (kv head, row tile) pair are
+//     rounded up to whole runs, so that a workgroup has part of one pair only.
+//   More than that: a run goes on through the next pair where one ends.  In front of a pair's units the line has kPieceCost places for
+//     what beginning and ending a piece takes, so that runs through many short ones are shorter.
 constexpr int kPieceCost = 8;
 struct SeqWork {
     int n, first, count;             // tokens; its new rows
     int units, pairs;                // units of 32 tokens; (kv head, row tile) pairs, none without rows
-    __device__ __forceinline__ int each() const { return units ? units + kPieceCost : 0; }     // places of a pair
 };
 __device__ __forceinline__ SeqWork work_of(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int s) {
     SeqWork w = {0, 0, 0, 0, 0};
@@ -75,40 +77,49 @@ __device__ __forceinline__ SeqWork of_lane(const SeqWork& w, int l) {
             __builtin_amdgcn_readlane(w.units, l), __builtin_amdgcn_readlane(w.pairs, l)};
 }
 
+// Sum over the lanes up to this one (all active): within rows of 16, then the rows' last lanes.
+__device__ __forceinline__ int prefix_sum(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // lane 15 to row 1, 47 to row 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // lane 31 to rows 2 and 3
+    return x;
+}
+
 // Where the lanes' sequences lie in the line.
 struct Line {
     SeqWork mine;                    // of sequence s0 + lane
     int s0, end;                     // end: of the lane's sequence
-    int run;                         // units of a workgroup's run
+    int round, cost;                 // a pair's places: its units in multiples of `round` (a power of two), and `cost` in front
+    int run;                         // places of a workgroup's run
 
-    __device__ __forceinline__ void step(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane, int before) {
-        end = mine.each() * mine.pairs;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int x = __shfl_up(end, d);
-            end += lane >= d ? x : 0;
-        }
-        end += before;
-    }
+    __device__ __forceinline__ static int places(int units, int round, int cost) { return units ? ((units + round - 1) & -round) + cost : 0; }
+    __device__ __forceinline__ int each(const SeqWork& w) const { return places(w.units, round, cost); }
     __device__ __forceinline__ void start(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
         s0 = 0;
         mine = work_of(v, g, row_start, lane);
-        step(v, g, row_start, lane, 0);
-        int total = __builtin_amdgcn_readlane(end, 63);
+        const int one = prefix_sum(places(mine.units, g.step, 0) * mine.pairs), two = prefix_sum(places(mine.units, 2 * g.step, 0) * mine.pairs);
+        const int long_ = prefix_sum(places(mine.units, 1, kPieceCost) * mine.pairs);
+        int t1 = __builtin_amdgcn_readlane(one, 63), t2 = __builtin_amdgcn_readlane(two, 63), tl = __builtin_amdgcn_readlane(long_, 63);
         for (int s = 64; s < v.n_seqs; s += 64) {
             const SeqWork w = work_of(v, g, row_start, s + lane);
-            int x = w.each() * w.pairs;
-#pragma unroll
-            for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-            total += x;
+            t1 += __builtin_amdgcn_readlane(prefix_sum(places(w.units, g.step, 0) * w.pairs), 63);
+            t2 += __builtin_amdgcn_readlane(prefix_sum(places(w.units, 2 * g.step, 0) * w.pairs), 63);
+            tl += __builtin_amdgcn_readlane(prefix_sum(places(w.units, 1, kPieceCost) * w.pairs), 63);
         }
-        run = __builtin_amdgcn_readfirstlane(max(kAttendMinUnits + kPieceCost, (total + g.groups - 1) / g.groups));
+        const bool fits1 = t1 <= g.groups * g.step, fits2 = t2 <= g.groups * 2 * g.step;
+        round = fits1 ? g.step : fits2 ? 2 * g.step : 1;
+        cost = fits1 | fits2 ? 0 : kPieceCost;
+        run = fits1 | fits2 ? round : (tl + g.groups - 1) / g.groups;
+        end = fits1 ? one : fits2 ? two : long_;
     }
     __device__ __forceinline__ void next(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
         const int before = __builtin_amdgcn_readlane(end, 63);
         s0 += 64;
         mine = work_of(v, g, row_start, s0 + lane);
-        step(v, g, row_start, lane, before);
+        end = before + prefix_sum(each(mine) * mine.pairs);
     }
 };
 
@@ -133,7 +144,7 @@ __device__ __forceinline__ RowShares row_shares(const PagesView& v, const Attend
     RowShares x;
     x.w = of_lane(line.mine, l);
     const int row_tiles = x.w.pairs / v.Hkv, pair = h * row_tiles + j / 16;
-    const int begin = __builtin_amdgcn_readlane(line.end, l) - x.w.each() * (x.w.pairs - pair) + kPieceCost, wg = begin / line.run;
+    const int begin = __builtin_amdgcn_readlane(line.end, l) - line.each(x.w) * (x.w.pairs - pair) + line.cost, wg = begin / line.run;
     x.used = x.w.units ? (begin + x.w.units - 1) / line.run - wg + 1 : 0;
     x.first = wg + pair_number(v, g, s, pair);
     return x;
@@ -545,9 +556,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_ker
         if (!behind) return;                         // (the end of the line; uniform in the workgroup)
         const int l = __builtin_ctzll(behind), s = line.s0 + l;
         const SeqWork sw = of_lane(line.mine, l);
-        const int n = sw.n, local = at - (__builtin_amdgcn_readlane(line.end, l) - sw.each() * sw.pairs);
-        const int pair = local / sw.each(), place = local - pair * sw.each(), places = min(sw.each() - place, run_end - at);
-        const int u_begin = max(place - kPieceCost, 0), u_end = place + places - kPieceCost;
+        const int each = line.each(sw), n = sw.n, local = at - (__builtin_amdgcn_readlane(line.end, l) - each * sw.pairs);
+        const int pair = local / each, place = local - pair * each, places = min(each - place, run_end - at);
+        const int u_begin = max(place - line.cost, 0), u_end = min(place + places - line.cost, sw.units);
         const int row_tiles = sw.pairs / v.Hkv, h = pair / row_tiles, rt = pair - h * row_tiles;
         const int count = min(sw.count, g.max_rows);
         at += places;

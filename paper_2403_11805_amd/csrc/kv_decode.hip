@@ -108,6 +108,7 @@ AttendGeom attend_geom(const kv_shape_t& s, int32_t n_seqs, int32_t max_rows) {
     g.rows = g.per * max_rows;
     g.row_tiles = (g.rows + 15) / 16;
     g.tile_rows = std::min(16, g.rows);
+    g.step = attend_step(s.head_dim);
     g.groups = static_cast<int32_t>(attend_groups(static_cast<int64_t>(n_seqs) * s.n_kv_heads * g.row_tiles, s.n_tokens, s.head_dim));
     g.scale_log2e = static_cast<float>(1.4426950408889634 / std::sqrt(static_cast<double>(s.head_dim)));
     return g;

@@ -63,12 +63,13 @@ inline int64_t attention_shares(int64_t pairs, int64_t n_kv_heads, int64_t tiles
 // Append: 16-byte pieces per lane of a wavefront's share of a row's K and V heads.
 inline int append_pieces_per_lane(int64_t n_rows, int pieces) { return n_rows * pieces >= 4 * 64 * 2048 ? 4 : 1; }
 
-// Attention over pages: workgroups, as many as are resident at once (two per CU, three at head_dim 64), no more than
-// there can be runs of kAttendMinUnits units of 32 tokens; `pairs` (sequence, kv head, row tile) triples of at most `tokens` tokens.
-constexpr int kAttendMinUnits = 4;
+// Attention over pages: units of 32 tokens that a workgroup's wavefronts take at once, and workgroups: as many as are resident at once
+// (two per CU, three at head_dim 64), no more than there can be such steps; `pairs` (sequence, kv head, row tile) triples of at
+// most `tokens` tokens.
+inline int attend_step(int head_dim) { return head_dim == 256 ? 2 : 4; }
 inline int64_t attend_groups(int64_t pairs, int64_t tokens, int head_dim) {
-    const int64_t units = pairs * ((tokens + 31) / 32), resident = head_dim == 64 ? 768 : 512;
-    return std::max<int64_t>(1, std::min<int64_t>(resident, (units + kAttendMinUnits - 1) / kAttendMinUnits));
+    const int64_t step = attend_step(head_dim), steps = pairs * (((tokens + 31) / 32 + step - 1) / step), resident = head_dim == 64 ? 768 : 512;
+    return std::max<int64_t>(1, std::min<int64_t>(resident, steps));
 }
 
 // Eviction: workgroups that share a pair's moves, `rows` at a time each.
