@@ -530,6 +530,10 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
     }
 }
 
+// Where dimensions d .. d + 3 of a state's row stand in LDS: the rows' quads are exchanged by the row's number, or else the 16 rows that a
+// wavefront writes at once would lie in the same banks (a row is a multiple of them).
+template <int D> __device__ __forceinline__ int o_at(int state_row, int row, int d) { return state_row * D + (d ^ (row * 4)); }
+
 // Grid: g.groups workgroups, each a run of the line.  The wavefronts of a workgroup take the pairs of tiles of a piece of the run (the part
 // that lies in one sequence, kv head and row tile) in turn, each with a state of its own; the four states meet in LDS.
 template <int D, int G, bool HP>
@@ -640,7 +644,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_ker
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int i = 0; i < DL; i += 4)
-                    *reinterpret_cast<f4_t*>(o_lds + (wave * g.tile_rows + l16) * D + DL * (4 * q4 + r) + i) =
+                    *reinterpret_cast<f4_t*>(o_lds + o_at<D>(wave * g.tile_rows + l16, l16, DL * (4 * q4 + r) + i)) =
                         f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
         }
         __syncthreads();
@@ -657,7 +661,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_ker
             for (int k = 0; k < kAttendWaves; ++k) {
                 const float m = ml_lds[k][0][row], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
                 sum += f * ml_lds[k][1][row];
-                o += *reinterpret_cast<const f4_t*>(o_lds + (k * g.tile_rows + row) * D + d) * f;
+                o += *reinterpret_cast<const f4_t*>(o_lds + o_at<D>(k * g.tile_rows + row, row, d)) * f;
             }
             const int64_t slot = slot0 + row;
             if (d == 0) *reinterpret_cast<float2*>(part_ml + slot * 2) = float2{ref, sum};
