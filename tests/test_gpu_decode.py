@@ -155,6 +155,71 @@ def test_attend_logits_keep_the_bits_of_small_products(width, apart, fmt):
         np.testing.assert_allclose(mass[s, :, :n], want[s, :, :n], rtol=2 * np.log(2) * delta + 2.0 ** -20, atol=0)
 
 
+def many(D, n_seqs, N, seed, lens=None):
+    rng = np.random.RandomState(seed)
+    p = Paged((1, 2, 4, D, N, 16, 64), rng.randint(0, N + 1, n_seqs) if lens is None else lens, (16, 16, 16, 8, 0), seed)
+    return p, rows(rng.randint(0, 3, n_seqs))
+
+
+@pytest.mark.parametrize("D,n_seqs,N", [(64, 65, 64), (128, 130, 48), (64, 200, 1024), (256, 70, 512)])
+def test_attend_many_sequences(D, n_seqs, N):
+    """More sequences than a wavefront has lanes, many of them empty or without rows; the last ones of each list get the longest work
+    in front of them.  200 sequences of up to 32 units are more than the workgroups take in whole steps, the others less."""
+    p, (start, n_rows) = many(D, n_seqs, N, 31)
+    check_attend(p, 0, p.halves(n_rows + 1, 4, D), start, 2, None, True)
+
+
+def test_attend_one_long_sequence_among_many_short_ones():
+    p, (start, n_rows) = many(64, 100, 2048, 32, [1] * 99 + [2048])
+    check_attend(p, 0, p.halves(n_rows, 4, 64), start, 2, None, True)
+
+
+def test_attend_rows_above_max_rows_are_left():
+    p = Paged((1, 2, 8, 64, 64, 16, 64), [60, 20], (16,), 33)
+    start, n_rows = rows([5, 1])
+    q = p.halves(n_rows, 8, 64)
+    check_attend(p, 0, q, start, 3, None, True)
+    got, _ = attend(p, 0, q, start, 3)
+    assert np.all(got[3:5] == 7) and not np.any(got[[0, 1, 2, 5]] == 7)
+
+
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+def test_keys_of_later_tokens_do_not_matter(what):
+    """A row's logits behind its own token are left out whatever they are."""
+    p = Paged((1, 1, 2, 128, 64, 16, 128), [40], (16,), 34)
+    start, n_rows = rows([4])
+    q = p.halves(n_rows, 2, 128)
+    want, _ = attend(p, 0, q, start, 4)
+    od.Slab(p.os, p.pool, p.off[0, 2], 16, 0, 0, 0).put(p.os, 39 - 32, np.full(128, what, dtype=np.float16))
+    got, _ = attend(p, 0, q, start, 4)
+    assert np.array_equal(got[:3], want[:3])
+
+
+def test_pages_past_four_gib():
+    """The same sequences in a pool whose records lie behind byte 2^32: every call does the same there."""
+    at = (1 << 32) + 4096
+    p = Paged((2, 2, 4, 128, 96, 16, 64), [96, 50], MIXED, 35)
+    pages, near = p.device()
+    pool = torch.zeros(at + p.pool.size, dtype=torch.uint8, device="cuda")
+    pool[at:] = near
+    far = kvs.Pages(p.ks, pool, pages.off + at, pages.bits, pages.length)
+    k, v, q = (put(p.halves(2, h, 128)) for h in (2, 2, 4))
+    mass, pos = (put(a) for a in p.book(1))
+    results = []
+    for pg in (pages, far):
+        ws = torch.zeros(kvs.kv_attend_workspace_bytes(p.ks, 2, 1, True), dtype=torch.uint8, device="cuda")
+        ws2 = torch.zeros(kvs.kv_evict_workspace_bytes(p.ks, 2, 1, 40), dtype=torch.uint8, device="cuda")
+        m, o = mass.clone(), pos.clone()
+        out = torch.zeros((2, 4, 128), dtype=torch.float16, device="cuda")
+        kvs.kv_append_tokens(pg, 1, k, v, mass=m[0], pos=o[0])
+        kvs.kv_attend_tokens(pg, 1, q, ws, out, mass_in=m[0], mass=m[0])
+        kvs.kv_evict_tokens(pg, 1, 2, m, o, 40, 2, 8, ws2, m, o)
+        results.append((out, m, o))
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert bool(results[0][0].any()) and torch.equal(pool[at:], near) and not bool(pool[:at].any())
+
+
 def test_attend_reads_rows_with_a_stride():
     p = Paged((2, 2, 4, 128, 64, 16, 128), [64, 20], MIXED, 6)
     qkv = torch.from_numpy(p.halves(2, 4 + 2 * 2, 128)).cuda()

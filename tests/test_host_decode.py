@@ -1,6 +1,9 @@
 """CPU tests of decoding on packed records: workspace sizes, refusals (nothing is launched), the rules that divide launches, and
 the oracle against closed forms and against itself."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -104,6 +107,27 @@ def test_workspace_sizes():
     for bad in ((GOOD, 0, 1, 1), (GOOD, 1, 0, 1), (GOOD, 1, 3, 1), (GOOD, 1, 1, 0)):
         with pytest.raises(kvs.KvError):
             kvs.kv_evict_workspace_bytes(*bad)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_launch_rules(tmp_path):
+    root, lib = os.path.dirname(os.path.dirname(os.path.abspath(__file__))), str(tmp_path / "librules.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", "-I",
+                    os.path.join(root, "paper_2403_11805_amd", "csrc"), os.path.join(root, "tests", "decode_rules_driver.cpp"), "-o", lib],
+                   check=True)
+    rules = ctypes.CDLL(lib)
+    for name in ("attend_groups", "evict_blocks", "append_pieces"):
+        getattr(rules, name).restype = ctypes.c_int64
+    rules.attend_groups.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
+    rules.evict_blocks.argtypes = [ctypes.c_int64] * 3
+    rules.append_pieces.argtypes = [ctypes.c_int64, ctypes.c_int]
+    for d, step, most in ((64, 4, 768), (128, 4, 512), (256, 2, 512)):
+        assert rules.attend_groups(1, 1, d) == 1 and rules.attend_groups(3, 32 * step, d) == 3 and rules.attend_groups(3, 32 * step + 1, d) == 6
+        assert rules.attend_groups(1 << 20, 1 << 15, d) == most
+    # never none, never more than the list has work for
+    assert rules.evict_blocks(1, 0, 64) == 1 and rules.evict_blocks(1, 65, 64) == 2 and rules.evict_blocks(1, 1 << 20, 64) == 2048
+    assert rules.evict_blocks(1 << 16, 1 << 20, 64) == 4
+    assert rules.append_pieces(1, 256) == 1 and rules.append_pieces(1 << 20, 256) == 4
 
 
 def test_binding_checks_tensors():
