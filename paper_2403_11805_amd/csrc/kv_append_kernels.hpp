@@ -5,6 +5,9 @@
 
 namespace kvs {
 
+// Bytes bound it: a row is read once and written once, 16 bytes a lane, past the caches.  Six prompts of 300 to 4096 tokens,
+// 32 kv heads of 128 (458 MB): 88 to 91 us in fp16 pages, 5.0 to 5.2 TB/s, 84 in packed ones.  One token for each of 64
+// sequences takes 3.1 us, which is a launch and three dependent loads.
 // Work unit: up to PPL * 64 pieces (8 elements, 16 bytes) of one row's K and V heads, K's first, per wavefront.  The row's
 // sequence, its page and the page's width are wave-uniform, so the width is one branch for the whole wavefront, and the rows'
 // loads are issued before the three dependent list loads that lead to the page.

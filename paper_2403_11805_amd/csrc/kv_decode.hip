@@ -289,7 +289,12 @@ int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_
 #define KV_LAUNCH(KEYS)                                                                                                                 \
     hipLaunchKernelGGL((evict_select_kernel<KEYS>), dim3(static_cast<uint32_t>(pairs)), dim3(kSelectThreads), 0, st, view, g, mass_in, \
                        pos_in, seen, moves, n_moves, mass, pos)
+    // Keys of a lane in registers, as few as the longest sequence may have: 2049 slots take 9.4 us with 4, 16.1 with 32 (every pass is
+    // written out key by key) and 12.7 read again by every pass; 6144 12.4 with 8, 17.6 with 32; 16384 19.5 with 16, 23.5 with 32;
+    // 32768 32 with 32, 79 read again.
     if (shape->n_tokens <= 4 * kSelectThreads) KV_LAUNCH(4);
+    else if (shape->n_tokens <= 8 * kSelectThreads) KV_LAUNCH(8);
+    else if (shape->n_tokens <= 16 * kSelectThreads) KV_LAUNCH(16);
     else if (shape->n_tokens <= 32 * kSelectThreads) KV_LAUNCH(32);
     else KV_LAUNCH(0);
 #undef KV_LAUNCH

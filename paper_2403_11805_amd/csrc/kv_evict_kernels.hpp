@@ -37,9 +37,11 @@ __device__ __forceinline__ int sum_of_first(int x, int count, int lane) {
 // the keep-th token is found digit by digit (11, 11 and 10 bits) from histograms in LDS; of the tokens that have exactly that key the
 // lowest slots are kept, as many as there is room for.  Kept tokens above `keep` and evicted ones below come out in ascending order
 // without a sort: ballots count within 64 slots, and one pass counts for the wavefronts behind.
-// Latency bounds it: a workgroup reads a few hundred KB at most.
+// Instructions bound it, of 16 wavefronts on one CU for a pair: 4 sequences of 2049 slots, 8 kv heads, 4 layers 9.4 us; 2 of 4096, 32 kv
+// heads, 8 layers (512 pairs, two rounds of workgroups) 16.8; 12 pairs of up to 32768 slots 32.  (The histograms' atomics are not what
+// it waits for: 32 copies of the first digit's took as long, and so did fewer vector and more scalar instructions.)
 template <int KEYS>
-__global__ __launch_bounds__(kSelectThreads, KEYS == 32 ? 4 : 8) void evict_select_kernel(PagesView v, EvictGeom g, const float* mass_in, const int32_t* pos_in,
+__global__ __launch_bounds__(kSelectThreads, KEYS >= 16 ? 4 : 8) void evict_select_kernel(PagesView v, EvictGeom g, const float* mass_in, const int32_t* pos_in,
                                                                       const int32_t* __restrict__ seen, int32_t* __restrict__ moves,
                                                                       int32_t* __restrict__ n_moves, float* mass, int32_t* pos) {
     constexpr int kKeys = KEYS ? KEYS : 1;
@@ -291,6 +293,8 @@ __device__ __forceinline__ void piece_store(const PagesView& v, uint8_t* record,
 
 // The moves of a pair's list, `blocks` workgroups per pair: D/8 neighbouring lanes carry kAtOnce rows, their K and their V, with their
 // weight and position.  Rows come from slots at or above `keep` and go to slots below it, so no move reads what another has written.
+// HBM bounds it: 512 pairs of 1170 moves of 512 bytes, 32 kv heads of 128 (613 MB) take 130 us, 4.7 TB/s; rows of one
+// head lie 256 bytes apart, K from V megabytes.  One move per pair takes 4 us: three dependent loads behind a launch.
 // A row's way is list entry - page entry - row - store: the four steps of the kAtOnce rows are taken together.
 constexpr int kAtOnce = 4;
 template <int D>

@@ -335,10 +335,10 @@ def test_evict(geom, lens, widths, keep, sink, recent, fmt, in_place):
 
 
 @pytest.mark.parametrize("N,lens,keep,sink,recent", [(4112, [4112, 4100], 1500, 4, 200), (8192, [8192, 70], 8000, 0, 0),
-                                                     (32784, [32784, 32769], 9000, 16, 1000)])
+                                                     (12304, [12304, 8200], 5000, 0, 100), (32784, [32784, 32769], 9000, 16, 1000)])
 @pytest.mark.parametrize("kind", ["ties", "all equal", "distinct"])
 def test_evict_of_long_sequences(N, lens, keep, sink, recent, kind):
-    """Ranges of slots that take a lane more than 4 and more than 32 keys."""
+    """Ranges of slots that take a lane more than 4, 8 and 32 keys."""
     p = Paged((1, 1, 1, 64, N, 16, 64), lens, (16,), 17)
     mass, pos = p.book(1)
     if kind == "all equal":
