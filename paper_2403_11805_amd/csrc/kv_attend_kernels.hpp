@@ -714,6 +714,7 @@ __device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int
 // Latency bounds it: a launch, the division found again, the shares' sums, the shares: 4 to 5 us (2.4 where no row is divided).  Weights
 // of 24 contexts of up to 8000 tokens (13 MB of logits read, 6 MB of weights read and written) 11 us in all.
 constexpr int kMaxPairRows = 1024;
+constexpr int kEarly = 4;
 template <int D>
 __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendGeom g, int32_t joins, int32_t blocks,
                                                             const int32_t* __restrict__ row_start, const float* __restrict__ part_o,
@@ -760,6 +761,17 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
     const RowShares sh = row_shares(v, g, row_start, lane, s, h, 0);
     const int n = sh.w.n, count = min(sh.w.count, g.max_rows) * g.per;
     if (t0 >= n || count == 0) return;
+    const int t = t0 + static_cast<int>(threadIdx.x) * 4;
+    const int64_t at = pair * v.N + t;
+    const float* x_at = logits + pair * g.rows * v.N + min(t, n - 1) / 4 * 4;
+    // The weights so far and the first rows' logits are on their way while references and sums are worked out (8 contexts of up to 4096
+    // tokens, 32 heads: 6.5 us, 7.4 without).  Past the last row it is read again; N and the logits' rows are multiples of 16.
+    f4_t early[kEarly];
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < kEarly; ++e) early[e] = *reinterpret_cast<const f4_t*>(x_at + static_cast<int64_t>(min(e, count - 1)) * v.N);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = mass_in && t + e < n ? mass_in[at + e] : 0.0f;
     for (int j = wave; j < count; j += 4) {
         const RowShares of = j < 16 ? sh : row_shares(v, g, row_start, lane, s, h, j);
         float ref, sum;
@@ -770,20 +782,21 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
         }
     }
     __syncthreads();
-    const int t = t0 + static_cast<int>(threadIdx.x) * 4;
     if (t >= n) return;
-    f4_t w = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int j = 0; j < count; ++j) {
-        const f4_t x = *reinterpret_cast<const f4_t*>(logits + (pair * g.rows + j) * v.N + t);
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](const f4_t& x, int j) {
         const float ref = refs[j], inv = invs[j];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - ref), inv, w[e]);
-    }
-    const int64_t at = pair * v.N + t;
+        for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - ref), inv, sum[e]);
+    };
+#pragma unroll
+    for (int j = 0; j < kEarly; ++j)
+        if (j < count) add(early[j], j);
+#pragma unroll 4
+    for (int j = kEarly; j < count; ++j) add(*reinterpret_cast<const f4_t*>(x_at + static_cast<int64_t>(j) * v.N), j);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (t + e < n) mass[at + e] = (mass_in ? mass_in[at + e] : 0.0f) + w[e];
+        if (t + e < n) mass[at + e] = w[e] + sum[e];
 }
 
 }  // namespace kvs
