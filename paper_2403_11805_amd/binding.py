@@ -621,7 +621,7 @@ class kv_pages_t(ctypes.Structure):
 class Pages:
     """Paged sequences (kv_pages_t) of one shape: the record pool, the page tables off and bits [n_seqs][stride] and the
     lengths [n_seqs].  Holds the tensors and the two C structures, so that a step marshals them once; what the tensors
-    hold may change from call to call."""
+    hold may change from call to call, but not which tensors they are."""
 
     def __init__(self, shape: Shape, pool: torch.Tensor, off: torch.Tensor, bits: torch.Tensor, length: torch.Tensor):
         if off.dim() != 2 or tuple(bits.shape) != tuple(off.shape) or tuple(length.shape) != (off.shape[0],):
@@ -637,6 +637,12 @@ class Pages:
         self._c = kv_pages_t(_dev(pool), pool.numel() * pool.element_size(), _dev(off, torch.int64), _dev(bits, torch.uint8),
                              _dev(length, torch.int32), off.shape[0], off.shape[1])
         self._refs = ctypes.byref(self._shape), ctypes.byref(self._c)
+        self._fixed = True
+
+    def __setattr__(self, name, value):
+        if "_fixed" in self.__dict__:
+            raise AttributeError(f"{name}: the tensors of Pages are fixed; change what they hold, or make other Pages")
+        object.__setattr__(self, name, value)
 
     def _on_device(self, stream):
         """The stream's address; the pages' device has to be the current one."""

@@ -67,6 +67,7 @@ def test_attend_one_width(D, G, widths, fmt):
     ((3, 2, 4, 64, 1024, 16, 64), [1024, 999, 3], [2, 1, 3], MIXED + (0, 0)),        # long: divided in shares
     ((1, 1, 32, 64, 128, 16, 64), [128, 100], [16, 7], MIXED),                       # 512 query rows
     ((1, 2, 4, 64, 64, 16, 64), [2, 5], [3, 8], (8, 16)),                            # more new rows than tokens
+    ((1, 1, 64, 64, 96, 16, 64), [90], [16], MIXED),                                 # 1024 query rows, the most
 ])
 @pytest.mark.parametrize("with_mass", [False, True])
 def test_attend_rows_and_pages(geom, lens, counts, widths, with_mass):
@@ -419,6 +420,44 @@ def test_decode_steps_captured_and_replayed():
         torch.cuda.synchronize()
         for t, e in zip(state, eager):
             assert torch.equal(t.view(torch.uint8), e.view(torch.uint8))
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured calls over other layers with one workspace, replayed in turn, with other work on the same memory between them."""
+    p = Paged((2, 2, 8, 128, 512, 16, 64), [512, 300], MIXED, 23)
+    pages, _ = p.device()
+    q = put(p.halves(2, 8, 128))
+    ws = torch.empty(kvs.kv_attend_workspace_bytes(p.ks, 2, 1, True), dtype=torch.uint8, device="cuda")
+    out, mass = torch.zeros((2, 2, 8, 128), dtype=torch.float16, device="cuda"), torch.zeros((2, 2, 2, 512), device="cuda")
+
+    def call(layer):
+        kvs.kv_attend_tokens(pages, layer, q, ws, out[layer], mass=mass[layer])
+
+    want = []
+    for layer in range(2):
+        call(layer)
+        want.append((out[layer].clone(), mass[layer].clone()))
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for layer, graph in enumerate(graphs):
+        with torch.cuda.graph(graph):
+            call(layer)
+    for turn in range(4):
+        for layer, graph in enumerate(graphs):
+            ws.fill_(0xff if turn % 2 else 0x3c)
+            out.zero_()
+            mass.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[layer], want[layer][0]) and torch.equal(mass[layer], want[layer][1])
+
+
+def test_the_tensors_of_pages_are_fixed():
+    p = Paged((1, 1, 1, 64, 16, 16, 64), [4], (16,), 24)
+    pages, _ = p.device()
+    for name in ("pool", "off", "bits", "length", "shape", "n_seqs"):
+        with pytest.raises(AttributeError):
+            setattr(pages, name, getattr(pages, name))
+    pages.length.fill_(3)
 
 
 def test_two_streams_at_once():
