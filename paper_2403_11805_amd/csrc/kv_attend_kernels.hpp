@@ -15,8 +15,8 @@
 // scale and minimum enter once per (token, group),
 //     S = sum_g (s_g / 2^-24) acc_g + mn_g qsum_g.
 // An MFMA lines its products up by the exponents without shifting a subnormal's leading zeros out first, and keeps so many bits less of
-// them: K's codes of 4 and 2 bits therefore stand at the mantissa's top (weights of 2-bit pages are off by 8e-7
-// so, by 7e-5 with the codes at its low end); those of 8 bits, which one byte move puts in place, lose 2 bits of 24 (off by 7e-7).
+// them: K's codes therefore stand at the mantissa's top (weights of 2-bit pages are off by 8e-7 so, by 7e-5 with
+// the codes at its low end; of 8-bit pages by 4e-7, and by up to 1.7e-6 at its low end, a shift less per pair).
 // V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s.  P enters as the sum of two
 // halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
 //
@@ -168,11 +168,12 @@ constexpr float kCode = 16777216.0f;       // 2^24: what a code in the low bits 
 
 // Eight dimensions of K from their 8 * W bits, in the order of paired(); codes come out as code / k_code<W>().  (W = 2: the
 // bits of dimensions 0-3 in the upper byte of the low half, those of 4-7 in that of the high one.)
-template <int W> __device__ __forceinline__ constexpr float k_code() { return W == 4 ? kCode / 64 : W == 2 ? kCode / 256 : kCode; }
+template <int W> __device__ __forceinline__ constexpr float k_code() { return kCode / (W == 8 ? 4 : W == 4 ? 64 : W == 2 ? 256 : 1); }
 template <int W> __device__ __forceinline__ u4_t k_operand(const uint32_t* w) {
     if constexpr (W == 16) return paired(w);
     else if constexpr (W == 8)
-        return u4_t{perm(w[1], w[0], 0x0c040c00u), perm(w[1], w[0], 0x0c050c01u), perm(w[1], w[0], 0x0c060c02u), perm(w[1], w[0], 0x0c070c03u)};
+        return u4_t{perm(w[1], w[0], 0x0c040c00u) << 2, perm(w[1], w[0], 0x0c050c01u) << 2, perm(w[1], w[0], 0x0c060c02u) << 2,
+                    perm(w[1], w[0], 0x0c070c03u) << 2};
     else if constexpr (W == 4)
         return u4_t{(w[0] << 6) & 0x03c003c0u, (w[0] << 2) & 0x03c003c0u, (w[0] >> 2) & 0x03c003c0u, (w[0] >> 6) & 0x03c003c0u};
     else return u4_t{w[0] & 0x03000300u, (w[0] >> 2) & 0x03000300u, (w[0] >> 4) & 0x03000300u, (w[0] >> 6) & 0x03000300u};

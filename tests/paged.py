@@ -84,8 +84,7 @@ def rows(counts, n_rows=None, lead=0):
 def attend_bars(paged, q, out, size, spread):
     """How far out may be from its value in 64 bits, by element.  A logit is a sum of D products in binary32 of q and codes, which reach
     a range of their group, twice the largest |k| = K: with the minima every partial sum is below 6 K sum |q| / sqrt(D), and each of the
-    D + 8 roundings is half a step, 2^-24.  (Codes of 8 bits have two leading zeros where they stand, so that each of the D / 32 matrix
-    instructions may chop twice at 2^-23 of 4 ranges: D K 2^-24 in all, within that.)  Weights change by twice a logit's error
+    D + 8 roundings is half a step, 2^-24.  Weights change by twice a logit's error
     relatively, and each is rounded to fp16 at worst, as is V (half a step each, 2^-11); then the result is rounded.  exp2 and the sums
     add 2^-20 with room to spare."""
     s = paged.os

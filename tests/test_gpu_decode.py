@@ -139,8 +139,8 @@ def test_attend_logits_keep_the_bits_of_small_products(width, apart, fmt):
     """q is 0 but for two dimensions that are summed by different matrix instructions and lie 2^apart apart, so that every sum of q * code
     fits 24 bits and is exact in binary32: 1025 * (2^apart + 1) * (2^width - 1) < 2^24.  What is left to round: scale and minimum (2, of
     at most K sum |q|), the factor to base 2 (2), the logit it gives (1), its difference to the reference (2, twice the size): 8 halves of
-    a step, 2^-24, counted as 12.  At width 8 a code has two leading zeros in its half, so each of the two instructions may chop twice at
-    2^-23 of four times a range (twice K): 64 more.  A weight is off by that in its own logit and in the sum's, 2 ln 2 times it
+    a step, 2^-24, counted as 12.  At width 8 the sum takes all 24 bits below a range (twice K), where each of the two instructions may
+    chop twice at 2^-23 of it: 16 more.  A weight is off by that in its own logit and in the sum's, 2 ln 2 times it
     relatively; exp2, the sums over 64 tokens and the division add less than 2^-20."""
     p = Paged((1, 2, 6, 64, 64, 16, 64), [64, 50], (width,), 12, fmt)
     biggest = max(float(np.abs(kv.astype(np.float64)).max()) for kv in p.kv)
@@ -151,7 +151,7 @@ def test_attend_logits_keep_the_bits_of_small_products(width, apart, fmt):
     q[1::2] *= -1
     _, mass = attend(p, 0, q, with_mass=True)
     want = od.attend(p.os, p.pool, *p.table(), 0, q, None, 1, None)[3]
-    delta = (12 + (64 if width == 8 else 0)) * 2.0 ** -24 * biggest * np.abs(q.astype(np.float64)).sum(-1).max() / 8 * np.log2(np.e)
+    delta = (12 + (16 if width == 8 else 0)) * 2.0 ** -24 * biggest * np.abs(q.astype(np.float64)).sum(-1).max() / 8 * np.log2(np.e)
     for s, n in enumerate(p.len):
         np.testing.assert_allclose(mass[s, :, :n], want[s, :, :n], rtol=2 * np.log(2) * delta + 2.0 ** -20, atol=0)
 
