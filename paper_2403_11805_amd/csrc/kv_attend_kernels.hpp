@@ -21,8 +21,8 @@
 // halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
 //
 // What bounds it.  fp16 pages: HBM, 16 contexts of 32768 tokens, 32 query heads on 8 kv heads of 128 (2.15 GB) 370 us, 5.8 TB/s; one of
-// 32768 30 us, 4.5 TB/s.  Packed pages: vector instructions, of which a unit of 32 tokens takes 400 (8 bits) to 476 (2 bits) beside 24
-// MFMAs; 24 contexts of 4096 take 48 us at 8 bits, 36 at 4, 34 at 2, 75 in fp16.  Short contexts: the chain of loads from the
+// 32768 30 us, 4.5 TB/s.  Packed pages: vector instructions, of which a unit of 32 tokens takes 431 (8 bits) to 476 (2 bits) beside 24
+// MFMAs; 24 contexts of 4096 take 47 us at 8 bits, 37 at 4, 34 at 2, 75 in fp16.  Short contexts: the chain of loads from the
 // lengths to the keys and of the arithmetic behind them, 5 to 10 us for one context of up to 1000 tokens (head_dim 64 to 256).
 #pragma once
 
