@@ -17,7 +17,8 @@
 // An MFMA lines its products up by the exponents without shifting a subnormal's leading zeros out first, and keeps so many bits less of
 // them: K's codes therefore stand at the mantissa's top (weights of 2-bit pages are off by 8e-7 so, by 7e-5 with
 // the codes at its low end; of 8-bit pages by 4e-7, and by up to 1.7e-6 at its low end, a shift less per pair).
-// V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s.  P enters as the sum of two
+// V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s: the value that a Load gives, off by
+// 2^-11 of itself at most, as the result is when it is rounded; more bits would take a second MFMA and twice the registers.  P enters as the sum of two
 // halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
 //
 // What bounds it.  fp16 pages: HBM, 16 contexts of 32768 tokens, 32 query heads on 8 kv heads of 128 (2.15 GB) 370 us, 5.8 TB/s; one of
