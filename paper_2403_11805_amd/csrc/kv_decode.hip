@@ -22,6 +22,9 @@ int launch_status(const char* what) {
     return e == hipSuccess ? KV_OK : hip_fail(e, what);
 }
 
+// Workgroups that one launch may have: a grid has less than 2^32 threads.
+constexpr int64_t most_groups(int threads) { return 0xffffffffLL / threads; }
+
 int check_paged_shape(const kv_shape_t* shape) {
     if (int rc = check_shape(shape)) return rc;
     if (!is_f16(*shape)) return fail(KV_ESHAPE, "paged sequences need an fp16 cache format");
@@ -128,13 +131,15 @@ AttendSpace attend_space(const kv_shape_t& s, int32_t n_seqs, const AttendGeom& 
     return w;
 }
 
-// The rows of a step and the work they make: units of 32 tokens of every (sequence, kv head, row tile) are counted in 31 bits.
+// The rows of a step and the work they make: units of 32 tokens of every (sequence, kv head, row tile) are counted in 31 bits, and
+// every row and every 1024 weights of a (sequence, kv head) has a workgroup of the second launch.
 int check_attend(const kv_shape_t* shape, int32_t n_seqs, int32_t max_rows) {
     if (max_rows < 1 || max_rows > 16) return fail(KV_EINVAL, "max_rows %d outside [1,16]", max_rows);
     const int64_t rows = static_cast<int64_t>(shape->n_q_heads / shape->n_kv_heads) * max_rows;
     if (rows > kMaxPairRows) return fail(KV_ESHAPE, "more than %d query rows per kv head", kMaxPairRows);
     const int64_t pairs = static_cast<int64_t>(n_seqs) * shape->n_kv_heads;
-    if (pairs * ((rows + 15) / 16) > 0x7fffffffLL / ((shape->n_tokens + 2047) / 32) || pairs * rows > 0x3fffffffLL)
+    if (pairs * ((rows + 15) / 16) > 0x7fffffffLL / ((shape->n_tokens + 2047) / 32) ||
+        pairs * (rows + (shape->n_tokens + 1023) / 1024) > most_groups(256))
         return fail(KV_ESHAPE, "n_seqs * n_kv_heads * n_tokens too large for one call");
     return KV_OK;
 }
@@ -162,7 +167,7 @@ int32_t kv_append_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     const int ppl = append_pieces_per_lane(n_rows, pieces);
     const int32_t tasks_per_row = (pieces + 64 * ppl - 1) / (64 * ppl);
     const int64_t tasks = static_cast<int64_t>(n_rows) * tasks_per_row, groups = (tasks + 3) / 4;
-    if (groups > 0x7fffffffLL) return fail(KV_ESHAPE, "append grid exceeds 2^31 workgroups");
+    if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows * n_kv_heads * head_dim too large for one call");
     const PagesView view = pages_view(*shape, *pages);
     const int lpg = log2_of(shape->group / 8);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -281,7 +286,8 @@ int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_
                     static_cast<unsigned long long>(need));
     const int32_t rows_per_group = 256 / (shape->head_dim / 8);
     const int32_t blocks = static_cast<int32_t>(evict_blocks(pairs, g.list, rows_per_group * kAtOnce));
-    if (pairs * std::max(blocks, 1) > 0x7fffffffLL) return fail(KV_ESHAPE, "eviction grid exceeds 2^31 workgroups");
+    if (pairs > most_groups(kSelectThreads) || pairs * blocks > most_groups(256))
+        return fail(KV_ESHAPE, "layers * n_seqs * n_kv_heads too large for one call");
     const PagesView view = pages_view(*shape, *pages);
     int32_t* n_moves = static_cast<int32_t*>(workspace);
     int32_t* moves = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + ((static_cast<uint64_t>(pairs) * 4 + 255) & ~255ull));

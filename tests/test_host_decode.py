@@ -97,6 +97,19 @@ def test_evict_refusals():
     assert binding.lib().kv_evict_tokens(*evict_args(begin=1, end=1, mass=None, ws=None)) == 0
 
 
+def test_grids_that_no_launch_can_have_are_refused():
+    """A launch has less than 2^32 threads: 16777215 workgroups of 256, 4194303 of 1024."""
+    tiny = GOOD._replace(n_tokens=16, n_kv_heads=1, n_q_heads=1, head_dim=64)
+    most = pages(n_seqs=65535)
+    refused(binding.KV_ESHAPE, "kv_append_tokens", *append_args(shape=tiny, n_rows=1 << 28, start=P))
+    wide = tiny._replace(n_kv_heads=32, n_q_heads=256)
+    refused(binding.KV_ESHAPE, "kv_attend_tokens", *attend_args(shape=wide, pg=most, stride=256 * 64, n_rows=65535))
+    with pytest.raises(kvs.KvError):
+        kvs.kv_attend_workspace_bytes(wide, 65535)
+    deep = tiny._replace(n_layers=65, n_kv_heads=1)
+    refused(binding.KV_ESHAPE, "kv_evict_tokens", *evict_args(shape=deep, pg=most, end=65, keep=4, sink=0, recent=0))
+
+
 def test_workspace_sizes():
     assert kvs.kv_attend_workspace_bytes(GOOD, 1, 1) > 0
     # the logits of every row, for the weights
