@@ -119,8 +119,8 @@ struct Line {
         }
         const bool fits1 = t1 <= g.groups * g.step, fits2 = t2 <= g.groups * 2 * g.step;
         round = fits1 ? g.step : fits2 ? 2 * g.step : 1;
-        cost = fits1 | fits2 ? 0 : kPieceCost;
-        run = fits1 | fits2 ? round : (tl + g.groups - 1) / g.groups;
+        cost = (fits1 | fits2) ? 0 : kPieceCost;
+        run = (fits1 | fits2) ? round : (tl + g.groups - 1) / g.groups;
         end = fits1 ? one : fits2 ? two : long_;
     }
     __device__ __forceinline__ void next(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
@@ -137,23 +137,32 @@ __device__ __forceinline__ int64_t pair_number(const PagesView& v, const AttendG
     return static_cast<int64_t>(s) * v.Hkv * g.row_tiles + pair;
 }
 
+// What attend_kernel leaves of the line for the launch behind it, so that that one need not go through all sequences again: the places of a
+// pair and of a run, then where each sequence ends (only of those that have places).
+struct LineNote {
+    int round, cost, run, unused;
+};
+__device__ __forceinline__ void leave_line(int32_t* __restrict__ note, const PagesView& v, const Line& line, int lane) {
+    if (line.s0 + lane < v.n_seqs) note[4 + line.s0 + lane] = line.end;
+}
+
 // The shares of row j of (sequence s, kv head h): `used` slots from `first` on.
 struct RowShares {
     SeqWork w;
     int used;
     int64_t first;
 };
-__device__ __forceinline__ RowShares row_shares(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane, int s,
-                                                int h, int j) {
-    Line line;
-    line.start(v, g, row_start, lane);
-    while (s >= line.s0 + 64) line.next(v, g, row_start, lane);
-    const int l = s - line.s0;
+__device__ __forceinline__ RowShares row_shares(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start,
+                                                const int32_t* __restrict__ note, int s, int h, int j) {
     RowShares x;
-    x.w = of_lane(line.mine, l);
+    x.w = work_of(v, g, row_start, s);
+    x.used = 0;
+    x.first = 0;
+    if (x.w.units == 0 || x.w.pairs == 0) return x;
+    const LineNote l = *reinterpret_cast<const LineNote*>(note);
     const int row_tiles = x.w.pairs / v.Hkv, pair = h * row_tiles + j / 16;
-    const int begin = __builtin_amdgcn_readlane(line.end, l) - line.each(x.w) * (x.w.pairs - pair) + line.cost, wg = begin / line.run;
-    x.used = x.w.units ? (begin + x.w.units - 1) / line.run - wg + 1 : 0;
+    const int begin = note[4 + s] - Line::places(x.w.units, l.round, l.cost) * (x.w.pairs - pair) + l.cost, wg = begin / l.run;
+    x.used = (begin + x.w.units - 1) / l.run - wg + 1;
     x.first = wg + pair_number(v, g, s, pair);
     return x;
 }
@@ -549,7 +558,7 @@ template <int D, int G, bool HP>
 __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
-                                                                   float* __restrict__ logits) {
+                                                                   float* __restrict__ logits, int32_t* __restrict__ note) {
     constexpr int DL = D / 16, NG = D / G, NT = D == 256 ? 1 : 2;      // (256: the registers of two tiles do not fit)
     extern __shared__ float o_lds[];                 // [kAttendWaves][tile_rows][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
@@ -558,13 +567,20 @@ __global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_ker
     Line line;
     line.start(v, g, row_start, lane);
     int at = static_cast<int>(blockIdx.x) * line.run;
-    const int run_end = at + line.run;
+    const int run_begin = at, run_end = at + line.run;
+    if (blockIdx.x == 0 && wave == 0) {
+        if (lane == 0) *reinterpret_cast<LineNote*>(note) = LineNote{line.round, line.cost, line.run, 0};
+        leave_line(note, v, line, lane);
+    }
     while (at < run_end) {
         // the piece that begins at `at`: its sequence, pair and units
         uint64_t behind = __ballot(line.end > at);
         while (!behind && line.s0 + 64 < v.n_seqs) {
+            const int before = __builtin_amdgcn_readlane(line.end, 63);
             line.next(v, g, row_start, lane);
             behind = __ballot(line.end > at);
+            // 64 sequences are noted by the workgroup whose run they begin in (where they have no places, by one or none)
+            if (wave == 0 && before >= run_begin && before < run_end) leave_line(note, v, line, lane);
         }
         if (!behind) return;                         // (the end of the line; uniform in the workgroup)
         const int l = __builtin_ctzll(behind), s = line.s0 + l;
@@ -713,15 +729,17 @@ __device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int
 // every (1024 / D)-th share.  The others, `blocks` of them per (sequence, kv head), make the weights of 1024 keys each from the logits
 // that the rows have left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
 // `weight` holds as many floats as the attention has workgroups.
-// Latency bounds it: a launch, the division found again, the shares' sums, the shares: 4 to 5 us (2.4 where no row is divided).  Weights
-// of 24 contexts of up to 8000 tokens (13 MB of logits read, 6 MB of weights read and written) 11 us in all.
+// Latency bounds it: a launch, the row's place in the line, the shares' sums, the shares: 4 to 5 us (2.4 where no row is divided).  Weights
+// of 24 contexts of up to 8000 tokens (13 MB of logits read, 6 MB of weights read and written) 10 us in all.  1024 contexts, 32
+// query heads: 44 us, 234 when every workgroup went through all sequences again for its place; 4096 contexts 163 and 3307.
 constexpr int kMaxPairRows = 1024;
 constexpr int kEarly = 4;
 template <int D>
 __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendGeom g, int32_t joins, int32_t blocks,
                                                             const int32_t* __restrict__ row_start, const float* __restrict__ part_o,
                                                             const float* __restrict__ part_ml, const float* __restrict__ logits,
-                                                            const float* mass_in, float* mass, _Float16* __restrict__ out) {
+                                                            const float* mass_in, float* mass, _Float16* __restrict__ out,
+                                                            const int32_t* __restrict__ note) {
     constexpr int kQuads = D / 4, kParts = 256 / kQuads;
     extern __shared__ float weight[];
     __shared__ float total;
@@ -731,7 +749,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
     const int id = static_cast<int>(blockIdx.x);
     if (id < joins) {
         const int pair = id / g.rows, j = id - pair * g.rows, s = pair / v.Hkv, h = pair - s * v.Hkv;
-        const RowShares sh = row_shares(v, g, row_start, lane, s, h, j);
+        const RowShares sh = row_shares(v, g, row_start, note, s, h, j);
         if (sh.used == 1 || j >= min(sh.w.count, g.max_rows) * g.per) return;
         const int64_t first = sh.first * g.tile_rows + j % 16;
         const int quad = threadIdx.x % kQuads, part = threadIdx.x / kQuads;
@@ -760,7 +778,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
     }
     const int64_t pair = (id - joins) / blocks;
     const int s = static_cast<int>(pair / v.Hkv), h = static_cast<int>(pair % v.Hkv), t0 = (id - joins) % blocks * 1024;
-    const RowShares sh = row_shares(v, g, row_start, lane, s, h, 0);
+    const RowShares sh = row_shares(v, g, row_start, note, s, h, 0);
     const int n = sh.w.n, count = min(sh.w.count, g.max_rows) * g.per;
     if (t0 >= n || count == 0) return;
     const int t = t0 + static_cast<int>(threadIdx.x) * 4;
@@ -775,7 +793,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = mass_in && t + e < n ? mass_in[at + e] : 0.0f;
     for (int j = wave; j < count; j += 4) {
-        const RowShares of = j < 16 ? sh : row_shares(v, g, row_start, lane, s, h, j);
+        const RowShares of = j < 16 ? sh : row_shares(v, g, row_start, note, s, h, j);
         float ref, sum;
         row_total(part_ml, of.first * g.tile_rows + j % 16, g.tile_rows, of.used, lane, nullptr, ref, sum);
         if (lane == 0) {

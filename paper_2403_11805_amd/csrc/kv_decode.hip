@@ -118,7 +118,7 @@ AttendGeom attend_geom(const kv_shape_t& s, int32_t n_seqs, int32_t max_rows) {
 }
 
 struct AttendSpace {
-    uint64_t part_o, part_ml, logits, all;      // byte offsets and the size of the workspace
+    uint64_t part_o, part_ml, note, logits, all;      // byte offsets and the size of the workspace
 };
 AttendSpace attend_space(const kv_shape_t& s, int32_t n_seqs, const AttendGeom& g, bool with_mass) {
     auto up = [](uint64_t x) { return (x + 255) & ~255ull; };
@@ -126,7 +126,8 @@ AttendSpace attend_space(const kv_shape_t& s, int32_t n_seqs, const AttendGeom& 
     AttendSpace w;
     w.part_o = 0;
     w.part_ml = w.part_o + up(rows * s.head_dim * 4);
-    w.logits = w.part_ml + up(rows * 8);
+    w.note = w.part_ml + up(rows * 8);
+    w.logits = w.note + up((4 + static_cast<uint64_t>(n_seqs)) * 4);
     w.all = w.logits + (with_mass ? up(static_cast<uint64_t>(n_seqs) * s.n_kv_heads * g.rows * s.n_tokens * 4) : 0);
     return w;
 }
@@ -217,6 +218,7 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     uint8_t* space = static_cast<uint8_t*>(workspace);
     float* part_o = reinterpret_cast<float*>(space + w.part_o);
     float* part_ml = reinterpret_cast<float*>(space + w.part_ml);
+    int32_t* note = reinterpret_cast<int32_t*>(space + w.note);
     float* logits = mass ? reinterpret_cast<float*>(space + w.logits) : nullptr;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const _Float16* q16 = static_cast<const _Float16*>(q);
@@ -226,9 +228,9 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
 #define KV_LAUNCH(D, G)                                                                                                                       \
     do {                                                                                                                                      \
         if (view.half_params)                                                                                                                 \
-            hipLaunchKernelGGL((attend_kernel<D, G, true>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits);     \
+            hipLaunchKernelGGL((attend_kernel<D, G, true>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits, note); \
         else                                                                                                                                  \
-            hipLaunchKernelGGL((attend_kernel<D, G, false>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits);    \
+            hipLaunchKernelGGL((attend_kernel<D, G, false>), grid, block, lds, st, view, g, q16, row_start, o16, part_o, part_ml, logits, note); \
     } while (0)
     switch (shape->head_dim * 1024 + shape->group) {
         case 64 * 1024 + 64: KV_LAUNCH(64, 64); break;
@@ -245,7 +247,7 @@ int32_t kv_attend_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32
     const uint32_t weights = static_cast<uint32_t>(g.groups) * 4;
 #define KV_LAUNCH(D)                                                                                                                  \
     hipLaunchKernelGGL((attend_finish_kernel<D>), finish, dim3(256), weights, st, view, g, joins, blocks, row_start, part_o, part_ml, \
-                       logits, mass_in, mass, o16)
+                       logits, mass_in, mass, o16, note)
     KV_BY_HEAD_DIM(shape->head_dim, KV_LAUNCH);
 #undef KV_LAUNCH
     return launch_status("attend_finish_kernel launch");
