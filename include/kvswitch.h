@@ -608,8 +608,8 @@ uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int3
  * per query head, query head h reading kv head h / (n_q_heads / n_kv_heads).  K counts with the values code * scale + mn
  * its codes stand for, V with these rounded to fp16; logits, softmax and sums are fp32, probabilities enter the product
  * with V as the sum of two fp16 numbers.  A row that sees no token gives zeros.  What lies behind a sequence's end may be
- * anything, and so may K of tokens that a row does not see; V of the tokens below len[s] has to be finite, or else the rows
- * of that sequence that do not see such a token may be NaN as well as those that do.
+ * anything, and so may K and V of tokens that a row does not see; a row that sees V that is not finite is NaN, in that
+ * dimension at least.
  *   q        dev fp16 [n_rows][n_q_heads][head_dim], q_stride elements from row to row (>= n_q_heads * head_dim, a
  *            multiple of 8);
  *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others'

@@ -373,6 +373,21 @@ __device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t, int va
     return x;
 }
 
+// Whether the lane's piece of V of its token r holds a value that is not finite.
+template <int D, int G, int W, bool HP> __device__ __forceinline__ bool not_finite(const VRegs<D, G, W, HP>& t, int r) {
+    if constexpr (W != 16) {
+        const float s = t.param(t.s, r), m = t.param(t.m, r);
+        return !(fabsf(s) + fabsf(m) < INFINITY);
+    } else {
+        typedef uint16_t us2_t __attribute__((ext_vector_type(2)));
+        us2_t most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < VRegs<D, G, W, HP>::kWords; ++i)
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(us2_t, t.v[r][i] & 0x7fff7fffu));
+        return __builtin_elementwise_max(most[0], most[1]) >= 0x7c00;
+    }
+}
+
 // V^T of one dimension for tokens (4q + 2j, 4q + 2j + 1) of a tile, as a pair of halves.
 template <int D, int G, int W, bool HP, int i>
 __device__ __forceinline__ uint32_t v_pair(const VRegs<D, G, W, HP>& t, const VScale<W>& x, int j) {
@@ -539,6 +554,33 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
 #pragma unroll
             for (int k = 0; k < NT; ++k) x[k] = v_scale<D, G, W, HP>(vr[k], tile[k].valid, lane);
         }
+        // 0 * V of a token that a row does not see is 0 only if V is finite: in tiles that not every row sees whole, V that is not counts as
+        // 0 for all rows, and makes those that do see its token NaN.  (What this takes in registers does not fit three wavefronts per SIMD at
+        // head_dim 64, which were 5 to 10 % faster there in packed pages.)
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
+                uint64_t lanes[4], any = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) any |= lanes[r] = __ballot((tile[k].first + 4 * q4 + r > rw.all_see) & not_finite<D, G, W, HP>(vr[k], r));
+                if (any) {                                               // (uniform)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const bool bad = (lanes[r] >> (16 * q4) & 0xffffull) != 0;         // in any of the token's lanes
+                        if constexpr (W == 16) {
+#pragma unroll
+                            for (int i = 0; i < VRegs<D, G, W, HP>::kWords; ++i) vr[k].v[r][i] = bad ? 0u : vr[k].v[r][i];
+                        } else {
+                            x[k].s[r] = bad ? 0.0f : x[k].s[r];
+                            x[k].odd[r] = bad ? 0.0f : x[k].odd[r];
+                            x[k].m[r] = bad ? 0.0f : x[k].m[r];
+                        }
+                        const bool poisoned = bad & (tile[k].first + 4 * q4 + r <= rw.last);
+                        hi[4 * k + r] = poisoned ? static_cast<_Float16>(NAN) : hi[4 * k + r];
+                    }
+                }
+            }
+        }
         unit_values<D, G, W, HP, NT>(vr, x, hi, lo, st);
         if (more) {
             at.here();
@@ -555,7 +597,7 @@ template <int D> __device__ __forceinline__ int o_at(int state_row, int row, int
 // Grid: g.groups workgroups, each a run of the line.  The wavefronts of a workgroup take the pairs of tiles of a piece of the run (the part
 // that lies in one sequence, kv head and row tile) in turn, each with a state of its own; the four states meet in LDS.
 template <int D, int G, bool HP>
-__global__ __launch_bounds__(64 * kAttendWaves, D == 64 ? 3 : 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
+__global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView v, AttendGeom g, const _Float16* __restrict__ q,
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                    float* __restrict__ logits, int32_t* __restrict__ note) {

@@ -66,14 +66,13 @@ inline int64_t attention_shares(int64_t pairs, int64_t n_kv_heads, int64_t tiles
 inline int append_pieces_per_lane(int64_t n_rows, int pieces) { return n_rows * pieces >= 4 * 64 * 2048 ? 4 : 1; }
 
 // Attention over pages: units of 32 tokens that a workgroup's wavefronts take at once, and workgroups: as many as are resident at once
-// (two per CU, three at head_dim 64), no more than there can be such steps; `pairs` (sequence, kv head, row tile) triples of at
+// (two per CU), no more than there can be such steps; `pairs` (sequence, kv head, row tile) triples of at
 // most `tokens` tokens.
 // 24 ragged packed contexts of up to 8000 tokens, 8 kv heads of 128: 49 us with 512 workgroups, 61 with 256, 60 with 768, whose third
-// of a CU's work waits for a place; 8 contexts of 32 kv heads 43, 50 and 50; 16 contexts of 32768 in fp16 371, 367 and 408.  At
-// head_dim 64, 16 contexts with drafts: 10.7 us with 768, 11.0 with 512.
+// of a CU's work waits for a place; 8 contexts of 32 kv heads 43, 50 and 50; 16 contexts of 32768 in fp16 371, 367 and 408.
 inline int attend_step(int head_dim) { return head_dim == 256 ? 2 : 4; }
 inline int64_t attend_groups(int64_t pairs, int64_t tokens, int head_dim) {
-    const int64_t step = attend_step(head_dim), steps = pairs * (((tokens + 31) / 32 + step - 1) / step), resident = head_dim == 64 ? 768 : 512;
+    const int64_t step = attend_step(head_dim), steps = pairs * (((tokens + 31) / 32 + step - 1) / step), resident = 512;
     return std::max<int64_t>(1, std::min<int64_t>(resident, steps));
 }
 

@@ -196,6 +196,27 @@ def test_keys_of_later_tokens_do_not_matter(what):
     assert np.array_equal(got[:3], want[:3])
 
 
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 64), (128, 128), (256, 64), (256, 256)])
+@pytest.mark.parametrize("width", MIXED)
+@pytest.mark.parametrize("fmt", [0, 3])
+@pytest.mark.parametrize("n,what", [(40, np.nan), (48, np.inf), (33, -np.inf)])
+def test_values_of_later_tokens_do_not_matter(D, G, width, fmt, n, what):
+    """V of the two newest tokens is not finite in a few dimensions: the rows in front of them and all weights stay as they were, the others are NaN."""
+    p = Paged((1, 2, 4, D, 64, 16, G), [n, 20], (width,), 36, fmt)
+    start, n_rows = rows([4, 1])
+    q = p.halves(n_rows, 4, D)
+    want, weights = attend(p, 0, q, start, 4, None, True)
+    for token in (n - 2, n - 1):
+        x = od.Slab(p.os, p.pool, p.off[0, token // 16], width, 0, 1, 1)
+        if width == 16:
+            x.codes[token % 16].view(np.float16)[[3, D - 1]] = what
+        else:
+            x.scale[token % 16, 0] = what
+    got, mass = attend(p, 0, q, start, 4, None, True)
+    assert np.array_equal(got[[0, 1, 4]], want[[0, 1, 4]]) and np.array_equal(mass, weights)
+    assert np.array_equal(got[2:4, :2], want[2:4, :2]) and np.isnan(got[2:4, 2:]).all()
+
+
 def test_pages_past_four_gib():
     """The same sequences in a pool whose records lie behind byte 2^32: every call does the same there."""
     at = (1 << 32) + 4096

@@ -134,7 +134,7 @@ def test_launch_rules(tmp_path):
     rules.attend_groups.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
     rules.evict_blocks.argtypes = [ctypes.c_int64] * 3
     rules.append_pieces.argtypes = [ctypes.c_int64, ctypes.c_int]
-    for d, step, most in ((64, 4, 768), (128, 4, 512), (256, 2, 512)):
+    for d, step, most in ((64, 4, 512), (128, 4, 512), (256, 2, 512)):
         assert rules.attend_groups(1, 1, d) == 1 and rules.attend_groups(3, 32 * step, d) == 3 and rules.attend_groups(3, 32 * step + 1, d) == 6
         assert rules.attend_groups(1 << 20, 1 << 15, d) == most
     # never none, never more than the list has work for
