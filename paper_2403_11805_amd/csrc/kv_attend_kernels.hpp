@@ -40,7 +40,7 @@ constexpr int kAttendWaves = 4;
 constexpr float kTop = 7.0f;         // a row's reference is set 2^7 below its largest logit so far ...
 constexpr float kSlack = 15.0f;      // ... and moves when a logit passes 2^15 above it: probabilities stay in fp16's range, and those
                                      // 2^-31 below the largest still count
-constexpr int kNowhere = 0x7fffff00;     // first token of a tile that no row sees
+constexpr int kNowhere = -1;         // first token of a tile that is not there
 
 struct AttendGeom {
     int32_t layer, n_rows, max_rows;
@@ -275,7 +275,7 @@ template <int D, int G, int W, bool HP> struct LaneAt {
     __device__ __forceinline__ void here() { asm volatile("" : "+v"(k), "+v"(v), "+v"(p), "+v"(vp)); }
 };
 
-// Issues the loads of a tile.
+// Issues the loads of a tile.  (WHOLE: all of its 16 tokens are there.)
 template <int D, int G, int W, bool HP>
 __device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, const LaneAt<D, G, W, HP>& at) {
     using A = LaneAt<D, G, W, HP>;
@@ -288,11 +288,11 @@ __device__ __forceinline__ void load_k(KRegs<D, G, W, HP>& t, const Tile& tile, 
 }
 // (What lies behind a sequence's tokens may be anything: V rows of missing tokens are replaced by the last one there is, and their
 // parameters are not used.)
-template <int D, int G, int W, bool HP>
+template <bool WHOLE, int D, int G, int W, bool HP>
 __device__ __forceinline__ void load_v(VRegs<D, G, W, HP>& t, const Tile& tile, const SlabSteps& step, const LaneAt<D, G, W, HP>& at, int lane) {
     using A = LaneAt<D, G, W, HP>;
     const uint8_t* vb = tile.codes + step.v_codes;
-    if (tile.valid == 16) {                                             // (uniform)
+    if constexpr (WHOLE) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) load_words<A::kMine>(vb + at.v + r * A::kRowBytes, t.v[r]);
     } else {
@@ -349,43 +349,15 @@ __device__ __forceinline__ f4_t tile_logits(const KRegs<D, G, W, HP>& t, const u
 template <int W> struct VScale {
     float s[4], odd[4], m[4];
 };
-template <int D, int G, int W, bool HP>
-__device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t, int valid, int lane) {
-    const int q4 = lane >> 4;
+template <int D, int G, int W, bool HP> __device__ __forceinline__ VScale<W> v_scale(const VRegs<D, G, W, HP>& t) {
     VScale<W> x;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        x.s[r] = t.param(t.s, r);
+        x.s[r] = __builtin_fmaf(t.param(t.s, r), kCode, 0.0f);
         x.m[r] = t.param(t.m, r);
-    }
-    if (valid < 16) {                                                   // (uniform) missing tokens: 0
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            x.s[r] = 4 * q4 + r < valid ? x.s[r] : 0.0f;
-            x.m[r] = 4 * q4 + r < valid ? x.m[r] : 0.0f;
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        x.s[r] = __builtin_fmaf(x.s[r], kCode, 0.0f);
         x.odd[r] = x.s[r] * (W == 4 ? 1.0f / 16 : 1.0f / 4);            // (unused at width 8)
     }
     return x;
-}
-
-// Whether the lane's piece of V of its token r holds a value that is not finite.
-template <int D, int G, int W, bool HP> __device__ __forceinline__ bool not_finite(const VRegs<D, G, W, HP>& t, int r) {
-    if constexpr (W != 16) {
-        const float s = t.param(t.s, r), m = t.param(t.m, r);
-        return !(fabsf(s) + fabsf(m) < INFINITY);
-    } else {
-        typedef uint16_t us2_t __attribute__((ext_vector_type(2)));
-        us2_t most = {0, 0};
-#pragma unroll
-        for (int i = 0; i < VRegs<D, G, W, HP>::kWords; ++i)
-            most = __builtin_elementwise_max(most, __builtin_bit_cast(us2_t, t.v[r][i] & 0x7fff7fffu));
-        return __builtin_elementwise_max(most[0], most[1]) >= 0x7c00;
-    }
 }
 
 // V^T of one dimension for tokens (4q + 2j, 4q + 2j + 1) of a tile, as a pair of halves.
@@ -449,8 +421,7 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
     return static_cast<uint64_t>(hi) << 32 | lo;
 }
 
-// The next NT of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time behind every row's last
-// token.
+// The next NT of the batch's `tiles` (a bit each); a last one without a partner comes twice, the second time nowhere.
 template <int NT> __device__ __forceinline__ void next_tiles(uint64_t& tiles, const TileBatch& tb, int n, uint8_t* pool, Tile* tile) {
     int at = __builtin_ctzll(tiles);
 #pragma unroll
@@ -476,8 +447,53 @@ template <int NT> __device__ __forceinline__ uint64_t own_tiles(bool of_width, i
     return all & __ballot(turn == wave);
 }
 
-// A wavefront's tiles of width W, NT at a time.  K of the next unit is loaded once K of this one has been used, and V likewise: the
-// loads are in flight during the other half of the arithmetic, without a second set of registers.
+// What a walk over tiles of one width needs beside them.
+template <int D, int G, int W, bool HP> struct WidthWalk {
+    SlabSteps step;
+    float qsum[D / G], scale;                  // scale: of what tile_logits gives: logits in units of log2
+    __device__ __forceinline__ WidthWalk(const PagesView& v, const RowsOfWave<D, G>& rw) {
+        const uint64_t rows = static_cast<uint64_t>(v.T) * static_cast<uint32_t>(v.Hkv), params = static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
+        step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
+#pragma unroll
+        for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / k_code<W>());
+        scale = W == 16 ? rw.scale : rw.scale * k_code<W>();
+    }
+};
+
+// The probabilities of a unit's logits s (in units of 1 / scale) against the rows' references, which move if they have to; the
+// sums take them in.
+template <int D, int NT>
+__device__ __forceinline__ void probabilities(const f4_t* s, float scale, RowState<D>& st, typename Halves<NT>::type& hi, typename Halves<NT>::type& lo) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < NT; ++k) top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
+    top *= scale;
+    if (__ballot(top > st.ref + kSlack)) {                               // (uniform)
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const bool moves = top > st.ref + kSlack;
+        const float to = moves ? top - kTop : st.ref, f = moves ? __builtin_amdgcn_exp2f(st.ref - to) : 1.0f;
+        st.ref = to;
+        st.sum *= f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
+    }
+    const float ref = st.ref == -INFINITY ? 0.0f : st.ref;               // (a row that has seen nothing: every logit is -inf)
+    // P = hi + lo: hi has the leading 11 bits of e, so that both conversions are exact (but for what lies below 2^-24)
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], scale, -ref));
+            const float lead = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e) & 0xffffe000u);
+            st.sum += e;
+            hi[4 * k + r] = static_cast<_Float16>(lead);
+            lo[4 * k + r] = static_cast<_Float16>(e - lead);
+        }
+}
+
+// A wavefront's tiles of width W that every row sees whole, NT at a time.  K of the next unit is loaded once K of this one has been used,
+// and V likewise: the loads are in flight during the other half of the arithmetic, without a second set of registers.
 template <int D, int G, int W, bool HP, int NT>
 __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, const RowsOfWave<D, G>& rw,
                                      RowState<D>& st, int lane) {
@@ -485,109 +501,123 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
     // What depends on the lane is worked out here, width by width: the compiler would keep it in registers for all four.
     asm volatile("" : "+v"(lane));
     const int q4 = lane >> 4;
-    const uint64_t rows = static_cast<uint64_t>(v.T) * static_cast<uint32_t>(v.Hkv), params = static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
-    const SlabSteps step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
-    float qsum[D / G];
-#pragma unroll
-    for (int i = 0; i < D / G; ++i) qsum[i] = rw.qsum[i] * (1.0f / k_code<W>());
-    const float scale = W == 16 ? rw.scale : rw.scale * k_code<W>();     // of what tile_logits gives: logits in units of log2
+    const WidthWalk<D, G, W, HP> ww(v, rw);
     KRegs<D, G, W, HP> kr[NT];
     VRegs<D, G, W, HP> vr[NT];
     Tile tile[NT], next[NT];
     LaneAt<D, G, W, HP> at(lane);
     next_tiles<NT>(tiles, tb, n, v.pool, next);
 #pragma unroll
-    for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, at);
+    for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], ww.step, at);
 #pragma unroll
-    for (int k = 0; k < NT; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, at, lane);
+    for (int k = 0; k < NT; ++k) load_v<true, D, G, W, HP>(vr[k], next[k], ww.step, at, lane);
     bool more = true;
     while (more) {
         f4_t s[NT];
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
             tile[k] = next[k];
-            s[k] = tile_logits<D, G, W, HP>(kr[k], rw.q, qsum);
+            s[k] = tile_logits<D, G, W, HP>(kr[k], rw.q, ww.qsum);
         }
         more = tiles != 0;
         if (more) {
             next_tiles<NT>(tiles, tb, n, v.pool, next);
             at.here();
 #pragma unroll
-            for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], step, at);
+            for (int k = 0; k < NT; ++k) load_k<D, G, W, HP>(kr[k], next[k], ww.step, at);
         }
-        float top = -INFINITY;
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
-            if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[k][r] = tile[k].first + 4 * q4 + r <= rw.last ? s[k][r] : -INFINITY;
-            }
-            if (rw.logits && tile[k].first != kNowhere) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k] * scale;
-            top = fmaxf(fmaxf(fmaxf(s[k][0], s[k][1]), fmaxf(s[k][2], s[k][3])), top);
+            if (k && tile[k].first == kNowhere) s[k] = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};             // (uniform)
+            else if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + tile[k].first + 4 * q4) = s[k] * ww.scale;
         }
-        top *= scale;
-        if (__ballot(top > st.ref + kSlack)) {                           // (uniform)
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const bool moves = top > st.ref + kSlack;
-            const float to = moves ? top - kTop : st.ref, f = moves ? __builtin_amdgcn_exp2f(st.ref - to) : 1.0f;
-            st.ref = to;
-            st.sum *= f;
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) st.o[i] *= f;
-        }
-        const float ref = st.ref == -INFINITY ? 0.0f : st.ref;           // (a row that has seen nothing: every logit is -inf)
-        // P = hi + lo: hi has the leading 11 bits of e, so that both conversions are exact (but for what lies below 2^-24)
         typename Halves<NT>::type hi, lo;
-#pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][r], scale, -ref));
-                const float lead = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e) & 0xffffe000u);
-                st.sum += e;
-                hi[4 * k + r] = static_cast<_Float16>(lead);
-                lo[4 * k + r] = static_cast<_Float16>(e - lead);
-            }
+        probabilities<D, NT>(s, ww.scale, st, hi, lo);
         VScale<W> x[NT];
         if constexpr (W != 16) {
 #pragma unroll
-            for (int k = 0; k < NT; ++k) x[k] = v_scale<D, G, W, HP>(vr[k], tile[k].valid, lane);
-        }
-        // 0 * V of a token that a row does not see is 0 only if V is finite: in tiles that not every row sees whole, V that is not counts as
-        // 0 for all rows, and makes those that do see its token NaN.  (What this takes in registers does not fit three wavefronts per SIMD at
-        // head_dim 64, which were 5 to 10 % faster there in packed pages.)
-#pragma unroll
-        for (int k = 0; k < NT; ++k) {
-            if (tile[k].first + 15 > rw.all_see) {                       // (uniform)
-                uint64_t lanes[4], any = 0;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) any |= lanes[r] = __ballot((tile[k].first + 4 * q4 + r > rw.all_see) & not_finite<D, G, W, HP>(vr[k], r));
-                if (any) {                                               // (uniform)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const bool bad = (lanes[r] >> (16 * q4) & 0xffffull) != 0;         // in any of the token's lanes
-                        if constexpr (W == 16) {
-#pragma unroll
-                            for (int i = 0; i < VRegs<D, G, W, HP>::kWords; ++i) vr[k].v[r][i] = bad ? 0u : vr[k].v[r][i];
-                        } else {
-                            x[k].s[r] = bad ? 0.0f : x[k].s[r];
-                            x[k].odd[r] = bad ? 0.0f : x[k].odd[r];
-                            x[k].m[r] = bad ? 0.0f : x[k].m[r];
-                        }
-                        const bool poisoned = bad & (tile[k].first + 4 * q4 + r <= rw.last);
-                        hi[4 * k + r] = poisoned ? static_cast<_Float16>(NAN) : hi[4 * k + r];
-                    }
-                }
-            }
+            for (int k = 0; k < NT; ++k) x[k] = v_scale<D, G, W, HP>(vr[k]);
         }
         unit_values<D, G, W, HP, NT>(vr, x, hi, lo, st);
         if (more) {
             at.here();
 #pragma unroll
-            for (int k = 0; k < NT; ++k) load_v<D, G, W, HP>(vr[k], next[k], step, at, lane);
+            for (int k = 0; k < NT; ++k) load_v<true, D, G, W, HP>(vr[k], next[k], ww.step, at, lane);
         }
     }
+}
+
+// V^T of a tile, every dimension of the lane's, as operands.
+template <int D, int G, int W, bool HP, int i = 0>
+__device__ __forceinline__ void tile_values(const VRegs<D, G, W, HP>& t, const VScale<W>& x, u2_t* y) {
+    y[i] = u2_t{v_pair<D, G, W, HP, i>(t, x, 0), v_pair<D, G, W, HP, i>(t, x, 1)};
+    if constexpr (i + 1 < D / 16) tile_values<D, G, W, HP, i + 1>(t, x, y);
+}
+
+// A wavefront's tiles of width W of which some row does not see some token: a sequence's last one or two, by themselves, so that nothing of
+// this takes registers or instructions from the walk above.  Logits behind a row's token are left out.  0 * V is 0 only if
+// V is finite: where a token that some row does not see has a value that is not (as it enters the product, a half: code * scale + mn can
+// pass a half's range with finite parameters), the token counts as 0 for all rows, and makes those that do see it NaN.
+template <int D, int G, int W, bool HP>
+__device__ __forceinline__ void walk_partly(uint64_t tiles, const TileBatch& tb, int n, const PagesView& v, const RowsOfWave<D, G>& rw,
+                                            RowState<D>& st, int lane) {
+    if (!tiles) return;
+    asm volatile("" : "+v"(lane));
+    const int q4 = lane >> 4;
+    const WidthWalk<D, G, W, HP> ww(v, rw);
+    const LaneAt<D, G, W, HP> at(lane);
+    do {
+        KRegs<D, G, W, HP> kr;
+        VRegs<D, G, W, HP> vr;
+        Tile tile;
+        next_tiles<1>(tiles, tb, n, v.pool, &tile);
+        load_k<D, G, W, HP>(kr, tile, ww.step, at);
+        load_v<false, D, G, W, HP>(vr, tile, ww.step, at, lane);
+        f4_t s = tile_logits<D, G, W, HP>(kr, rw.q, ww.qsum);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = tile.first + 4 * q4 + r <= rw.last ? s[r] : -INFINITY;
+        if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + tile.first + 4 * q4) = s * ww.scale;
+        h4_t hi, lo;
+        probabilities<D, 1>(&s, ww.scale, st, hi, lo);
+        VScale<W> x;
+        if constexpr (W != 16) {
+            x = v_scale<D, G, W, HP>(vr);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {                                // missing tokens: 0
+                const bool there = 4 * q4 + r < tile.valid;
+                x.s[r] = there ? x.s[r] : 0.0f;
+                x.odd[r] = there ? x.odd[r] : 0.0f;
+                x.m[r] = there ? x.m[r] : 0.0f;
+            }
+        }
+        u2_t y[D / 16];
+        tile_values<D, G, W, HP>(vr, x, y);
+        typedef uint16_t us2_t __attribute__((ext_vector_type(2)));
+        us2_t most[2] = {{0, 0}, {0, 0}};                                // of the magnitudes' bits, token by token
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) most[j] = __builtin_elementwise_max(most[j], __builtin_bit_cast(us2_t, y[i][j] & 0x7fff7fffu));
+        uint64_t lanes[4], any = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) any |= lanes[r] = __ballot((tile.first + 4 * q4 + r > rw.all_see) & (most[r / 2][r % 2] >= 0x7c00));
+        if (any) {                                                       // (uniform)
+            uint32_t keep[2] = {0, 0};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool bad = (lanes[r] >> (16 * q4) & 0xffffull) != 0;                 // in any of the token's lanes
+                keep[r / 2] |= bad ? 0u : 0xffffu << (16 * (r % 2));
+                hi[r] = (bad & (tile.first + 4 * q4 + r <= rw.last)) ? static_cast<_Float16>(NAN) : hi[r];
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) y[i] = u2_t{y[i].x & keep[0], y[i].y & keep[1]};
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            st.o[i] = mfma(__builtin_bit_cast(h4_t, y[i]), lo, st.o[i]);
+            st.o[i] = mfma(__builtin_bit_cast(h4_t, y[i]), hi, st.o[i]);
+        }
+    } while (tiles);
 }
 
 // Where dimensions d .. d + 3 of a state's row stand in LDS: the rows' quads are exchanged by the row's number, or else the 16 rows that a
@@ -642,6 +672,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
         rw.scale = g.scale_log2e;
         rw.last = ok ? n - sw.count + nth : -1;
         rw.all_see = n - sw.count + rt * 16 / g.per;
+        const int none_sees = n - sw.count + min(count, (rt * 16 + 15) / g.per + 1);       // tokens from this one on are seen by no row
         rw.logits = logits && ok ? logits + ((static_cast<int64_t>(s) * v.Hkv + h) * g.rows + j) * v.N : nullptr;
         const _Float16* qp = q + static_cast<int64_t>(sw.first + (ok ? nth : 0)) * g.q_stride + (ok ? head : 0) * D;     // (count >= 1)
 #pragma unroll
@@ -681,17 +712,26 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
             const int page = in ? tile_page : 0;
             const uint64_t off = offs[page];
             const uint32_t b = bits[page];
-            const uint32_t width = (in & page_present(v, off, b)) ? b : 0u;
+            // (what no row sees is left out like an absent page)
+            const uint32_t width = (in & page_present(v, off, b) & (tile * 16 < none_sees)) ? b : 0u;
+            const bool whole = tile * 16 + 15 <= rw.all_see;
             const uint32_t row = static_cast<uint32_t>(k_slab * v.T + tile * 16 - page * v.T);     // of the record's rows
             tb.codes = off + static_cast<uint64_t>(row) * (D / 8 * b);
             tb.scales = off + v.bit_bytes * b + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
             int dealt = 0;
-            const uint64_t tiles16 = own_tiles<NT>(width == 16, wave, dealt), tiles8 = own_tiles<NT>(width == 8, wave, dealt);
-            const uint64_t tiles4 = own_tiles<NT>(width == 4, wave, dealt), tiles2 = own_tiles<NT>(width == 2, wave, dealt);
+            const uint64_t tiles16 = own_tiles<NT>(whole & (width == 16), wave, dealt), tiles8 = own_tiles<NT>(whole & (width == 8), wave, dealt);
+            const uint64_t tiles4 = own_tiles<NT>(whole & (width == 4), wave, dealt), tiles2 = own_tiles<NT>(whole & (width == 2), wave, dealt);
+            const uint64_t partly = own_tiles<1>(!whole & (width != 0), wave, dealt);
             walk<D, G, 16, HP, NT>(tiles16, tb, n, v, rw, st, lane);
             walk<D, G, 8, HP, NT>(tiles8, tb, n, v, rw, st, lane);
             walk<D, G, 4, HP, NT>(tiles4, tb, n, v, rw, st, lane);
             walk<D, G, 2, HP, NT>(tiles2, tb, n, v, rw, st, lane);
+            if (partly) {
+                walk_partly<D, G, 16, HP>(partly & __ballot(width == 16), tb, n, v, rw, st, lane);
+                walk_partly<D, G, 8, HP>(partly & __ballot(width == 8), tb, n, v, rw, st, lane);
+                walk_partly<D, G, 4, HP>(partly & __ballot(width == 4), tb, n, v, rw, st, lane);
+                walk_partly<D, G, 2, HP>(partly & __ballot(width == 2), tb, n, v, rw, st, lane);
+            }
             if (logits && wave == 0) {               // what the tokens of absent tiles would have had
                 for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
                     const int t = 16 * (2 * u + __builtin_ctzll(none));

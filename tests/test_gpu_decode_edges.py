@@ -1,0 +1,83 @@
+"""GPU tests of decoding on packed records where values, sizes and the division of work are at their edges, against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.decode as od
+import paper_2403_11805_amd as kvs
+
+from paged import Paged, rows
+from test_gpu_decode import attend, check_attend, put
+
+pytestmark = pytest.mark.gpu
+
+
+def values(p, s, token, head=1):
+    """The V row of a token in layer 0."""
+    return od.Slab(p.os, p.pool, p.off[s, token // p.os.T], p.bits[s, token // p.os.T], 0, 1, head), token % p.os.T
+
+
+# rows of V that are finite halves, with parameters that are finite, and whose top code stands for more than a half holds
+@pytest.mark.parametrize("low", [0.0, -65504.0])
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 64), (128, 128), (256, 64), (256, 256)])
+@pytest.mark.parametrize("width", [8, 4, 2])
+@pytest.mark.parametrize("n", [40, 48, 33])
+def test_values_that_pass_a_half_do_not_reach_rows_in_front_of_them(D, G, width, n, low):
+    """The two newest tokens, appended as they come, have V from `low` to 65504 in a format that rounds the scale up to a half: the rows
+    in front of them and all weights stay as they were.  (Only where the format does that; a row that sees such a value is not finite.)"""
+    p = Paged((1, 2, 4, D, 64, 16, G), [n, 20], (width,), 36, 3)
+    start, n_rows = rows([4, 1])
+    q = p.halves(n_rows, 4, D)
+    k, v = p.halves(n_rows, 2, D), p.halves(n_rows, 2, D)
+
+    def decoded(v):
+        pages, pool = p.device()
+        kvs.kv_append_tokens(pages, 0, put(k), put(v), row_start=put(start))
+        ws = torch.empty(kvs.kv_attend_workspace_bytes(p.ks, 2, 4, True), dtype=torch.uint8, device="cuda")
+        out, mass = torch.empty((n_rows, 4, D), dtype=torch.float16, device="cuda"), torch.zeros((2, 2, 64), device="cuda")
+        kvs.kv_attend_tokens(pages, 0, put(q), ws, out, row_start=put(start), max_rows=4, mass=mass)
+        return out.cpu().numpy(), mass.cpu().numpy(), pool.cpu().numpy()
+
+    want, weights, _ = decoded(v)
+    v[2:4, 1, :] = low
+    v[2:4, 1, 5] = 65504
+    got, mass, pool = decoded(v)
+    held = od.Slab(p.os, pool, p.off[0, (n - 1) // 16], width, 0, 1, 1)
+    assert np.isfinite(held.scale[(n - 1) % 16]).all() and np.isfinite(held.mn[(n - 1) % 16]).all()
+    over = held.values(p.os)[(n - 1) % 16] >= 65520                    # what a half rounds to infinity
+    assert over[5]
+    assert np.array_equal(got[[0, 1, 4]], want[[0, 1, 4]]) and np.array_equal(mass, weights)
+    assert np.array_equal(got[2:4, :2], want[2:4, :2]) and not np.isfinite(got[2:4, 2:][..., over]).any()
+
+
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 64), (256, 256)])
+@pytest.mark.parametrize("width", [8, 4, 2])
+def test_large_scales_do_not_reach_rows_in_front_of_them(D, G, width):
+    """The same with a binary32 scale of a million, and a tile without a partner that is taken twice."""
+    for n in (20, 36, 52):
+        p = Paged((1, 2, 4, D, 64, 16, G), [n, 17], (width,), 37, 0)
+        start, n_rows = rows([3, 1])
+        q = p.halves(n_rows, 4, D)
+        want, weights = attend(p, 0, q, start, 3, None, True)
+        slab, row = values(p, 0, n - 1)
+        slab.scale[row], slab.mn[row], slab.codes[row] = 1e6, -3.0, 0xff
+        got, mass = attend(p, 0, q, start, 3, None, True)
+        assert np.array_equal(got[[0, 1, 3]], want[[0, 1, 3]]) and np.array_equal(mass, weights)
+        assert np.array_equal(got[2, :2], want[2, :2]) and not np.isfinite(got[2, 2:]).any()
+
+
+@pytest.mark.parametrize("fmt", [0, 3])
+@pytest.mark.parametrize("width", [8, 4, 2])
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 64), (256, 128)])
+def test_finite_values_stay_finite_whatever_their_parameters(D, G, width, fmt):
+    """What counts is the value a code stands for: rows of V whose scale would pass a half with a code that they do not have, and rows that
+    reach both ends of a half (their minimum and their range are finite, the sum of the magnitudes is not a half)."""
+    p = Paged((1, 2, 4, D, 64, 16, G), [45, 31], (width,), 38, fmt)
+    start, n_rows = rows([4, 2])
+    for s, n in enumerate(p.len):
+        for token, (scale, low) in zip((n - 1, n - 2), ((60000.0, 0.25), (65472.0 / (2 ** width - 1), -65472.0))):
+            slab, row = values(p, s, token)
+            slab.scale[row], slab.mn[row], slab.codes[row] = scale, low, 0
+        if width == 8:
+            slab.codes[row, ::2] = 255                                   # -65472 + 65472, to fp16's rounding of the scale
+    check_attend(p, 0, p.halves(n_rows, 4, D), start, 4, p.book()[0], True)
