@@ -66,23 +66,21 @@ struct AttendGeom {
 constexpr int kPieceCost = 8;
 struct SeqWork {
     int n, first, count;             // tokens; its new rows
-    int units, pairs;                // units of 32 tokens; (kv head, row tile) pairs, none without rows
+    __device__ __forceinline__ int units() const { return (n + 31) >> 5; }                 // of 32 tokens
+    __device__ __forceinline__ int row_tiles(const AttendGeom& g) const { return (min(count, g.max_rows) * g.per + 15) >> 4; }
 };
 __device__ __forceinline__ SeqWork work_of(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int s) {
-    SeqWork w = {0, 0, 0, 0, 0};
+    SeqWork w = {0, 0, 0};
     if (s < v.n_seqs) {
         w.n = seq_len(v, s);
         const SeqRows rows = seq_rows(row_start, s, g.n_rows);
         w.first = rows.first;
         w.count = rows.count;
-        w.units = (w.n + 31) >> 5;
-        w.pairs = v.Hkv * ((min(w.count, g.max_rows) * g.per + 15) >> 4);
     }
     return w;
 }
 __device__ __forceinline__ SeqWork of_lane(const SeqWork& w, int l) {
-    return {__builtin_amdgcn_readlane(w.n, l), __builtin_amdgcn_readlane(w.first, l), __builtin_amdgcn_readlane(w.count, l),
-            __builtin_amdgcn_readlane(w.units, l), __builtin_amdgcn_readlane(w.pairs, l)};
+    return {__builtin_amdgcn_readlane(w.n, l), __builtin_amdgcn_readlane(w.first, l), __builtin_amdgcn_readlane(w.count, l)};
 }
 
 // Sum over the lanes up to this one (all active): within rows of 16, then the rows' last lanes.
@@ -104,18 +102,20 @@ struct Line {
     int run;                         // places of a workgroup's run
 
     __device__ __forceinline__ static int places(int units, int round, int cost) { return units ? ((units + round - 1) & -round) + cost : 0; }
-    __device__ __forceinline__ int each(const SeqWork& w) const { return places(w.units, round, cost); }
+    __device__ __forceinline__ int each(const SeqWork& w) const { return places(w.units(), round, cost); }
     __device__ __forceinline__ void start(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
         s0 = 0;
         mine = work_of(v, g, row_start, lane);
-        const int one = prefix_sum(places(mine.units, g.step, 0) * mine.pairs), two = prefix_sum(places(mine.units, 2 * g.step, 0) * mine.pairs);
-        const int long_ = prefix_sum(places(mine.units, 1, kPieceCost) * mine.pairs);
+        const int units = mine.units(), pairs = v.Hkv * mine.row_tiles(g);
+        const int one = prefix_sum(places(units, g.step, 0) * pairs), two = prefix_sum(places(units, 2 * g.step, 0) * pairs);
+        const int long_ = prefix_sum(places(units, 1, kPieceCost) * pairs);
         int t1 = __builtin_amdgcn_readlane(one, 63), t2 = __builtin_amdgcn_readlane(two, 63), tl = __builtin_amdgcn_readlane(long_, 63);
         for (int s = 64; s < v.n_seqs; s += 64) {
             const SeqWork w = work_of(v, g, row_start, s + lane);
-            t1 += __builtin_amdgcn_readlane(prefix_sum(places(w.units, g.step, 0) * w.pairs), 63);
-            t2 += __builtin_amdgcn_readlane(prefix_sum(places(w.units, 2 * g.step, 0) * w.pairs), 63);
-            tl += __builtin_amdgcn_readlane(prefix_sum(places(w.units, 1, kPieceCost) * w.pairs), 63);
+            const int u = w.units(), p = v.Hkv * w.row_tiles(g);
+            t1 += __builtin_amdgcn_readlane(prefix_sum(places(u, g.step, 0) * p), 63);
+            t2 += __builtin_amdgcn_readlane(prefix_sum(places(u, 2 * g.step, 0) * p), 63);
+            tl += __builtin_amdgcn_readlane(prefix_sum(places(u, 1, kPieceCost) * p), 63);
         }
         const bool fits1 = t1 <= g.groups * g.step, fits2 = t2 <= g.groups * 2 * g.step;
         round = fits1 ? g.step : fits2 ? 2 * g.step : 1;
@@ -127,7 +127,7 @@ struct Line {
         const int before = __builtin_amdgcn_readlane(end, 63);
         s0 += 64;
         mine = work_of(v, g, row_start, s0 + lane);
-        end = before + prefix_sum(each(mine) * mine.pairs);
+        end = before + prefix_sum(each(mine) * v.Hkv * mine.row_tiles(g));
     }
 };
 
@@ -158,11 +158,12 @@ __device__ __forceinline__ RowShares row_shares(const PagesView& v, const Attend
     x.w = work_of(v, g, row_start, s);
     x.used = 0;
     x.first = 0;
-    if (x.w.units == 0 || x.w.pairs == 0) return x;
+    const int units = x.w.units(), row_tiles = x.w.row_tiles(g);
+    if (units == 0 || row_tiles == 0) return x;
     const LineNote l = *reinterpret_cast<const LineNote*>(note);
-    const int row_tiles = x.w.pairs / v.Hkv, pair = h * row_tiles + j / 16;
-    const int begin = note[4 + s] - Line::places(x.w.units, l.round, l.cost) * (x.w.pairs - pair) + l.cost, wg = begin / l.run;
-    x.used = (begin + x.w.units - 1) / l.run - wg + 1;
+    const int pair = h * row_tiles + j / 16;
+    const int begin = note[4 + s] - Line::places(units, l.round, l.cost) * (v.Hkv * row_tiles - pair) + l.cost, wg = begin / l.run;
+    x.used = (begin + units - 1) / l.run - wg + 1;
     x.first = wg + pair_number(v, g, s, pair);
     return x;
 }
@@ -439,8 +440,7 @@ template <int NT> __device__ __forceinline__ void next_tiles(uint64_t& tiles, co
 // The wavefront's share of a batch's tiles of one width: tiles are put together within their width, whatever the order of the pages
 // (the order of tokens does not matter to attention), and the units of NT, counted over all widths, go to the wavefronts in turn.
 // (Without a branch: copies that the compiler makes of registers where a branch of some lanes ends have gone wrong here.)
-template <int NT> __device__ __forceinline__ uint64_t own_tiles(bool of_width, int wave, int& units) {
-    const uint64_t all = __ballot(of_width);
+template <int NT> __device__ __forceinline__ uint64_t own_tiles(uint64_t all, int wave, int& units) {
     const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
     const int turn = (units + rank / NT) & (kAttendWaves - 1);
     units += (__builtin_popcountll(all) + NT - 1) / NT;
@@ -450,7 +450,7 @@ template <int NT> __device__ __forceinline__ uint64_t own_tiles(bool of_width, i
 // What a walk over tiles of one width needs beside them.
 template <int D, int G, int W, bool HP> struct WidthWalk {
     SlabSteps step;
-    float qsum[D / G], scale;                  // scale: of what tile_logits gives: logits in units of log2
+    float qsum[D / G], scale;                  // of what tile_logits takes and gives (scale: logits in units of log2)
     __device__ __forceinline__ WidthWalk(const PagesView& v, const RowsOfWave<D, G>& rw) {
         const uint64_t rows = static_cast<uint64_t>(v.T) * static_cast<uint32_t>(v.Hkv), params = static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
         step = {static_cast<uint64_t>(v.slabs) * v.T * params, rows * (D * W / 8), rows * params};
@@ -518,6 +518,8 @@ __device__ __forceinline__ void walk(uint64_t tiles, const TileBatch& tb, int n,
         for (int k = 0; k < NT; ++k) {
             tile[k] = next[k];
             s[k] = tile_logits<D, G, W, HP>(kr[k], rw.q, ww.qsum);
+            // (Worked out before the next K is loaded: put off behind that, what they are made of would not fit the registers beside it.)
+            if constexpr (D == 256 && W != 16) asm volatile("" : "+v"(s[k]));
         }
         more = tiles != 0;
         if (more) {
@@ -634,9 +636,9 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
     constexpr int DL = D / 16, NG = D / G, NT = D == 256 ? 1 : 2;      // (256: the registers of two tiles do not fit)
     extern __shared__ float o_lds[];                 // [kAttendWaves][tile_rows][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
-    const int lane = threadIdx.x & 63, l16 = lane & 15, q4 = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     Line line;
+    int lane = threadIdx.x & 63;
     line.start(v, g, row_start, lane);
     int at = static_cast<int>(blockIdx.x) * line.run;
     const int run_begin = at, run_end = at + line.run;
@@ -657,15 +659,20 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
         if (!behind) return;                         // (the end of the line; uniform in the workgroup)
         const int l = __builtin_ctzll(behind), s = line.s0 + l;
         const SeqWork sw = of_lane(line.mine, l);
-        const int each = line.each(sw), n = sw.n, local = at - (__builtin_amdgcn_readlane(line.end, l) - each * sw.pairs);
+        const int row_tiles = sw.row_tiles(g), units = sw.units();
+        const int each = line.each(sw), n = sw.n, local = at - (__builtin_amdgcn_readlane(line.end, l) - each * v.Hkv * row_tiles);
         const int pair = local / each, place = local - pair * each, places = min(each - place, run_end - at);
-        const int u_begin = max(place - line.cost, 0), u_end = min(place + places - line.cost, sw.units);
-        const int row_tiles = sw.pairs / v.Hkv, h = pair / row_tiles, rt = pair - h * row_tiles;
+        const int u_begin = max(place - line.cost, 0), u_end = min(place + places - line.cost, units);
+        const int h = pair / row_tiles, rt = pair - h * row_tiles;
         const int count = min(sw.count, g.max_rows);
         at += places;
         if (u_end <= u_begin) continue;              // the run ends in front of the pair's first unit
 
+        // What depends on the lane is worked out piece by piece, and again where the piece ends: kept over the walk it would not fit the
+        // registers at head_dim 256.
+        asm volatile("" : "+v"(lane));
         // this lane's query row
+        const int l16 = lane & 15, q4 = lane >> 4;
         const int j = rt * 16 + l16, nth = j / g.per, head = h * g.per + j % g.per;
         const bool ok = j < count * g.per;
         RowsOfWave<D, G> rw;
@@ -718,23 +725,25 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
             const uint32_t row = static_cast<uint32_t>(k_slab * v.T + tile * 16 - page * v.T);     // of the record's rows
             tb.codes = off + static_cast<uint64_t>(row) * (D / 8 * b);
             tb.scales = off + v.bit_bytes * b + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.groups * (HP ? 2 : 4));
+            const uint64_t of16 = __ballot(width == 16), of8 = __ballot(width == 8), of4 = __ballot(width == 4), of2 = __ballot(width == 2);
+            const uint64_t seen_whole = __ballot(whole), none = __ballot(in && width == 0);
             int dealt = 0;
-            const uint64_t tiles16 = own_tiles<NT>(whole & (width == 16), wave, dealt), tiles8 = own_tiles<NT>(whole & (width == 8), wave, dealt);
-            const uint64_t tiles4 = own_tiles<NT>(whole & (width == 4), wave, dealt), tiles2 = own_tiles<NT>(whole & (width == 2), wave, dealt);
-            const uint64_t partly = own_tiles<1>(!whole & (width != 0), wave, dealt);
+            const uint64_t tiles16 = own_tiles<NT>(of16 & seen_whole, wave, dealt), tiles8 = own_tiles<NT>(of8 & seen_whole, wave, dealt);
+            const uint64_t tiles4 = own_tiles<NT>(of4 & seen_whole, wave, dealt), tiles2 = own_tiles<NT>(of2 & seen_whole, wave, dealt);
+            const uint64_t partly = own_tiles<1>((of16 | of8 | of4 | of2) & ~seen_whole, wave, dealt);
             walk<D, G, 16, HP, NT>(tiles16, tb, n, v, rw, st, lane);
             walk<D, G, 8, HP, NT>(tiles8, tb, n, v, rw, st, lane);
             walk<D, G, 4, HP, NT>(tiles4, tb, n, v, rw, st, lane);
             walk<D, G, 2, HP, NT>(tiles2, tb, n, v, rw, st, lane);
             if (partly) {
-                walk_partly<D, G, 16, HP>(partly & __ballot(width == 16), tb, n, v, rw, st, lane);
-                walk_partly<D, G, 8, HP>(partly & __ballot(width == 8), tb, n, v, rw, st, lane);
-                walk_partly<D, G, 4, HP>(partly & __ballot(width == 4), tb, n, v, rw, st, lane);
-                walk_partly<D, G, 2, HP>(partly & __ballot(width == 2), tb, n, v, rw, st, lane);
+                walk_partly<D, G, 16, HP>(partly & of16, tb, n, v, rw, st, lane);
+                walk_partly<D, G, 8, HP>(partly & of8, tb, n, v, rw, st, lane);
+                walk_partly<D, G, 4, HP>(partly & of4, tb, n, v, rw, st, lane);
+                walk_partly<D, G, 2, HP>(partly & of2, tb, n, v, rw, st, lane);
             }
             if (logits && wave == 0) {               // what the tokens of absent tiles would have had
-                for (uint64_t none = __ballot(in && width == 0); none; none &= none - 1) {
-                    const int t = 16 * (2 * u + __builtin_ctzll(none));
+                for (uint64_t left = none; left; left &= left - 1) {
+                    const int t = 16 * (2 * u + __builtin_ctzll(left));
                     if (rw.logits) *reinterpret_cast<f4_t*>(rw.logits + t + 4 * q4) = f4_t{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 }
             }
@@ -742,23 +751,25 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
         // the four states against one reference per row
         st.sum += __shfl_xor(st.sum, 16);
         st.sum += __shfl_xor(st.sum, 32);
-        if (q4 == 0) {
-            ml_lds[wave][0][l16] = st.ref;
-            ml_lds[wave][1][l16] = st.sum;
+        const int here = min(16, count * g.per - rt * 16);               // rows of this tile
+        asm volatile("" : "+v"(lane));
+        const int end_row = lane & 15, end_q4 = lane >> 4;
+        if (end_q4 == 0) {
+            ml_lds[wave][0][end_row] = st.ref;
+            ml_lds[wave][1][end_row] = st.sum;
         }
-        if (ok) {
+        if (end_row < here) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int i = 0; i < DL; i += 4)
-                    *reinterpret_cast<f4_t*>(o_lds + o_at<D>(wave * g.tile_rows + l16, l16, DL * (4 * q4 + r) + i)) =
+                    *reinterpret_cast<f4_t*>(o_lds + o_at<D>(wave * g.tile_rows + end_row, end_row, DL * (4 * end_q4 + r) + i)) =
                         f4_t{st.o[i][r], st.o[i + 1][r], st.o[i + 2][r], st.o[i + 3][r]};
         }
         __syncthreads();
-        const bool whole = u_begin == 0 && u_end == sw.units;
+        const bool whole = u_begin == 0 && u_end == units;
         const int64_t slot0 = (blockIdx.x + pair_number(v, g, s, pair)) * g.tile_rows;
-        const int here = min(16, count * g.per - rt * 16);               // rows of this tile
-        for (int i = threadIdx.x; i < here * (D / 4); i += 64 * kAttendWaves) {
+        for (int i = wave * 64 + lane; i < here * (D / 4); i += 64 * kAttendWaves) {
             const int row = i / (D / 4), d = i % (D / 4) * 4;
             float ref = -INFINITY, sum = 0.0f;
 #pragma unroll
