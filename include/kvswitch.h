@@ -607,9 +607,9 @@ uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int3
  *   out = softmax(q K^T / sqrt(head_dim), tokens up to the row's own, absent pages left out) V
  * per query head, query head h reading kv head h / (n_q_heads / n_kv_heads).  K counts with the values code * scale + mn
  * its codes stand for, V with these rounded to fp16; logits, softmax and sums are fp32, probabilities enter the product
- * with V as the sum of two fp16 numbers.  A row that sees no token gives zeros.  What lies behind a sequence's end may be
- * anything, and so may K and V of tokens that a row does not see; a row that sees V that is not finite is NaN, in that
- * dimension at least.
+ * with V as the sum of two fp16 numbers.  A row that sees no token, or none whose logit is more than -inf, gives zeros; one with
+ * a logit that is NaN or +inf is NaN.  What lies behind a sequence's end may be anything, and so may K and V of tokens that a
+ * row does not see; a row that sees V that is not finite is NaN, in that dimension at least.
  *   q        dev fp16 [n_rows][n_q_heads][head_dim], q_stride elements from row to row (>= n_q_heads * head_dim, a
  *            multiple of 8);
  *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others'
@@ -617,7 +617,8 @@ uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int3
  *   mass     dev fp32 [n_seqs][n_kv_heads][n_tokens] of this layer, may be NULL: for every slot below len[s] of a
  *            sequence that has new rows
  *              mass = mass_in + sum over its rows and the query heads of the kv head of the softmax weights
- *            (0 in absent pages); other entries are untouched.  mass_in: same shape, may equal mass (the weights
+ *            (0 in absent pages; of a row whose logits make it NaN the weights are NaN, but for tokens that it does not see
+ *            or whose logit is -inf); other entries are untouched.  mass_in: same shape, may equal mass (the weights
  *            accumulate in place) or be NULL (zeros), but not overlap it otherwise;
  *   out      dev fp16 [n_rows][n_q_heads][head_dim], 16-byte aligned;
  *   workspace dev, >= kv_attend_workspace_bytes(), 256-byte aligned, contents scratch.

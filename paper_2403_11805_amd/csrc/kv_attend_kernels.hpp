@@ -891,7 +891,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
         row_total(part_ml, of.first * g.tile_rows + j % 16, g.tile_rows, of.used, lane, nullptr, ref, sum);
         if (lane == 0) {
             refs[j] = sum > 0.0f ? ref : 0.0f;                   // (a row that sees nothing weighs nothing: its logits are -inf)
-            invs[j] = sum > 0.0f ? 1.0f / sum : 0.0f;
+            invs[j] = sum > 0.0f ? 1.0f / sum : sum;             // (0 then; NaN if a logit is NaN or +inf)
         }
     }
     __syncthreads();
@@ -899,8 +899,13 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(PagesView v, AttendG
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     auto add = [&](const f4_t& x, int j) {
         const float ref = refs[j], inv = invs[j];
+        if (inv != inv) {                                        // a row that is NaN: so are its weights, of the tokens it sees
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - ref), inv, sum[e]);
+            for (int e = 0; e < 4; ++e) sum[e] = x[e] == -INFINITY ? sum[e] : inv;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] = __builtin_fmaf(__builtin_amdgcn_exp2f(x[e] - ref), inv, sum[e]);
+        }
     };
 #pragma unroll
     for (int j = 0; j < kEarly; ++j)

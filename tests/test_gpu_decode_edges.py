@@ -81,3 +81,33 @@ def test_finite_values_stay_finite_whatever_their_parameters(D, G, width, fmt):
         if width == 8:
             slab.codes[row, ::2] = 255                                   # -65472 + 65472, to fp16's rounding of the scale
     check_attend(p, 0, p.halves(n_rows, 4, D), start, 4, p.book()[0], True)
+
+
+@pytest.mark.parametrize("what", [np.inf, np.nan])
+@pytest.mark.parametrize("width", [16, 8, 4, 2])
+@pytest.mark.parametrize("D,N,n,token", [(64, 64, 40, 20), (64, 1024, 900, 3), (64, 64, 40, 38), (128, 1024, 1000, 998), (256, 64, 33, 31), (256, 512, 500, 100)])
+def test_weights_of_rows_whose_logits_are_not_finite(D, N, n, token, width, what):
+    """K of a token is NaN or gives a logit of +inf in one kv head.  Rows of that head that see the token are NaN, and so are their weights, of
+    every token that they see; what they do not see (tokens behind them, an absent page) gets nothing from them, and other rows and heads
+    are as they were."""
+    p = Paged((1, 2, 4, D, N, 16, 64), [n, 20], (width,), 40, 0)
+    p.bits[0, 0 if token >= 16 else 1] = 0
+    absent = np.arange(16) + (0 if token >= 16 else 16)
+    start, n_rows = rows([5, 1])
+    q = np.abs(p.halves(n_rows, 4, D)) + np.float16(0.125)               # (infinite K is +inf times a sum of these)
+    mass_in = p.book()[0]
+    want, weights = attend(p, 0, q, start, 4, mass_in, True)               # (the fifth row is not computed)
+    slab = od.Slab(p.os, p.pool, p.off[0, token // 16], width, 0, 0, 1)
+    if width == 16:
+        slab.codes[token % 16].view(np.float16)[3] = what
+    else:
+        slab.mn[token % 16] = what
+    got, mass = attend(p, 0, q, start, 4, mass_in, True)
+    sees = np.array([n - 5 + j >= token for j in range(4)])
+    assert np.isnan(got[:4, 2:][sees]).all() and np.array_equal(got[:4, 2:][~sees], want[:4, 2:][~sees])
+    assert np.array_equal(got[:4, :2], want[:4, :2]) and np.array_equal(got[4:], want[4:])
+    assert np.array_equal(mass[1], weights[1]) and np.array_equal(mass[0, 0], weights[0, 0])
+    last = n - 5 + np.flatnonzero(sees)[-1]                               # the last token that a row of these sees
+    seen = np.arange(N) <= last
+    seen[absent] = False
+    assert np.isnan(mass[0, 1, seen]).all() and np.array_equal(mass[0, 1, ~seen], weights[0, 1, ~seen])
