@@ -609,7 +609,8 @@ uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int3
  * its codes stand for, V with these rounded to fp16; logits, softmax and sums are fp32, probabilities enter the product
  * with V as the sum of two fp16 numbers.  A row that sees no token, or none whose logit is more than -inf, gives zeros; one with
  * a logit that is NaN or +inf is NaN.  What lies behind a sequence's end may be anything, and so may K and V of tokens that a
- * row does not see; a row that sees V that is not finite is NaN, in that dimension at least.
+ * row does not see; a row that sees V that is not finite (as rounded to fp16) is not finite itself, in that dimension at
+ * least: infinite or NaN, as the token's place and weight have it.
  *   q        dev fp16 [n_rows][n_q_heads][head_dim], q_stride elements from row to row (>= n_q_heads * head_dim, a
  *            multiple of 8);
  *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others'

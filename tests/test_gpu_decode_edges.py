@@ -83,6 +83,28 @@ def test_finite_values_stay_finite_whatever_their_parameters(D, G, width, fmt):
     check_attend(p, 0, p.halves(n_rows, 4, D), start, 4, p.book()[0], True)
 
 
+@pytest.mark.parametrize("what", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("width", [16, 8, 4, 2])
+@pytest.mark.parametrize("D,G", [(64, 64), (128, 64), (256, 256)])
+def test_values_that_are_not_finite_in_a_tile_that_every_row_sees(D, G, width, what):
+    """A row that sees them is not finite in their dimensions; the other dimensions and the other heads are as they were, and so are weights."""
+    p = Paged((1, 2, 4, D, 128, 16, G), [100, 20], (width,), 39, 0)
+    start, n_rows = rows([2, 1])
+    q = p.halves(n_rows, 4, D)
+    want, weights = attend(p, 0, q, start, 2, None, True)
+    slab, row = values(p, 0, 3)
+    hit = np.zeros(D, dtype=bool)
+    if width == 16:
+        hit[[3, D - 1]] = True
+        slab.codes[row].view(np.float16)[hit] = what
+    else:
+        hit[:G] = True
+        slab.mn[row, 0] = what
+    got, mass = attend(p, 0, q, start, 2, None, True)
+    assert not np.isfinite(got[:2, 2:][..., hit]).any() and np.array_equal(got[:2, 2:][..., ~hit], want[:2, 2:][..., ~hit])
+    assert np.array_equal(got[:2, :2], want[:2, :2]) and np.array_equal(got[2], want[2]) and np.array_equal(mass, weights)
+
+
 @pytest.mark.parametrize("what", [np.inf, np.nan])
 @pytest.mark.parametrize("width", [16, 8, 4, 2])
 @pytest.mark.parametrize("D,N,n,token", [(64, 64, 40, 20), (64, 1024, 900, 3), (64, 64, 40, 38), (128, 1024, 1000, 998), (256, 64, 33, 31), (256, 512, 500, 100)])
