@@ -63,7 +63,6 @@ struct AttendGeom {
 //     what beginning and ending a piece takes, so that runs through many short ones are shorter.
 // One context, 32 kv heads of 128, whole steps against the line: 64 tokens 6.8 against 11.2 us, 512 8.3 and 12.5, 2048 10.6 and 12.8, 4096
 // 14.1 and 16.1.  24 ragged contexts: 49 us with 8 places, 50 with 16, 71 with none; 8 of 32 kv heads 43, 45 and 43.
-constexpr int kPieceCost = 8;
 struct SeqWork {
     int n, first, count;             // tokens; its new rows
     __device__ __forceinline__ int units() const { return (n + 31) >> 5; }                 // of 32 tokens
@@ -98,30 +97,29 @@ __device__ __forceinline__ int prefix_sum(int x) {
 struct Line {
     SeqWork mine;                    // of sequence s0 + lane
     int s0, end;                     // end: of the lane's sequence
-    int round, cost;                 // a pair's places: its units in multiples of `round` (a power of two), and `cost` in front
+    int round, cost;                 // of a pair's places
     int run;                         // places of a workgroup's run
 
-    __device__ __forceinline__ static int places(int units, int round, int cost) { return units ? ((units + round - 1) & -round) + cost : 0; }
-    __device__ __forceinline__ int each(const SeqWork& w) const { return places(w.units(), round, cost); }
+    __device__ __forceinline__ int each(const SeqWork& w) const { return attend_places(w.units(), round, cost); }
     __device__ __forceinline__ void start(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
         s0 = 0;
         mine = work_of(v, g, row_start, lane);
         const int units = mine.units(), pairs = v.Hkv * mine.row_tiles(g);
-        const int one = prefix_sum(places(units, g.step, 0) * pairs), two = prefix_sum(places(units, 2 * g.step, 0) * pairs);
-        const int long_ = prefix_sum(places(units, 1, kPieceCost) * pairs);
+        const int one = prefix_sum(attend_places(units, g.step, 0) * pairs), two = prefix_sum(attend_places(units, 2 * g.step, 0) * pairs);
+        const int long_ = prefix_sum(attend_places(units, 1, kPieceCost) * pairs);
         int t1 = __builtin_amdgcn_readlane(one, 63), t2 = __builtin_amdgcn_readlane(two, 63), tl = __builtin_amdgcn_readlane(long_, 63);
         for (int s = 64; s < v.n_seqs; s += 64) {
             const SeqWork w = work_of(v, g, row_start, s + lane);
             const int u = w.units(), p = v.Hkv * w.row_tiles(g);
-            t1 += __builtin_amdgcn_readlane(prefix_sum(places(u, g.step, 0) * p), 63);
-            t2 += __builtin_amdgcn_readlane(prefix_sum(places(u, 2 * g.step, 0) * p), 63);
-            tl += __builtin_amdgcn_readlane(prefix_sum(places(u, 1, kPieceCost) * p), 63);
+            t1 += __builtin_amdgcn_readlane(prefix_sum(attend_places(u, g.step, 0) * p), 63);
+            t2 += __builtin_amdgcn_readlane(prefix_sum(attend_places(u, 2 * g.step, 0) * p), 63);
+            tl += __builtin_amdgcn_readlane(prefix_sum(attend_places(u, 1, kPieceCost) * p), 63);
         }
-        const bool fits1 = t1 <= g.groups * g.step, fits2 = t2 <= g.groups * 2 * g.step;
-        round = fits1 ? g.step : fits2 ? 2 * g.step : 1;
-        cost = (fits1 | fits2) ? 0 : kPieceCost;
-        run = (fits1 | fits2) ? round : (tl + g.groups - 1) / g.groups;
-        end = fits1 ? one : fits2 ? two : long_;
+        const AttendDivision d = attend_division(t1, t2, tl, g.groups, g.step);
+        round = d.round;
+        cost = d.cost;
+        run = d.run;
+        end = round == g.step ? one : round == 1 ? long_ : two;
     }
     __device__ __forceinline__ void next(const PagesView& v, const AttendGeom& g, const int32_t* __restrict__ row_start, int lane) {
         const int before = __builtin_amdgcn_readlane(end, 63);
@@ -162,7 +160,7 @@ __device__ __forceinline__ RowShares row_shares(const PagesView& v, const Attend
     if (units == 0 || row_tiles == 0) return x;
     const LineNote l = *reinterpret_cast<const LineNote*>(note);
     const int pair = h * row_tiles + j / 16;
-    const int begin = note[4 + s] - Line::places(units, l.round, l.cost) * (v.Hkv * row_tiles - pair) + l.cost, wg = begin / l.run;
+    const int begin = note[4 + s] - attend_places(units, l.round, l.cost) * (v.Hkv * row_tiles - pair) + l.cost, wg = begin / l.run;
     x.used = (begin + units - 1) / l.run - wg + 1;
     x.first = wg + pair_number(v, g, s, pair);
     return x;

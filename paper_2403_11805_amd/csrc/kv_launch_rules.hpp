@@ -76,6 +76,20 @@ inline int64_t attend_groups(int64_t pairs, int64_t tokens, int head_dim) {
     return std::max<int64_t>(1, std::min<int64_t>(resident, steps));
 }
 
+// Attention over pages: places that a (kv head, row tile) pair of `units` units of 32 tokens takes in the line of work: its units in multiples
+// of `round` (a power of two), and `cost` in front of them; and what a workgroup takes of the line, from the sum of the places of all pairs
+// with rounds of one and of two steps, and with kPieceCost in front (the measurements stand at the kernel).
+constexpr int kPieceCost = 8;
+constexpr int32_t attend_places(int32_t units, int32_t round, int32_t cost) { return units ? ((units + round - 1) & -round) + cost : 0; }
+struct AttendDivision {
+    int32_t round, cost, run;
+};
+constexpr AttendDivision attend_division(int32_t in_steps, int32_t in_two_steps, int32_t in_line, int32_t groups, int32_t step) {
+    if (in_steps <= groups * step) return {step, 0, step};
+    if (in_two_steps <= groups * 2 * step) return {2 * step, 0, 2 * step};
+    return {1, kPieceCost, (in_line + groups - 1) / groups};
+}
+
 // Eviction: workgroups that share a pair's moves, `rows` at a time each: some 2048 in all, at least four a pair.  512 pairs of 1170 moves
 // 130 us with 1024 or 2048, 145 with 4096; 12 pairs of up to 5700 moves 27 us with 4096, 28 with 2048, 31 with 1024.
 inline int64_t evict_blocks(int64_t pairs, int64_t list, int64_t rows) {

@@ -6,6 +6,7 @@ import torch
 import oracle.decode as od
 import paper_2403_11805_amd as kvs
 
+from division_cases import CASES, lengths_and_rows
 from paged import Paged, rows
 from test_gpu_decode import attend, check_attend, put
 
@@ -133,3 +134,14 @@ def test_weights_of_rows_whose_logits_are_not_finite(D, N, n, token, width, what
     seen = np.arange(N) <= last
     seen[absent] = False
     assert np.isnan(mass[0, 1, seen]).all() and np.array_equal(mass[0, 1, ~seen], weights[0, 1, ~seen])
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
+def test_attend_however_its_work_is_divided(case):
+    """(test_attend_division.py holds the cases to their ways.)"""
+    way, D, G, Hkv, Hq, n, N, most = case
+    lens, counts = lengths_and_rows(case)
+    p = Paged((1, Hkv, Hq, D, N, 16, G), lens, (16, 8, 4, 2, 16, 0), 43)
+    start, n_rows = rows(counts)
+    mass_in = p.book()[0] if way != "two" else None
+    check_attend(p, 0, p.halves(n_rows, Hq, D), start, most, mass_in, True)
