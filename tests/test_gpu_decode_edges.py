@@ -7,8 +7,9 @@ import oracle.decode as od
 import paper_2403_11805_amd as kvs
 
 from division_cases import CASES, lengths_and_rows
+from halves import cancelling, exact_values, halves_bar
 from paged import Paged, rows
-from test_gpu_decode import attend, check_attend, put
+from test_gpu_decode import attend, check_attend, put, run_evict
 
 pytestmark = pytest.mark.gpu
 
@@ -136,6 +137,20 @@ def test_weights_of_rows_whose_logits_are_not_finite(D, N, n, token, width, what
     assert np.isnan(mass[0, 1, seen]).all() and np.array_equal(mass[0, 1, ~seen], weights[0, 1, ~seen])
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [20, 37, 64])
+def test_probabilities_keep_22_bits(D, n):
+    """V is made to cancel, so that what is left of a result shows the probabilities' own rounding (see halves.py)."""
+    p = Paged((1, 1, 1, D, 320, 16, 64), [n], (16,), 41)
+    q, k, v, weights = cancelling(D, n, 41)
+    for token in range(n):
+        for w, x in ((0, k), (1, v)):
+            od.Slab(p.os, p.pool, p.off[0, token // 16], 16, 0, w, 0).put(p.os, token % 16, x[token])
+    got, _ = attend(p, 0, q[None, None])
+    want = exact_values(weights, v)
+    assert np.all(np.abs(got[0, 0].astype(np.float64) - want) <= halves_bar(weights, v))
+
+
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
 def test_attend_however_its_work_is_divided(case):
     """(test_attend_division.py holds the cases to their ways.)"""
@@ -145,3 +160,19 @@ def test_attend_however_its_work_is_divided(case):
     start, n_rows = rows(counts)
     mass_in = p.book()[0] if way != "two" else None
     check_attend(p, 0, p.halves(n_rows, Hq, D), start, most, mass_in, True)
+
+
+@pytest.mark.parametrize("N,lens,keep", [(4096, [4096, 4081], 1000), (8192, [8192, 8191], 5000), (16384, [16384, 16370], 3000),
+                                         (16400, [16400, 16385], 9000), (32768, [32768, 20000], 7000)])
+@pytest.mark.parametrize("kind", ["ties", "distinct"])
+def test_evict_at_the_bounds_of_keys_per_lane(N, lens, keep, kind):
+    """Capacities that take exactly 4, 8, 16 and 32 keys a lane, the first that takes 32, and sequences that fill them."""
+    p = Paged((1, 1, 1, 64, N, 16, 64), lens, (16,), 44)
+    mass, pos = p.book(1)
+    if kind == "distinct":
+        mass = p.rng.permutation(mass.size).reshape(mass.shape).astype(np.float32) - 1000
+    pool, m, q = run_evict(p, (0, 1), mass, pos, keep, 4, 100)
+    want = p.pool.copy()
+    wm, wp = od.evict(p.os, want, *p.table(), (0, 1), mass, pos, keep, 4, 100)
+    assert np.array_equal(pool, want)
+    assert np.array_equal(m[..., :keep], wm[..., :keep]) and np.array_equal(q[..., :keep], wp[..., :keep])
