@@ -8,18 +8,19 @@ on first attribute access so that importing the package never needs the library.
 from __future__ import annotations
 
 import importlib
+import sys
 
 __all__ = ["binding", "build", "synth"]
+
+_BINDING = f"{__name__}.binding"
 
 
 def __getattr__(name):
     if name in __all__:
         return importlib.import_module(f"{__name__}.{name}")
-    binding = importlib.import_module(f"{__name__}.binding")
+    # looked up in the binding every time, so that what is replaced there is replaced here too (0.4 us; import_module takes 3)
+    binding = sys.modules.get(_BINDING) or importlib.import_module(_BINDING)
     try:
-        found = getattr(binding, name)
+        return getattr(binding, name)
     except AttributeError:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}") from None
-    if name.startswith("kv_"):           # an entry point: the next access finds it here (3 us less per call)
-        globals()[name] = found
-    return found
