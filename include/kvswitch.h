@@ -583,7 +583,7 @@ typedef struct {
  * [row_start[s], row_start[s+1]) of n_rows (row_start: dev i32 [n_seqs+1], ascending; NULL: one row per sequence,
  * n_rows == n_seqs).  Its j-th of c rows is its token len[s] - c + j.  A sequence may have none; a row whose token
  * would be negative has no place and sees nothing; rows in front of row_start[0] or behind row_start[n_seqs] belong
- * to no sequence: nothing of theirs is read or written. */
+ * to no sequence: nothing of theirs is used or written. */
 
 /* Append (Claim with contents, Sec. 3.1 primitive 1): writes the K and V rows of the new tokens to their places in
  * one layer of their pages, each at the width of its page: fp16 copied, 8 / 4 / 2 bits quantised by the rule above
@@ -614,7 +614,8 @@ uint64_t kv_attend_workspace_bytes(const kv_shape_t* shape, int32_t n_seqs, int3
  *   q        dev fp16 [n_rows][n_q_heads][head_dim], q_stride elements from row to row (>= n_q_heads * head_dim, a
  *            multiple of 8);
  *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others'
- *            output is left as it was);
+ *            output is left as it was).  n_q_heads / n_kv_heads * max_rows =: R <= 1024, and n_seqs * n_kv_heads *
+ *            (R + ceil(n_tokens / 1024)) < 2^24 (else KV_ESHAPE);
  *   mass     dev fp32 [n_seqs][n_kv_heads][n_tokens] of this layer, may be NULL: for every slot below len[s] of a
  *            sequence that has new rows
  *              mass = mass_in + sum over its rows and the query heads of the kv head of the softmax weights

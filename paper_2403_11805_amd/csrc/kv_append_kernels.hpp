@@ -5,9 +5,11 @@
 
 namespace kvs {
 
-// Bytes bound it: a row is read once and written once, 16 bytes a lane, past the caches.  Six prompts of 300 to 4096 tokens,
-// 32 kv heads of 128 (458 MB): 88 to 91 us in fp16 pages, 5.0 to 5.2 TB/s, 84 in packed ones.  One token for each of 64
-// sequences takes 3.1 us, which is a launch and three dependent loads.
+// Bytes bound it in fp16 pages: a row is read once and written once, 16 bytes a lane, past the caches.  Six prompts of 300 to 4096
+// tokens, 32 kv heads of 128 (458 MB): 88 to 91 us, 5.0 to 5.2 TB/s.  Packed pages take as long for fewer bytes: 88 us at 8 bits (355
+// MB), 83 at 4 (298), 92 at 2 (270, two groups per row).  The memory gets as many write requests as in fp16 (4.4 million against 4.1
+// at 8 bits, half of them not whole; 3.3 at 2 bits, seven eighths), and vector instructions take 50 us of it.  One token for each
+// of 64 sequences takes 3.1 us, 3.5 to 3.7 packed, which is a launch and three dependent loads.
 // Work unit: up to PPL * 64 pieces (8 elements, 16 bytes) of one row's K and V heads, K's first, per wavefront.  The row's
 // sequence, its page and the page's width are wave-uniform, so the width is one branch for the whole wavefront, and the rows'
 // loads are issued before the three dependent list loads that lead to the page.

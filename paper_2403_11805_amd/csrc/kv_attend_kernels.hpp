@@ -17,14 +17,18 @@
 // An MFMA lines its products up by the exponents without shifting a subnormal's leading zeros out first, and keeps so many bits less of
 // them: K's codes therefore stand at the mantissa's top (weights of 2-bit pages are off by 8e-7 so, by 7e-5 with
 // the codes at its low end; of 8-bit pages by 4e-7, and by up to 1.7e-6 at its low end, a shift less per pair).
-// V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s: the value that a Load gives, off by
-// 2^-11 of itself at most, as the result is when it is rounded; more bits would take a second MFMA and twice the registers.  P enters as the sum of two
-// halves (22 bits): the second MFMA costs nothing next to the loads, and fp16's 11 bits would be the largest error of a result.
+// V is dequantised by one v_fma_mix per element, fp16(code * s + mn), the power of two taken into s: off by 2^-11 of itself at most, as the
+// result is when it is rounded.  (A Load rounds the product to binary32 first, so that its half can be the neighbour of this one.)  More
+// bits would take a second MFMA and half as many operands again; as it is, results over packed pages are off by 2.3e-4 of their norm
+// against 64 bits, and by 2.0e-4 if V is not rounded.  P enters as the sum of two halves (22 bits): the second MFMA costs nothing next to the
+// loads, and 11 bits would be the largest error of a result.
 //
-// What bounds it.  fp16 pages: HBM, 16 contexts of 32768 tokens, 32 query heads on 8 kv heads of 128 (2.15 GB) 370 us, 5.8 TB/s; one of
-// 32768 30 us, 4.5 TB/s.  Packed pages: vector instructions, of which a unit of 32 tokens takes 431 (8 bits) to 476 (2 bits) beside 24
-// MFMAs; 24 contexts of 4096 take 47 us at 8 bits, 37 at 4, 34 at 2, 75 in fp16.  Short contexts: the chain of loads from the
-// lengths to the keys and of the arithmetic behind them, 5 to 10 us for one context of up to 1000 tokens (head_dim 64 to 256).
+// What bounds it.  fp16 pages: HBM, 16 contexts of 32768 tokens, 32 query heads on 8 kv heads of 128 (2.15 GB) 364 to 375 us, 5.7 to 5.9 TB/s;
+// one of 32768 30 us, of which some 6 are the chain below.  Packed pages: vector instructions, of which a unit of 32 tokens at head_dim 128
+// takes 346 (8 bits) to 380 (2 bits) beside 24 MFMAs with one group per row and parameters in binary16, 406 to 441 with two in
+// binary32, 196 in fp16 (at head_dim 256 a unit is 16 tokens: 320 to 342, 40 MFMAs); 24 contexts of 4096 take 47 us at 8 bits, 36 at
+// 4, 34 at 2, 76 in fp16.  Short contexts: the chain of loads from the lengths to the keys and of the arithmetic behind them, 5 to 9.5
+// us for one context of up to 1000 tokens (head_dim 64 to 256).
 #pragma once
 
 #include "kv_launch_rules.hpp"
@@ -437,7 +441,8 @@ template <int NT> __device__ __forceinline__ void next_tiles(uint64_t& tiles, co
 
 // The wavefront's share of a batch's tiles of one width: tiles are put together within their width, whatever the order of the pages
 // (the order of tokens does not matter to attention), and the units of NT, counted over all widths, go to the wavefronts in turn.
-// (Without a branch: copies that the compiler makes of registers where a branch of some lanes ends have gone wrong here.)
+// (Without a branch: copies that the compiler made of registers where a branch of some lanes ended were made for these lanes only, when the
+// kernel had more to hold than its registers; tests/test_kernel_resources.py keeps it below that.)
 template <int NT> __device__ __forceinline__ uint64_t own_tiles(uint64_t all, int wave, int& units) {
     const int rank = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
     const int turn = (units + rank / NT) & (kAttendWaves - 1);
@@ -631,7 +636,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, 2) void attend_kernel(PagesView 
                                                                    const int32_t* __restrict__ row_start, _Float16* __restrict__ out,
                                                                    float* __restrict__ part_o, float* __restrict__ part_ml,
                                                                    float* __restrict__ logits, int32_t* __restrict__ note) {
-    constexpr int DL = D / 16, NG = D / G, NT = D == 256 ? 1 : 2;      // (256: the registers of two tiles do not fit)
+    constexpr int DL = D / 16, NG = D / G, NT = D == 256 ? 1 : 2;      // (256: two tiles spill 42 to 119 registers)
     extern __shared__ float o_lds[];                 // [kAttendWaves][tile_rows][D]
     __shared__ float ml_lds[kAttendWaves][2][16];
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
@@ -821,8 +826,8 @@ __device__ __forceinline__ void row_total(const float* __restrict__ part_ml, int
 // that the rows have left: mass = mass_in + sum over rows of 2^(logit - reference) / sum.
 // `weight` holds as many floats as the attention has workgroups.
 // Latency bounds it: a launch, the row's place in the line, the shares' sums, the shares: 4 to 5 us (2.4 where no row is divided).  Weights
-// of 24 contexts of up to 8000 tokens (13 MB of logits read, 6 MB of weights read and written) 10 us in all.  1024 contexts, 32
-// query heads: 44 us, 234 when every workgroup went through all sequences again for its place; 4096 contexts 163 and 3307.
+// of 24 contexts of up to 8000 tokens (13 MB of logits read, 6 MB of weights read and written) 10.6 us in all.  Nearly all workgroups of many
+// sequences find nothing divided: 1024 contexts, 32 query heads, 41 us, 4096 contexts 149.
 constexpr int kMaxPairRows = 1024;
 constexpr int kEarly = 4;
 template <int D>

@@ -293,8 +293,10 @@ __device__ __forceinline__ void piece_store(const PagesView& v, uint8_t* record,
 
 // The moves of a pair's list, `blocks` workgroups per pair: D/8 neighbouring lanes carry kAtOnce rows, their K and their V, with their
 // weight and position.  Rows come from slots at or above `keep` and go to slots below it, so no move reads what another has written.
-// HBM bounds it: 512 pairs of 1170 moves of 512 bytes, 32 kv heads of 128 (613 MB) take 130 us, 4.7 TB/s; rows of one
+// HBM bounds it in fp16 pages: 512 pairs of 1170 moves of 512 bytes, 32 kv heads of 128 (613 MB) take 130 us, 4.7 TB/s; rows of one
 // head lie 256 bytes apart, K from V megabytes.  One move per pair takes 4 us: three dependent loads behind a launch.
+// Rows of packed pages are moved one at a time, and the chain of their loads bounds it (wavefronts wait for three quarters of their time): the
+// same moves take 275 us at 8 bits, 252 at 4, 237 at 2 (345, 192, 115 MB), 302 where pages of all three change a row's width.
 // A row's way is list entry - page entry - row - store: the four steps of the kAtOnce rows are taken together.
 constexpr int kAtOnce = 4;
 template <int D>

@@ -62,7 +62,8 @@ inline int64_t attention_shares(int64_t pairs, int64_t n_kv_heads, int64_t tiles
 
 // Append: 16-byte pieces per lane of a wavefront's share of a row's K and V heads: one, until four leave some 2048 wavefronts.
 // One token for each of 64 sequences, 8 kv heads of 128, 3.2 us with one, 3.7 with four; a prompt of 500 tokens 3.8 and 4.2, four
-// of 512 6.1 and 5.2, of 2048 14.9 and 12.1; six of up to 4096, 32 kv heads, 96.6 and 91.3 (packed pages 108.2 and 84.0).
+// of 512 6.1 and 5.2, of 2048 14.9 and 12.1; six of up to 4096, 32 kv heads, 97.7 and 89.9 (pages of
+// 8, 4 and 2 bits 113, 111, 110 and 88, 81, 92).
 inline int append_pieces_per_lane(int64_t n_rows, int pieces) { return n_rows * pieces >= 4 * 64 * 2048 ? 4 : 1; }
 
 // Attention over pages: units of 32 tokens that a workgroup's wavefronts take at once, and workgroups: as many as are resident at once
