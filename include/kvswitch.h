@@ -658,6 +658,81 @@ int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_
                         void* workspace, uint64_t workspace_bytes,
                         float* mass, int32_t* pos, void* stream);
 
+/* ------------------------------------------------ latent caches */
+
+/* A model whose heads share one latent vector a token: a token's row in the cache is a latent c of latent_dim numbers, from which one weight
+ * matrix makes the key and the value of every head, and a position part r of rope_dim numbers that is a key of every head as it is,
+ *     k[h] = (c w_k[h], r),   v[h] = c w_v[h].
+ * The cache holds c and r, once for all heads.  Its records lie in pages (kv_pages_t) like those of the calls above, with the same rules for
+ * tables, lengths, absent pages and new rows, at widths {16, 8, 4, 2}: the record of a page of width b is
+ *     codes  [n_layers][chunk_tokens][latent_dim * b / 8]     (b = 16: the latents in fp16)
+ *     scale  [n_layers][chunk_tokens][latent_dim / group]     fp32, format 3: binary16      (b < 16 only)
+ *     mn     same shape                                                                     (b < 16 only)
+ *     r      [n_layers][chunk_tokens][rope_dim]               fp16 at every width
+ * with codes, scale and mn of a token's groups as in formats 0 and 3: positions hang on r and it is a ninth of a row, so it is not packed.
+ * Requirements (else KV_ESHAPE): latent_dim in {256, 512}, rope_dim in {32, 64}, key_dim and value_dim in {64, 128}, 1 <= n_heads <= 1024, group
+ * in {64, 128, 256, 512} dividing latent_dim, format 0 or 3, chunk_tokens % 16 == 0 and <= 1024, n_tokens (the most of a sequence) a multiple
+ * of chunk_tokens and at most 16777216, n_layers * chunk_tokens <= 16777216.
+ * With kv_latent_read_tokens and kv_latent_append_tokens through a second table a page changes its width: its rows are read and appended
+ * to a page of the other. */
+typedef struct {
+    int32_t n_layers;
+    int32_t n_heads;       /* query heads */
+    int32_t latent_dim;
+    int32_t rope_dim;
+    int32_t key_dim;       /* of a head, without the position part */
+    int32_t value_dim;     /* of a head */
+    int32_t n_tokens;
+    int32_t chunk_tokens;
+    int32_t group;         /* quantisation group along latent_dim */
+    int32_t format;        /* KV_FMT_F16_GROUPS (0) or KV_FMT_F16_GROUPS_H (3) */
+} kv_latent_shape_t;
+
+/* Bytes of one page's record at width `bits`; 0 if shape or bits are invalid. */
+uint64_t kv_latent_record_bytes(const kv_latent_shape_t* shape, int32_t bits);
+
+/* Append: the rows of the new tokens to their places in one layer of their pages, each at the width of its page.
+ *   c   dev fp16 [n_rows][latent_dim], c_stride elements from row to row; r dev fp16 [n_rows][rope_dim], r_stride elements (strides
+ *       multiples of 8, c and r 16-byte aligned: both may be parts of one projection's output).
+ * n_rows == 0 is a no-op. */
+int32_t kv_latent_append_tokens(const kv_latent_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                                const void* c, int64_t c_stride, const void* r, int64_t r_stride,
+                                int32_t n_rows, const int32_t* row_start, void* stream);
+
+/* Read: the same rows back from their pages, in fp16, as a Load gives them: fp16(code * scale + mn), product and sum rounded separately.
+ * Rows that have no place, or one in an absent page, are left as they are.  (A table with other lengths reads other tokens.) */
+int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                              void* c, int64_t c_stride, void* r, int64_t r_stride,
+                              int32_t n_rows, const int32_t* row_start, void* stream);
+
+/* Attention of the new rows to one layer's pages as they are packed,
+ *   out[h] = softmax((q[h] . (c w_k[h], r)) / sqrt(key_dim + rope_dim), tokens up to the row's own, absent pages left out) (c w_v[h]),
+ * with c as kv_latent_read_tokens gives it.  Logits, softmax and sums are fp32.  A row that sees no token, or none whose logit is more than
+ * -inf, gives zeros; one with a logit that is NaN or +inf is NaN.  What lies behind a sequence's end may be anything, and so may the rows of
+ * tokens that a row does not see; a row that sees a token whose latent is not finite is not finite itself.
+ *   q    dev fp16 [n_rows][n_heads][key_dim + rope_dim], position part last, q_stride elements from row to row (a multiple of 8);
+ *   w    dev fp16 [latent_dim][n_heads][key_dim + value_dim]: w_k[h], then w_v[h], for head after head;
+ *   out  dev fp16 [n_rows][n_heads][value_dim]; q, w and out 16-byte aligned;
+ *   workspace  dev, >= the call's _workspace_bytes(), 256-byte aligned, contents scratch.
+ * Rows and pages must not alias out or the workspace.  n_rows == 0 is a no-op.
+ *
+ * kv_latent_attend_tokens takes the absorbed form, for few new rows: q[h] w_k[h]^T is rounded to fp16 and has to be in its range, the cache is
+ * read once for all heads, and the sum of weights times latents goes through w_v[h].
+ *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others' output is left as it
+ *            was).
+ * kv_latent_attend_prompts takes the expanded form, for any number of new rows: keys and values of all heads are made in the workspace, rounded
+ * to fp16 and to be in its range.
+ *   n_tokens 1 .. 67108864: at least as many as the sequences that have new rows have tokens together.  Where they have more, sequences from the
+ *            first on whose tokens do not fit in are left out: their rows' output is left as it was. */
+uint64_t kv_latent_attend_workspace_bytes(const kv_latent_shape_t* shape, int32_t n_seqs, int32_t max_rows);
+int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                                const void* q, int64_t q_stride, int32_t n_rows, const int32_t* row_start, int32_t max_rows,
+                                const void* w, void* workspace, uint64_t workspace_bytes, void* out, void* stream);
+uint64_t kv_latent_prompts_workspace_bytes(const kv_latent_shape_t* shape, int32_t n_seqs, int64_t n_tokens);
+int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_t* pages, int32_t layer,
+                                 const void* q, int64_t q_stride, int32_t n_rows, const int32_t* row_start, int64_t n_tokens,
+                                 const void* w, void* workspace, uint64_t workspace_bytes, void* out, void* stream);
+
 /* -------------------------------------------- host lifecycle (Sec. 3.4 ii) */
 
 /* LCTRU queue: concatenated sub-queues, one per bit-width, least compressed

@@ -103,6 +103,13 @@ _SIGNATURES = {
     "kv_attend_tokens": (_i32, [_vp, _vp, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _vp, _vp, _u64, _vp, _vp]),
     "kv_evict_workspace_bytes": (_u64, [_vp, _i32, _i32, _i32]),
     "kv_evict_tokens": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _u64, _vp, _vp, _vp]),
+    "kv_latent_record_bytes": (_u64, [_vp, _i32]),
+    "kv_latent_append_tokens": (_i32, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _vp, _vp]),
+    "kv_latent_read_tokens": (_i32, [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _i32, _vp, _vp]),
+    "kv_latent_attend_workspace_bytes": (_u64, [_vp, _i32, _i32]),
+    "kv_latent_attend_tokens": (_i32, [_vp, _vp, _i32, _vp, _i64, _i32, _vp, _i32, _vp, _vp, _u64, _vp, _vp]),
+    "kv_latent_prompts_workspace_bytes": (_u64, [_vp, _i32, _i64]),
+    "kv_latent_attend_prompts": (_i32, [_vp, _vp, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _vp, _u64, _vp, _vp]),
     "kv_lctru_create": (_vp, []),
     "kv_lctru_destroy": (None, [_vp]),
     "kv_lctru_insert": (_i32, [_vp, _i32, _i32, _i32, _u64, _u64]),
@@ -618,12 +625,10 @@ class kv_pages_t(ctypes.Structure):
                 ("n_seqs", _i32), ("stride", _i32)]
 
 
-class Pages:
-    """Paged sequences (kv_pages_t) of one shape: the record pool, the page tables off and bits [n_seqs][stride] and the
-    lengths [n_seqs].  Holds the tensors and the two C structures, so that a step marshals them once; what the tensors
-    hold may change from call to call, but not which tensors they are."""
+class _PagedSequences:
+    """What Pages and LatentPages share: the tensors of paged sequences and the C structures made of them."""
 
-    def __init__(self, shape: Shape, pool: torch.Tensor, off: torch.Tensor, bits: torch.Tensor, length: torch.Tensor):
+    def _hold(self, shape, pool, off, bits, length):
         if off.dim() != 2 or tuple(bits.shape) != tuple(off.shape) or tuple(length.shape) != (off.shape[0],):
             raise ValueError("off and bits must be [n_seqs][stride], length [n_seqs]")
         for t in (off, bits, length):
@@ -632,12 +637,10 @@ class Pages:
         self.shape, self.pool, self.off, self.bits, self.length = shape, pool, off, bits, length
         self.n_seqs = off.shape[0]
         self._index = pool.get_device()
-        self._book_shape = (self.n_seqs, shape.n_kv_heads, shape.n_tokens)
         self._shape = shape.c()
         self._c = kv_pages_t(_dev(pool), pool.numel() * pool.element_size(), _dev(off, torch.int64), _dev(bits, torch.uint8),
                              _dev(length, torch.int32), off.shape[0], off.shape[1])
         self._refs = ctypes.byref(self._shape), ctypes.byref(self._c)
-        self._fixed = True
 
     def __setattr__(self, name, value):
         if "_fixed" in self.__dict__:
@@ -662,9 +665,9 @@ class Pages:
         _dev(t, dtype)
         raise ValueError(f"{name} must be on cuda:{self._index}, got {t.device}")
 
-    def _rows(self, t, heads, name):
-        """Address and row stride of fp16 rows [n_rows][heads][head_dim], whose rows may lie apart."""
-        d, size, stride = self.shape.head_dim, t.shape, t.stride()
+    def _rows(self, t, heads, name, d):
+        """Address and row stride of fp16 rows [n_rows][heads][d], whose rows may lie apart."""
+        size, stride = t.shape, t.stride()
         if len(size) != 3 or size[1] != heads or size[2] != d:
             raise ValueError(f"{name} must be [n_rows][{heads}][{d}], got {list(size)}")
         if t.dtype is not torch.float16 or t.get_device() != self._index:
@@ -679,6 +682,17 @@ class Pages:
             raise ValueError(f"the workspace must be on cuda:{self._index}, got {t.device}")
         return _dev(t), t.numel() * t.element_size()
 
+
+class Pages(_PagedSequences):
+    """Paged sequences (kv_pages_t) of one shape: the record pool, the page tables off and bits [n_seqs][stride] and the
+    lengths [n_seqs].  Holds the tensors and the two C structures, so that a step marshals them once; what the tensors
+    hold may change from call to call, but not which tensors they are."""
+
+    def __init__(self, shape: Shape, pool: torch.Tensor, off: torch.Tensor, bits: torch.Tensor, length: torch.Tensor):
+        self._hold(shape, pool, off, bits, length)
+        self._book_shape = (self.n_seqs, shape.n_kv_heads, shape.n_tokens)
+        self._fixed = True
+
     def _book(self, t, dtype, name, layers=None):
         return self._arg(t, dtype, self._book_shape if layers is None else (layers,) + self._book_shape, name)
 
@@ -686,8 +700,8 @@ class Pages:
 def kv_append_tokens(pages: Pages, layer: int, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor = None,
                      seen: torch.Tensor = None, mass: torch.Tensor = None, pos: torch.Tensor = None, stream=None) -> None:
     heads = pages.shape.n_kv_heads
-    k_at, stride = pages._rows(k, heads, "k")
-    v_at, v_stride = pages._rows(v, heads, "v")
+    k_at, stride = pages._rows(k, heads, "k", pages.shape.head_dim)
+    v_at, v_stride = pages._rows(v, heads, "v", pages.shape.head_dim)
     if v.shape != k.shape or v_stride != stride:
         raise ValueError("k and v must have the same shape and row stride")
     n = pages.n_seqs
@@ -709,7 +723,7 @@ def kv_attend_workspace_bytes(shape: Shape, n_seqs: int, max_rows: int = 1, with
 def kv_attend_tokens(pages: Pages, layer: int, q: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor,
                      row_start: torch.Tensor = None, max_rows: int = 1, mass_in: torch.Tensor = None,
                      mass: torch.Tensor = None, stream=None) -> None:
-    q_at, stride = pages._rows(q, pages.shape.n_q_heads, "q")
+    q_at, stride = pages._rows(q, pages.shape.n_q_heads, "q", pages.shape.head_dim)
     _check(lib().kv_attend_tokens(*pages._refs, layer, q_at, stride, q.shape[0],
                                   pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"), max_rows,
                                   pages._book(mass_in, torch.float32, "mass_in"), pages._book(mass, torch.float32, "mass"),
@@ -736,6 +750,117 @@ def kv_evict_tokens(pages: Pages, layer_begin: int, layer_end: int, mass_in: tor
                                  *pages._space(workspace),
                                  pages._book(mass, torch.float32, "mass", layers), pages._book(pos, torch.int32, "pos", layers),
                                  pages._on_device(stream)))
+
+
+# ------------------------------------------------------------------ latent caches
+
+class kv_latent_shape_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("n_layers", "n_heads", "latent_dim", "rope_dim", "key_dim", "value_dim", "n_tokens", "chunk_tokens", "group",
+                 "format")]
+
+
+class LatentShape(NamedTuple):
+    n_layers: int
+    n_heads: int
+    latent_dim: int
+    rope_dim: int
+    key_dim: int
+    value_dim: int
+    n_tokens: int
+    chunk_tokens: int
+    group: int
+    format: int = 0      # KV_FMT_F16_GROUPS or KV_FMT_F16_GROUPS_H
+
+    @property
+    def n_chunks(self) -> int:
+        return self.n_tokens // self.chunk_tokens
+
+    def c(self) -> kv_latent_shape_t:
+        return kv_latent_shape_t(*self)
+
+
+def kv_latent_record_bytes(shape: LatentShape, bits: int) -> int:
+    s = shape.c()
+    n = int(lib().kv_latent_record_bytes(ctypes.byref(s), bits))
+    if n == 0:
+        raise KvError(KV_EINVAL, kv_last_error())
+    return n
+
+
+class LatentPages(_PagedSequences):
+    """Paged sequences of a latent cache, as Pages are of one with heads."""
+
+    def __init__(self, shape: LatentShape, pool: torch.Tensor, off: torch.Tensor, bits: torch.Tensor, length: torch.Tensor):
+        self._hold(shape, pool, off, bits, length)
+        self._fixed = True
+
+    def _flat(self, t, dim, name):
+        """Address and row stride of fp16 rows [n_rows][dim], whose rows may lie apart."""
+        size, stride = t.shape, t.stride()
+        if len(size) != 2 or size[1] != dim:
+            raise ValueError(f"{name} must be [n_rows][{dim}], got {list(size)}")
+        if t.dtype is not torch.float16 or t.get_device() != self._index:
+            raise TypeError(f"{name} must be torch.float16 on cuda:{self._index}, got {t.dtype} on {t.device}")
+        if stride[1] != 1:
+            raise TypeError(f"a row of {name} must be contiguous")
+        return t.data_ptr(), (stride[0] if size[0] > 1 else -(-dim // 8) * 8)
+
+    def _moved(self, c, r, row_start):
+        """What kv_latent_append_tokens and kv_latent_read_tokens take of the rows."""
+        if c.shape[0] != r.shape[0]:
+            raise ValueError(f"c has {c.shape[0]} rows, r has {r.shape[0]}")
+        return (*self._flat(c, self.shape.latent_dim, "c"), *self._flat(r, self.shape.rope_dim, "r"), c.shape[0],
+                self._arg(row_start, torch.int32, (self.n_seqs + 1,), "row_start"))
+
+    def _asked(self, q, w, out):
+        """Addresses of queries, weights and output, the rows' number and stride."""
+        s = self.shape
+        q_at, stride = self._rows(q, s.n_heads, "q", s.key_dim + s.rope_dim)
+        return (q_at, stride, q.shape[0], self._arg(w, torch.float16, (s.latent_dim, s.n_heads, s.key_dim + s.value_dim), "w"),
+                self._arg(out, torch.float16, (q.shape[0], s.n_heads, s.value_dim), "out"))
+
+
+def kv_latent_append_tokens(pages: LatentPages, layer: int, c: torch.Tensor, r: torch.Tensor, row_start: torch.Tensor = None,
+                            stream=None) -> None:
+    _check(lib().kv_latent_append_tokens(*pages._refs, layer, *pages._moved(c, r, row_start), pages._on_device(stream)))
+
+
+def kv_latent_read_tokens(pages: LatentPages, layer: int, c: torch.Tensor, r: torch.Tensor, row_start: torch.Tensor = None,
+                          stream=None) -> None:
+    _check(lib().kv_latent_read_tokens(*pages._refs, layer, *pages._moved(c, r, row_start), pages._on_device(stream)))
+
+
+def kv_latent_attend_workspace_bytes(shape: LatentShape, n_seqs: int, max_rows: int = 1) -> int:
+    s = shape.c()
+    n = int(lib().kv_latent_attend_workspace_bytes(ctypes.byref(s), n_seqs, max_rows))
+    if n == 0:
+        raise KvError(KV_EINVAL, kv_last_error())
+    return n
+
+
+def kv_latent_attend_tokens(pages: LatentPages, layer: int, q: torch.Tensor, w: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor,
+                            row_start: torch.Tensor = None, max_rows: int = 1, stream=None) -> None:
+    q_at, stride, n, w_at, out_at = pages._asked(q, w, out)
+    _check(lib().kv_latent_attend_tokens(*pages._refs, layer, q_at, stride, n,
+                                         pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"), max_rows, w_at,
+                                         *pages._space(workspace), out_at, pages._on_device(stream)))
+
+
+def kv_latent_prompts_workspace_bytes(shape: LatentShape, n_seqs: int, n_tokens: int) -> int:
+    s = shape.c()
+    n = int(lib().kv_latent_prompts_workspace_bytes(ctypes.byref(s), n_seqs, n_tokens))
+    if n == 0:
+        raise KvError(KV_EINVAL, kv_last_error())
+    return n
+
+
+def kv_latent_attend_prompts(pages: LatentPages, layer: int, q: torch.Tensor, w: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor,
+                             n_tokens: int, row_start: torch.Tensor = None, stream=None) -> None:
+    q_at, stride, n, w_at, out_at = pages._asked(q, w, out)
+    _check(lib().kv_latent_attend_prompts(*pages._refs, layer, q_at, stride, n,
+                                          pages._arg(row_start, torch.int32, (pages.n_seqs + 1,), "row_start"), n_tokens, w_at,
+                                          *pages._space(workspace), out_at, pages._on_device(stream)))
 
 
 # ------------------------------------------------------------------ host lifecycle

@@ -5,7 +5,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kv_internal.h"
+#include "kv_decode_checks.hpp"
 #include "kv_launch_rules.hpp"
 #include "kv_append_kernels.hpp"
 #include "kv_attend_kernels.hpp"
@@ -14,16 +14,6 @@
 using namespace kvs;
 
 namespace {
-
-int hip_fail(hipError_t e, const char* what) { return fail(KV_EHIP, "%s: %s", what, hipGetErrorString(e)); }
-
-int launch_status(const char* what) {
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? KV_OK : hip_fail(e, what);
-}
-
-// Workgroups that one launch may have: a grid has less than 2^32 threads.
-constexpr int64_t most_groups(int threads) { return 0xffffffffLL / threads; }
 
 int check_paged_shape(const kv_shape_t* shape) {
     if (int rc = check_shape(shape)) return rc;
@@ -35,36 +25,13 @@ int check_paged_shape(const kv_shape_t* shape) {
     return KV_OK;
 }
 
-int check_seqs(int32_t n_seqs) {
-    return n_seqs < 1 || n_seqs > 65535 ? fail(KV_EINVAL, "n_seqs %d outside [1, 65535]", n_seqs) : KV_OK;
-}
-
 int check_pages(const kv_shape_t* shape, const kv_pages_t* pages) {
     if (int rc = check_paged_shape(shape)) return rc;
-    if (!pages) return fail(KV_EINVAL, "pages is NULL");
-    if (int rc = check_seqs(pages->n_seqs)) return rc;
-    if (!pages->pool || !pages->off || !pages->bits || !pages->len) return fail(KV_EINVAL, "NULL device pointer in pages");
-    if (!aligned(pages->pool, 16) || !aligned(pages->off, 8) || !aligned(pages->len, 4))
-        return fail(KV_EINVAL, "pages: pool must be 16-byte aligned, off 8-byte, len 4-byte aligned");
-    if (pages->stride < shape->n_tokens / shape->chunk_tokens)
-        return fail(KV_EINVAL, "pages: stride %d is less than the %d pages of a sequence", pages->stride,
-                    shape->n_tokens / shape->chunk_tokens);
-    return KV_OK;
+    return check_page_table(pages, shape->n_tokens / shape->chunk_tokens);
 }
 
 int check_layer(const kv_shape_t* shape, int32_t layer) {
     return layer < 0 || layer >= shape->n_layers ? fail(KV_EINVAL, "layer %d outside [0,%d)", layer, shape->n_layers) : KV_OK;
-}
-
-// The rows of a step: their number, their list, and the elements from one to the next.
-int check_rows(const kv_pages_t* pages, int32_t n_rows, const int32_t* row_start, int64_t stride, int64_t least) {
-    if (n_rows < 0) return fail(KV_EINVAL, "n_rows %d is negative", n_rows);
-    if (!row_start && n_rows != pages->n_seqs)
-        return fail(KV_EINVAL, "without row_start n_rows (%d) must be n_seqs (%d)", n_rows, pages->n_seqs);
-    if (!aligned(row_start, 4)) return fail(KV_EINVAL, "row_start must be 4-byte aligned");
-    if (stride < least || stride % 8) return fail(KV_EINVAL, "row stride %lld is less than %lld or no multiple of 8",
-                                                  static_cast<long long>(stride), static_cast<long long>(least));
-    return KV_OK;
 }
 
 PagesView pages_view(const kv_shape_t& s, const kv_pages_t& p) {
@@ -88,12 +55,6 @@ PagesView pages_view(const kv_shape_t& s, const kv_pages_t& p) {
     v.bit_bytes = record_bytes(s, 16) / 16;
     v.param_bytes = record_bytes(s, 2) - 2 * v.bit_bytes;
     return v;
-}
-
-int log2_of(int v) {
-    int l = 0;
-    while ((1 << l) < v) ++l;
-    return l;
 }
 
 // Launches K<head_dim, ...>.

@@ -61,6 +61,30 @@ int check_shape(const kv_shape_t* s) {
     return KV_OK;
 }
 
+int check_latent_shape(const kv_latent_shape_t* s) {
+    if (!s) return fail(KV_EINVAL, "shape is NULL");
+    if (s->n_layers <= 0 || s->n_heads <= 0 || s->n_tokens <= 0 || s->chunk_tokens <= 0)
+        return fail(KV_ESHAPE, "every shape field must be positive");
+    if (s->n_heads > 1024) return fail(KV_ESHAPE, "n_heads %d exceeds 1024", s->n_heads);
+    if (s->latent_dim != 256 && s->latent_dim != 512) return fail(KV_ESHAPE, "latent_dim %d not in {256,512}", s->latent_dim);
+    if (s->rope_dim != 32 && s->rope_dim != 64) return fail(KV_ESHAPE, "rope_dim %d not in {32,64}", s->rope_dim);
+    if ((s->key_dim != 64 && s->key_dim != 128) || (s->value_dim != 64 && s->value_dim != 128))
+        return fail(KV_ESHAPE, "key_dim %d and value_dim %d must be 64 or 128", s->key_dim, s->value_dim);
+    if (s->group != 64 && s->group != 128 && s->group != 256 && s->group != 512)
+        return fail(KV_ESHAPE, "group %d not in {64,128,256,512}", s->group);
+    if (s->latent_dim % s->group) return fail(KV_ESHAPE, "latent_dim %d is not a multiple of group %d", s->latent_dim, s->group);
+    if (s->format != KV_FMT_F16_GROUPS && s->format != KV_FMT_F16_GROUPS_H)
+        return fail(KV_ESHAPE, "latent caches need an fp16 cache format, got %d", s->format);
+    if (s->chunk_tokens % 16 || s->chunk_tokens > 1024)
+        return fail(KV_ESHAPE, "latent caches need chunk_tokens %% 16 == 0, at most 1024, got %d", s->chunk_tokens);
+    if (s->n_tokens % s->chunk_tokens)
+        return fail(KV_ESHAPE, "n_tokens %d is not a multiple of chunk_tokens %d", s->n_tokens, s->chunk_tokens);
+    if (s->n_tokens > (1 << 24)) return fail(KV_ESHAPE, "n_tokens %d exceeds 16777216", s->n_tokens);
+    if (static_cast<int64_t>(s->n_layers) * s->chunk_tokens > (1 << 24))
+        return fail(KV_ESHAPE, "n_layers * chunk_tokens exceeds 16777216");
+    return KV_OK;
+}
+
 }  // namespace kvs
 
 using namespace kvs;
@@ -76,6 +100,15 @@ uint64_t kv_record_bytes(const kv_shape_t* shape, int32_t bits) {
         return 0;
     }
     return record_bytes(*shape, bits);
+}
+
+uint64_t kv_latent_record_bytes(const kv_latent_shape_t* shape, int32_t bits) {
+    if (check_latent_shape(shape) != KV_OK) return 0;
+    if (bits != 16 && bits != 8 && bits != 4 && bits != 2) {
+        fail(KV_EBITS, "bits %d not in {16,8,4,2}", bits);
+        return 0;
+    }
+    return latent_record_bytes(*shape, bits);
 }
 
 int32_t kv_chunk_offsets(const kv_shape_t* shape, const uint8_t* bits, uint64_t* off) {

@@ -52,6 +52,19 @@ inline uint64_t record_bytes(const kv_shape_t& s, int bits) {
                    meta * static_cast<uint64_t>(s.head_dim / s.group));
 }
 
+// Latent caches: KV_OK, or KV_EINVAL / KV_ESHAPE with the error text set; bytes of one page's record (both already validated).
+int check_latent_shape(const kv_latent_shape_t* s);
+inline uint64_t latent_param_bytes(const kv_latent_shape_t& s) {
+    return static_cast<uint64_t>(s.n_layers) * s.chunk_tokens * (s.latent_dim / s.group) * (s.format == KV_FMT_F16_GROUPS_H ? 4u : 8u);
+}
+inline uint64_t latent_record_bytes(const kv_latent_shape_t& s, int bits) {
+    const uint64_t rows = static_cast<uint64_t>(s.n_layers) * s.chunk_tokens;
+    return rows * (static_cast<uint64_t>(s.latent_dim) * bits / 8u + 2u * s.rope_dim) + (bits == 16 ? 0 : latent_param_bytes(s));
+}
+
+// C[M][N] = A[M][K] * B[K][N] in fp16 on the library's own product (M rows of A in fragment order, M a multiple of 32), enqueued on `stream`.
+int own_product(void* stream, int64_t M, int64_t N, int64_t K, const void* A, const void* B, void* C, const char* what);
+
 inline bool aligned(const void* p, uintptr_t a) {
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }

@@ -1,0 +1,286 @@
+// Latent attention in the expanded form, for many new rows at once: keys and values of every head are made from the latents,
+//     k[h] = (c w_k[h], r),   v[h] = c w_v[h],
+// by one product over all tokens (kv_gemm_kernels.hpp), and the new rows attend to them, 2 H (Dk + Dr + Dv) operations a (row, token).
+//
+// Room for the tokens: each sequence that has new rows gets whole tiles of 32 tokens, one sequence after the other, as far as the room
+// reaches; a sequence that does not fit in gets none, and its rows are not computed.
+#pragma once
+
+#include "kv_latent_attend_kernels.hpp"
+
+namespace kvs {
+
+typedef float lf16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kPromptRows = 128;          // query rows of a workgroup
+
+struct PromptGeom {
+    int32_t n_rows, H;
+    int32_t cap_tiles;                    // tiles of 32 tokens that there is room for
+    int32_t row_tiles;                    // row tiles of the grid
+    int64_t q_stride;
+    float scale_log2e;
+};
+
+// What the first kernel leaves: where each sequence's token tiles and row tiles end.
+struct PromptTable {
+    int32_t* tile_end;                    // [n_seqs]
+    int32_t* row_end;                     // [n_seqs]
+};
+
+__global__ __launch_bounds__(64) void latent_table_kernel(LatentView v, PromptGeom g, const int32_t* __restrict__ row_start, PromptTable t) {
+    const int lane = threadIdx.x;
+    int tiles = 0, row_tiles = 0;
+    for (int s0 = 0; s0 < v.p.n_seqs; s0 += 64) {
+        const int s = s0 + lane;
+        SeqRows rows = {0, 0};
+        int units = 0;
+        if (s < v.p.n_seqs) {
+            rows = seq_rows(row_start, s, g.n_rows);
+            units = rows.count ? (seq_len(v.p, s) + kLatentTile - 1) / kLatentTile : 0;
+        }
+        // (in order: what does not fit in leaves its room to nobody)
+        const int end = tiles + latent_prefix_sum(units);
+        const bool fits = end <= g.cap_tiles;
+        const int row_to = row_tiles + latent_prefix_sum(fits ? (rows.count + kPromptRows - 1) / kPromptRows : 0);
+        if (s < v.p.n_seqs) {
+            t.tile_end[s] = min(end, g.cap_tiles);
+            t.row_end[s] = row_to;
+        }
+        tiles = min(__builtin_amdgcn_readlane(end, 63), g.cap_tiles + 1);
+        row_tiles = __builtin_amdgcn_readlane(row_to, 63);
+    }
+}
+
+// The first s with end[s] > x (ascending), -1 if there is none (wave-uniform).
+__device__ __forceinline__ int first_behind(const int32_t* __restrict__ end, int n_seqs, int x, int lane) {
+    int lo = 0, n = n_seqs;
+    while (n > 64) {
+        const int step = (n + 63) >> 6, i = min(lane * step + step - 1, n - 1);
+        const int cnt = __builtin_popcountll(__ballot(lane * step < n && end[lo + i] <= x));
+        lo += min(cnt * step, n);
+        n = min(step, n - min(cnt * step, n));
+    }
+    if (n <= 0) return -1;
+    const uint64_t any = __ballot(lane < n && end[lo + min(lane, n - 1)] > x);
+    return any ? lo + __builtin_ctzll(any) : -1;
+}
+
+// A tile of 32 tokens from their pages: latents in the product's fragment order, position parts row-major, whether each half's page is
+// there; tokens that are not there are zeros.
+template <int DC, int DR>
+__global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, PromptGeom g, PromptTable t, int32_t lpg_log2, _Float16* __restrict__ latents,
+                                                            _Float16* __restrict__ ropes, uint8_t* __restrict__ there) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int tile = static_cast<int>(blockIdx.x);
+    const int s = __builtin_amdgcn_readfirstlane(first_behind(t.tile_end, v.p.n_seqs, tile, lane));
+    if (s < 0) return;
+    const int base = s ? t.tile_end[s - 1] : 0, n = seq_len(v.p, s);
+    const int token0 = (tile - base) * kLatentTile + (wave >> 1) * 16;      // of this wavefront's half
+    const int page = min(token0, v.p.N - 1) / v.p.T;
+    const int64_t entry = static_cast<int64_t>(s) * v.p.stride + page;
+    const uint64_t off = v.p.off[entry];
+    const int b = v.p.bits[entry];
+    const bool have = token0 < n && latent_present(v, off, b);
+    if (threadIdx.x % 128 == 0) there[tile * 2 + (wave >> 1)] = have ? 1 : 0;
+    // a lane has one token and every eighth piece, so that sixteen tokens' pieces are written side by side
+    const int tk = (wave >> 1) * 16 + (lane & 15), token = token0 + (lane & 15);
+    const bool ok = have && token < n;
+    const uint8_t* record = v.p.pool + (have ? off : 0);
+    const int in_page = token - page * v.p.T;
+    const SlabAt slab = slab_at<DC>(v.p, b, v.layer);
+    u4_t* to = reinterpret_cast<u4_t*>(latents) + static_cast<int64_t>(tile) * (kLatentTile * DC / 8);
+    const int first = (wave & 1) * 4 + (lane >> 4);
+#pragma unroll 4
+    for (int p = first; p < DC / 8; p += 8) {
+        u4_t x = {0u, 0u, 0u, 0u};
+        if (ok) x = read_piece<DC>(v, record, slab, b, in_page * (DC / 8) + p, lpg_log2);
+        to[p * kLatentTile + tk] = x;
+    }
+    if (first < DR / 8) {
+        u4_t x = {0u, 0u, 0u, 0u};
+        if (ok) x = reinterpret_cast<const u4_t*>(record + rope_at(v, b))[in_page * (DR / 8) + first];
+        reinterpret_cast<u4_t*>(ropes)[(static_cast<int64_t>(tile) * kLatentTile + tk) * (DR / 8) + first] = x;
+    }
+}
+
+// Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them.
+template <int DK, int DR, int DV>
+__global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, PromptGeom g, PromptTable t, const int32_t* __restrict__ row_start,
+                                                               const _Float16* __restrict__ q, const _Float16* __restrict__ kv,
+                                                               const _Float16* __restrict__ ropes, const uint8_t* __restrict__ there,
+                                                               _Float16* __restrict__ out) {
+    constexpr int kRopeAt = kLatentTile * DK * 2, kValueAt = kRopeAt + kLatentTile * DR * 2, kTileBytes = kValueAt + kLatentTile * DV * 2;
+    constexpr int KS = DK / 16, KR = DR / 16, VB = DV / 32, kBufs = 3;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kBufs * kTileBytes];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    // workgroups are dealt to the eight XCDs in turn: those of a head go to one of them, whose L2 then holds its keys and values
+    int h, rt;
+    if (g.H % 8 == 0) {
+        const int id = static_cast<int>(blockIdx.x) >> 3;
+        h = id / g.row_tiles * 8 + (static_cast<int>(blockIdx.x) & 7);
+        rt = g.row_tiles - 1 - id % g.row_tiles;
+    } else {
+        h = static_cast<int>(blockIdx.x) / g.row_tiles;
+        rt = g.row_tiles - 1 - static_cast<int>(blockIdx.x) % g.row_tiles;
+    }
+    const int s = __builtin_amdgcn_readfirstlane(first_behind(t.row_end, v.p.n_seqs, rt, lane));
+    if (s < 0) return;
+    const int rt_in = rt - (s ? t.row_end[s - 1] : 0), base = s ? t.tile_end[s - 1] : 0;
+    const int n = seq_len(v.p, s);
+    const SeqRows rows = seq_rows(row_start, s, g.n_rows);
+    const int row0 = rt_in * kPromptRows, m = row0 + wave * 32 + l32;
+    const bool ok = m < rows.count;
+    const int behind = n - rows.count;                                     // the token of row 0
+    const int pos = ok ? behind + m : -1;
+    const int min_pos = behind + row0 + wave * 32, max_pos = behind + min(row0 + wave * 32 + 31, rows.count - 1);
+    const int end_pos = behind + min(row0 + kPromptRows, rows.count) - 1;  // of the workgroup's last row
+    const int n_tiles = end_pos < 0 ? 0 : end_pos / kLatentTile + 1;
+    h8_t qf[KS + KR];
+    {
+        const _Float16* from = q + (rows.first + (ok ? m : 0)) * g.q_stride + h * (DK + DR) + 8 * half;
+#pragma unroll
+        for (int k = 0; k < KS + KR; ++k) qf[k] = *reinterpret_cast<const h8_t*>(from + 16 * k);
+    }
+    const int64_t kv_row = static_cast<int64_t>(g.H) * (DK + DV) * 2;
+    const uint8_t* keys = reinterpret_cast<const uint8_t*>(kv) + static_cast<int64_t>(base) * kLatentTile * kv_row + h * ((DK + DV) * 2);
+    const uint8_t* rope = reinterpret_cast<const uint8_t*>(ropes) + static_cast<int64_t>(base) * kLatentTile * (DR * 2);
+    const uint8_t* have = there + base * 2;
+    auto swz = [](int token, int pieces) __attribute__((always_inline)) {
+        return pieces == 4 ? (token >> 1) & 3 : latent_swizzle(token) & (pieces - 1);
+    };
+    constexpr int kLoads = (DK + DV) / 64 + 1;                             // of a wavefront for a tile
+    auto fetch = [&](int tile, int buf) __attribute__((always_inline)) {
+        uint8_t* to = lds + buf * kTileBytes;
+        const uint8_t* from = keys + static_cast<int64_t>(tile) * kLatentTile * kv_row;
+        constexpr int kk = DK / 8, kv_ = DV / 8, kr = DR / 8;
+#pragma unroll
+        for (int i = 0; i < DK / 64; ++i) {
+            const int p = (i * 4 + wave) * 64 + lane, tk = p / kk, slot = p % kk;
+            to_lds(from, static_cast<uint32_t>(tk * kv_row + ((slot ^ swz(tk, kk)) << 4)), to + (i * 4 + wave) * 1024);
+        }
+        {
+            const int i = DR == 64 ? wave : wave & 1, p = i * 64 + lane, tk = p / kr, slot = p % kr;
+            to_lds(rope + static_cast<int64_t>(tile) * (kLatentTile * DR * 2), static_cast<uint32_t>(tk * (DR * 2) + ((slot ^ swz(tk, kr)) << 4)), to + kRopeAt + i * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < DV / 64; ++i) {
+            const int p = (i * 4 + wave) * 64 + lane, tk = p / kv_, slot = p % kv_;
+            to_lds(from, static_cast<uint32_t>(tk * kv_row + DK * 2 + ((slot ^ swz(tk, kv_)) << 4)), to + kValueAt + (i * 4 + wave) * 1024);
+        }
+    };
+    lf16_t o[VB];
+#pragma unroll
+    for (int b = 0; b < VB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
+    float ref = -INFINITY, sum = 0.0f;
+    if (n_tiles > 0) {
+        fetch(0, 0);
+        fetch(min(1, n_tiles - 1), 1);
+    }
+    int buf = 0;
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        const bool have0 = have[2 * tile] != 0, have1 = have[2 * tile + 1] != 0;
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+        const int next2 = buf == 0 ? 2 : buf - 1;
+        fetch(min(tile + 2, n_tiles - 1), next2);
+        const uint8_t* at = lds + buf * kTileBytes;
+        buf = buf == 2 ? 0 : buf + 1;
+        const int token0 = tile * kLatentTile;
+        if (token0 > max_pos) continue;                                    // (uniform; behind all of this wavefront's rows)
+        lf16_t sc;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KS + KR; ++k) {
+            const uint8_t* p = k < KS ? at + l32 * (DK * 2) + (((2 * k + half) ^ swz(l32, DK / 8)) << 4)
+                                      : at + kRopeAt + l32 * (DR * 2) + (((2 * (k - KS) + half) ^ swz(l32, DR / 8)) << 4);
+            sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc, 0, 0, 0);
+        }
+        // sc[e]: token 8 (e / 4) + 4 half + e % 4 against this lane's row
+        const bool edge = token0 + kLatentTile - 1 > min_pos;
+        uint32_t bad = 0u;
+        if (edge) {
+            // Values that are not finite must not reach rows that do not see their token, whose probability of 0 does not hold them off: they
+            // are left out below, and rows that see them are NaN.
+            bool found = false;
+#pragma unroll 1
+            for (int p = half; p < DV / 8; p += 2) {
+                const u4_t y = *reinterpret_cast<const u4_t*>(at + kValueAt + l32 * (DV * 2) + (p << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) found |= (y[e] & 0x7c00u) == 0x7c00u || (y[e] & 0x7c000000u) == 0x7c000000u;
+            }
+            const uint64_t any = __ballot(found);
+            bad = static_cast<uint32_t>(any) | static_cast<uint32_t>(any >> 32);
+        }
+        if (edge || !have0 || !have1) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int tk = 8 * (e / 4) + 4 * half + e % 4;
+                if (bad >> tk & 1) sc[e] = NAN;
+                if (!(e < 8 ? have0 : have1) || token0 + tk > pos) sc[e] = -INFINITY;
+            }
+        }
+        float m_tile = sc[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) m_tile = fmaxf(m_tile, sc[e]);
+        m_tile *= g.scale_log2e;
+        if (__any(m_tile > ref + kLatentSlack)) {
+            const float m = xhalf_max(m_tile);
+            const float to = m > ref + kLatentSlack ? m - kLatentTop : ref;
+            const float alpha = to == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
+            sum *= alpha;
+#pragma unroll
+            for (int b = 0; b < VB; ++b) o[b] *= alpha;
+        }
+        const float r = ref == -INFINITY ? 0.0f : ref;
+        h8_t p[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], g.scale_log2e, -r));
+            sum += x;
+            p[e / 8][e % 8] = static_cast<_Float16>(x);
+        }
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const int tk = 16 * st + 4 * half + ((lane & 15) >> 2), piece = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+                const uint8_t* lo_at = at + kValueAt + tk * (DV * 2) + ((piece ^ swz(tk, DV / 8)) << 4) + (lane & 1) * 8;
+                const uint8_t* hi_at = at + kValueAt + (tk + 8) * (DV * 2) + ((piece ^ swz(tk + 8, DV / 8)) << 4) + (lane & 1) * 8;
+                const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(lo_at));
+                const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(hi_at));
+                const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
+                h8_t vf = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+                if (bad) {                                                 // (uniform)
+                    u4_t y = __builtin_bit_cast(u4_t, vf);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
+                        if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
+                    }
+                    vf = __builtin_bit_cast(h8_t, y);
+                }
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[st], o[b], 0, 0, 0);
+            }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                       // (LDS is not left while it is written to)
+    if (ok) {
+        const float all = xhalf_sum(sum), inv = all > 0.0f ? 1.0f / all : all;     // a row that sees nothing: zeros; NaN stays
+        _Float16* to = out + (static_cast<int64_t>(rows.first + m) * g.H + h) * DV;
+#pragma unroll
+        for (int b = 0; b < VB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lh4_t x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(o[b][4 * j + e] * inv);
+                *reinterpret_cast<lh4_t*>(to + 32 * b + 8 * j + 4 * half) = x;
+            }
+    }
+}
+
+}  // namespace kvs
