@@ -672,7 +672,7 @@ int32_t kv_evict_tokens(const kv_shape_t* shape, const kv_pages_t* pages, int32_
  * with codes, scale and mn of a token's groups as in formats 0 and 3: positions hang on r and it is a ninth of a row, so it is not packed.
  * Requirements (else KV_ESHAPE): latent_dim in {256, 512}, rope_dim in {32, 64}, key_dim and value_dim in {64, 128}, 1 <= n_heads <= 1024, group
  * in {64, 128, 256, 512} dividing latent_dim, format 0 or 3, chunk_tokens % 16 == 0 and <= 1024, n_tokens (the most of a sequence) a multiple
- * of chunk_tokens and at most 16777216, n_layers * chunk_tokens <= 16777216.
+ * of chunk_tokens and at most 16777216, n_layers * chunk_tokens <= 1048576.
  * With kv_latent_read_tokens and kv_latent_append_tokens through a second table a page changes its width: its rows are read and appended
  * to a page of the other. */
 typedef struct {

@@ -80,8 +80,8 @@ int check_latent_shape(const kv_latent_shape_t* s) {
     if (s->n_tokens % s->chunk_tokens)
         return fail(KV_ESHAPE, "n_tokens %d is not a multiple of chunk_tokens %d", s->n_tokens, s->chunk_tokens);
     if (s->n_tokens > (1 << 24)) return fail(KV_ESHAPE, "n_tokens %d exceeds 16777216", s->n_tokens);
-    if (static_cast<int64_t>(s->n_layers) * s->chunk_tokens > (1 << 24))
-        return fail(KV_ESHAPE, "n_layers * chunk_tokens exceeds 16777216");
+    if (static_cast<int64_t>(s->n_layers) * s->chunk_tokens > (1 << 20))
+        return fail(KV_ESHAPE, "n_layers * chunk_tokens exceeds 1048576");
     return KV_OK;
 }
 

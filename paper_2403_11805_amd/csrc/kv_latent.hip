@@ -60,7 +60,7 @@ int check_moved_rows(const kv_latent_shape_t* shape, const kv_pages_t* pages, in
 
 double latent_scale(const kv_latent_shape_t& s) { return 1.4426950408889634 / std::sqrt(static_cast<double>(s.key_dim + s.rope_dim)); }
 
-int32_t tile_rows_log2(int64_t rows) { return rows <= 16 ? 4 : rows <= 32 ? 5 : 6; }
+int32_t tile_rows_log2(int64_t rows) { return rows <= 16 ? 4 : rows <= 32 ? 5 : rows <= 64 ? 6 : 7; }
 
 LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_rows) {
     LatentGeom g = {};
@@ -71,20 +71,22 @@ LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_r
     g.Dv = s.value_dim;
     g.tile_log2 = tile_rows_log2(rows);
     g.row_tiles = static_cast<int32_t>((rows + (1 << g.tile_log2) - 1) >> g.tile_log2);
-    const int64_t units = static_cast<int64_t>(n_seqs) * g.row_tiles * ((s.n_tokens + kLatentTile - 1) / kLatentTile);
-    g.groups = static_cast<int32_t>(std::min<int64_t>(512, units));
+    const int64_t pairs = static_cast<int64_t>(n_seqs) * g.row_tiles, units = pairs * ((s.n_tokens + kLatentTile - 1) / kLatentTile);
+    g.groups = static_cast<int32_t>(std::min<int64_t>(256, units + pairs * kLatentCost));
     g.scale_log2e = static_cast<float>(latent_scale(s));
     return g;
 }
 
 struct LatentSpace {
-    uint64_t qa, part_o, part_ml, line, zeros, all;      // byte offsets and the size of the workspace
+    uint64_t qa, joined, part_o, part_ml, line, zeros, all;      // byte offsets and the size of the workspace
 };
 LatentSpace latent_space(const kv_latent_shape_t& s, int32_t n_seqs, const LatentGeom& g) {
     const uint64_t rows = (g.groups + static_cast<uint64_t>(n_seqs) * g.row_tiles) << g.tile_log2;
     LatentSpace w;
     w.qa = 0;
-    w.part_o = w.qa + up256(static_cast<uint64_t>(n_seqs) * g.max_rows * s.n_heads * s.latent_dim * 2);
+    const uint64_t latents = static_cast<uint64_t>(n_seqs) * g.max_rows * s.n_heads * s.latent_dim * 2;
+    w.joined = w.qa + up256(latents);
+    w.part_o = w.joined + up256(2 * latents);
     w.part_ml = w.part_o + up256(rows * s.latent_dim * 4);
     w.line = w.part_ml + up256(rows * 8);
     w.zeros = w.line + up256((4 + static_cast<uint64_t>(n_seqs)) * 4);
@@ -97,7 +99,7 @@ int check_latent_attend(const kv_latent_shape_t* shape, int32_t n_seqs, int32_t 
     if (max_rows < 1 || max_rows > 16) return fail(KV_EINVAL, "max_rows %d outside [1,16]", max_rows);
     const int64_t rows = static_cast<int64_t>(shape->n_heads) * max_rows, tile = 1 << tile_rows_log2(rows);
     const int64_t pairs = n_seqs * ((rows + tile - 1) / tile), units = (shape->n_tokens + kLatentTile - 1) / kLatentTile;
-    if (pairs * (units + kPieceCost + 1) > 0x7fffffffLL / 2 ||
+    if (pairs * (units + kLatentCost + 1) > 0x7fffffffLL / 2 ||
         static_cast<int64_t>(n_seqs) * max_rows * (shape->n_heads * (shape->latent_dim / 128) + 1) > most_groups(256))
         return fail(KV_ESHAPE, "n_seqs * n_heads * n_tokens too large for one call");
     return KV_OK;
@@ -226,13 +228,14 @@ int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t
 #undef KV_LAUNCH
     if (int rc = launch_status("latent_absorb_kernel launch")) return rc;
     const dim3 attend(static_cast<uint32_t>(g.groups));
-#define KV_LAUNCH(D, R, M) \
-    hipLaunchKernelGGL((latent_attend_kernel<D, R, M>), attend, dim3(256), 0, st, view, g, qa, q16, row_start, line, zeros, lpg, part_o, part_ml)
+    const LatentAttendArgs args = {view, g, qa, q16, row_start, line, zeros, part_o, part_ml, lpg};
+#define KV_LAUNCH(D, R, M) hipLaunchKernelGGL((latent_attend_kernel<D, R, M>), attend, dim3(64 * kLatentWaves), 0, st, args)
 #define KV_BY_ROWS(D, R)                        \
     do {                                        \
         if (g.tile_log2 == 4) KV_LAUNCH(D, R, 16);      \
         else if (g.tile_log2 == 5) KV_LAUNCH(D, R, 32); \
-        else KV_LAUNCH(D, R, 64);               \
+        else if (g.tile_log2 == 6) KV_LAUNCH(D, R, 64); \
+        else KV_LAUNCH(D, R, 128);              \
     } while (0)
     if (dc == 512) {
         if (shape->rope_dim == 64) KV_BY_ROWS(512, 64);
@@ -244,26 +247,33 @@ int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t
 #undef KV_BY_ROWS
 #undef KV_LAUNCH
     if (int rc = launch_status("latent_attend_kernel launch")) return rc;
-    const int per = all_rows > 16 ? 16 : 4;
-    const dim3 project(static_cast<uint32_t>(shape->n_heads), static_cast<uint32_t>((all_rows + per - 1) / per));
-    const uint32_t lds = static_cast<uint32_t>(g.groups) * 16;
-#define KV_LAUNCH(D, V, ROWS) \
-    hipLaunchKernelGGL((latent_project_kernel<D, V, ROWS>), project, dim3(256), lds, st, view, g, w16, row_start, line, part_o, part_ml, static_cast<_Float16*>(out))
-#define KV_BY_DIMS(ROWS)                                             \
-    do {                                                             \
-        if (dc == 512) {                                             \
-            if (shape->value_dim == 128) KV_LAUNCH(512, 128, ROWS);  \
-            else KV_LAUNCH(512, 64, ROWS);                           \
-        } else {                                                     \
-            if (shape->value_dim == 128) KV_LAUNCH(256, 128, ROWS);  \
-            else KV_LAUNCH(256, 64, ROWS);                           \
-        }                                                            \
-    } while (0)
-    if (per == 16) KV_BY_DIMS(16);
-    else KV_BY_DIMS(4);
-#undef KV_BY_DIMS
+    const int64_t heads_rows = static_cast<int64_t>(all_rows) * shape->n_heads;
+    _Float16 *hi = reinterpret_cast<_Float16*>(space + sp.joined), *lo = hi + heads_rows * dc;
+    const uint32_t lds = static_cast<uint32_t>(g.groups) * 4;
+#define KV_LAUNCH(D, PER)                                                                                                              \
+    hipLaunchKernelGGL((latent_join_kernel<D, PER>), dim3(static_cast<uint32_t>((heads_rows * PER + 3) / 4)), dim3(256), lds * (4 / PER), st, \
+                       view, g, row_start, line, part_o, part_ml, hi, lo)
+    if (join_shares_rows(heads_rows)) {
+        if (dc == 512) KV_LAUNCH(512, 4);
+        else KV_LAUNCH(256, 4);
+    } else {
+        if (dc == 512) KV_LAUNCH(512, 1);
+        else KV_LAUNCH(256, 1);
+    }
 #undef KV_LAUNCH
-    return launch_status("latent_project_kernel launch");
+    if (int rc = launch_status("latent_join_kernel launch")) return rc;
+    const dim3 values(static_cast<uint32_t>(shape->n_heads * (shape->value_dim / 64)), static_cast<uint32_t>((all_rows + 15) / 16));
+#define KV_LAUNCH(D, V) \
+    hipLaunchKernelGGL((latent_values_kernel<D, V>), values, dim3(256), 0, st, view, g, w16, row_start, hi, lo, static_cast<_Float16*>(out))
+    if (dc == 512) {
+        if (shape->value_dim == 128) KV_LAUNCH(512, 128);
+        else KV_LAUNCH(512, 64);
+    } else {
+        if (shape->value_dim == 128) KV_LAUNCH(256, 128);
+        else KV_LAUNCH(256, 64);
+    }
+#undef KV_LAUNCH
+    return launch_status("latent_values_kernel launch");
 }
 
 uint64_t kv_latent_prompts_workspace_bytes(const kv_latent_shape_t* shape, int32_t n_seqs, int64_t n_tokens) {

@@ -1,9 +1,9 @@
 // Latent attention in the absorbed form: queries are taken to the latents' space, where one row a token is key and value of all heads,
 //     q'[h] = w_k[h] q[h],   s = (q'[h] c + q_r[h] r) / sqrt(Dk + Dr),   out[h] = w_v[h]^T (softmax(s) c),
 // so that a token's row is read once for all heads and the wide products are those with the cache, 2 H (2 DC + Dr) operations a (query
-// row, token), instead of the 2 DC H (Dk + Dv) a token that making its keys and values takes.  Three launches: latent_absorb_kernel (q' of
-// the new rows, and how the work is divided), latent_attend_kernel (shares of the attention), latent_project_kernel (the shares joined,
-// the values made).
+// row, token), instead of the 2 DC H (Dk + Dv) a token that making its keys and values takes.  Four launches: latent_absorb_kernel (q' of
+// the new rows, and how the work is divided), latent_attend_kernel (shares of the attention), latent_join_kernel (the shares joined) and
+// latent_values_kernel.
 #pragma once
 
 #include "kv_lane_ops.hpp"
@@ -19,6 +19,7 @@ typedef short ls4_t __attribute__((ext_vector_type(4)));
 constexpr int kLatentTile = 32;            // tokens of a tile
 constexpr float kLatentTop = 7.0f;         // a row's reference is set 2^7 below its largest logit so far ...
 constexpr float kLatentSlack = 15.0f;      // ... and moves when a logit passes 2^15 above it: probabilities stay in fp16's range
+constexpr int kLatentWaves = 8;             // wavefronts of an attention workgroup
 constexpr int kZeroBytes = 2048;           // of zeros, which stand for rows that are not there
 
 struct LatentGeom {
@@ -31,11 +32,10 @@ struct LatentGeom {
     float scale_log2e;                     // log2(e) / sqrt(Dk + Dr)
 };
 
-// Where the work lies in a line of places, tile by tile, row tile by row tile, sequence by sequence: the places in front of a row tile
-// and of a workgroup's run, then where each sequence's work ends.
-struct LatentLine {
-    int32_t round, cost, run, unused;
-};
+// How the work is divided.  The token tiles of all sequences and row tiles stand in one line, row tile by row tile, sequence by sequence, with
+// kLatentCost places in front of each row tile's for what beginning and ending takes, and every workgroup takes a run of it (latent_run).
+// line: the run's length, then, from line[4] on, where each sequence's places end.
+__device__ __forceinline__ int latent_places(int units) { return units ? units + kLatentCost : 0; }
 struct LatentSeq {
     int n, first, count, rows, row_tiles, units;     // tokens; new rows; query rows, tiles of them; tiles of tokens
 };
@@ -66,19 +66,17 @@ __device__ __forceinline__ int latent_prefix_sum(int x) {
 // One wavefront makes the line.
 __device__ __forceinline__ void latent_make_line(const LatentView& v, const LatentGeom& g, const int32_t* __restrict__ row_start,
                                                  int32_t* __restrict__ line, int lane) {
-    int t1 = 0, t2 = 0, tl = 0;
+    int units = 0, pairs = 0;
     for (int s0 = 0; s0 < v.p.n_seqs; s0 += 64) {
         const LatentSeq w = latent_seq(v, g, row_start, s0 + lane);
-        t1 += __builtin_amdgcn_readlane(latent_prefix_sum(attend_places(w.units, 1, 0) * w.row_tiles), 63);
-        t2 += __builtin_amdgcn_readlane(latent_prefix_sum(attend_places(w.units, 2, 0) * w.row_tiles), 63);
-        tl += __builtin_amdgcn_readlane(latent_prefix_sum(attend_places(w.units, 1, kPieceCost) * w.row_tiles), 63);
+        units += __builtin_amdgcn_readlane(latent_prefix_sum(w.units * w.row_tiles), 63);
+        pairs += __builtin_amdgcn_readlane(latent_prefix_sum(w.units ? w.row_tiles : 0), 63);
     }
-    const AttendDivision d = attend_division(t1, t2, tl, g.groups, 1);
-    if (lane == 0) *reinterpret_cast<LatentLine*>(line) = LatentLine{d.round, d.cost, d.run, 0};
+    if (lane == 0) line[0] = latent_run(units, pairs, g.groups, 1 << g.tile_log2);
     int before = 0;
     for (int s0 = 0; s0 < v.p.n_seqs; s0 += 64) {
         const LatentSeq w = latent_seq(v, g, row_start, s0 + lane);
-        const int end = before + latent_prefix_sum(attend_places(w.units, d.round, d.cost) * w.row_tiles);
+        const int end = before + latent_prefix_sum(latent_places(w.units) * w.row_tiles);
         if (s0 + lane < v.p.n_seqs) line[4 + s0 + lane] = end;
         before = __builtin_amdgcn_readlane(end, 63);
     }
@@ -156,119 +154,180 @@ __global__ __launch_bounds__(256) void latent_absorb_kernel(LatentView v, Latent
     }
 }
 
-// Where piece p (16 bytes) of token t of a tile stands in LDS: the latents' rows first, then the position parts'.  Pieces are permuted by
-// the token, so that neither reading eight tokens' piece at once (keys) nor two pieces of four tokens (values, transposed) meets a bank twice.
-__device__ __forceinline__ int latent_swizzle(int t) { return ((t & 3) << 1) | ((t >> 2) & 1) | (t & 8); }
+// Where piece p (16 bytes) of token t of a tile stands in LDS, in rows of latents and of position parts: pieces are permuted by the token.  A read
+// of 16 bytes a lane takes four turns, of lanes 0-3, 12-15, 20-27, then 4-11, 16-19, 28-31, and the same of the upper half; one of 8 bytes
+// two, of half the lanes each.  The permutations put the pieces of a turn on different banks, both for keys (the same piece of 16 tokens, then the
+// one beside it) and for values (two pieces of eight tokens).  Measured with a permutation that does not, 43 % of the turns twice.
+__device__ __forceinline__ int latent_swizzle(int t) { return (t & 7) << 1; }
+template <int DR> __device__ __forceinline__ int rope_swizzle(int t) {
+    if (DR == 64) return (t >> 1) & 7;                                      // two tokens of eight pieces stand side by side,
+    const int q = t >> 2;                                                   // four of four pieces
+    return ((q ^ (q >> 1)) & 1) << 1 | ((q >> 1) & 1);
+}
 template <int DC> __device__ __forceinline__ int tile_latent(int t, int p) { return t * (DC * 2) + ((p ^ latent_swizzle(t)) << 4); }
-template <int DC, int DR> __device__ __forceinline__ int tile_rope(int t, int p) {
-    const int s = DR == 64 ? latent_swizzle(t) & 7 : (t >> 1) & 3;
-    return kLatentTile * DC * 2 + t * (DR * 2) + ((p ^ s) << 4);
+template <int DR> __device__ __forceinline__ int tile_rope(int t, int p) { return t * (DR * 2) + ((p ^ rope_swizzle<DR>(t)) << 4); }
+
+// Waits until at most n (3, 4, 5, else none) of the wavefront's loads are in flight.
+__device__ __forceinline__ void wait_loads(int n) {
+    if (n == 5) asm volatile("s_waitcnt vmcnt(5)" ::: "memory");
+    else if (n == 4) asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+    else if (n == 3) asm volatile("s_waitcnt vmcnt(3)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+// Waits for the other wavefronts; LDS is not touched across it.
+__device__ __forceinline__ void arrive() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Loads from memory to LDS, without registers in between: lane i's 16 bytes (to_lds_dwords: 4) to 16 i (4 i) behind the place that lds_place() has
+// named last plus OFFSET, from a base for all lanes, an offset of the lane, and OFFSET again; or (to_lds_from) from an address of the lane.  The
+// compiler would wait for all such loads in front of every read of LDS that they might write to, and a tile ahead would never be one; so they
+// are written out, and wait_loads() waits for them.  The place stands in a register that the loads behind it hold for some 200 cycles each: it is
+// named once for all rows of a wavefront.
+__device__ __forceinline__ void lds_place(uint8_t* to) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)to)));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(at) : "memory");
+}
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at) {
+    asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(at), "s"(base), "n"(OFFSET) : "memory");
+}
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds_dwords(const uint8_t* base, uint32_t at) {
+    asm volatile("global_load_lds_dword %0, %1 offset:%2" ::"v"(at), "s"(base - OFFSET), "n"(OFFSET) : "memory");
+}
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds_from(const uint8_t* from) {
+    asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from - OFFSET), "n"(OFFSET) : "memory");
 }
 
-// Waits until at most N of a wavefront's loads are in flight, then for the other wavefronts; memory is not touched across it.
-template <int N> __device__ __forceinline__ void arrive() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+// Packed latents of a wavefront's TW tokens: codes and parameters come to LDS as they are, into the place that its rows will have there (codes in
+// front, scales and minima in the last quarter).  -> the loads issued.
+template <int DC, int W, int TW>
+__device__ __forceinline__ int packed_fetch(const uint8_t* codes, const uint8_t* scales, uint8_t* rows, uint32_t mn_step, uint32_t param_bytes,
+                                            uint32_t lane) {
+    constexpr int kBytes = TW * DC * W / 8, kParams = TW * DC * 2 * 3 / 4;
+    static_assert(kBytes <= kParams, "codes and parameters do not overlap");
+    lds_place(rows);
+    if (kBytes >= 1024 || lane * 16 < kBytes) to_lds(codes, lane * 16);
+    if constexpr (kBytes > 1024) to_lds<1024>(codes, lane * 16);
+    static_assert(kBytes <= 2048, "two loads of codes");
+    if (lane * 4 < param_bytes) {
+        to_lds_dwords<kParams>(scales, lane * 4);
+        to_lds_dwords<kParams + TW * DC / 4>(scales + mn_step, lane * 4);
+    }
+    return (kBytes + 1023) / 1024 + 2;
 }
 
-// 16 bytes a lane from memory to LDS, lane i's at 16 i behind `to` (the same for all lanes), without registers in between: from a base for all
-// lanes and an offset of the lane, or from an address of the lane.  The compiler would wait for all such loads in front of every read of LDS
-// that they might write to, and a tile ahead would never be one; so they are written out, and arrive() waits for them.
-__device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at, uint8_t* to) {
-    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)to)));
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_at), "v"(at), "s"(base) : "memory");
-}
-__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
-    const uint32_t lds_at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)to)));
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_at), "v"(from) : "memory");
-}
-
-// What a wavefront brings of a tile: eight tokens, half of one page's sixteen; wave-uniform.
-struct TileHalf {
-    const uint8_t *codes, *scale, *rope;   // of its first token; from scale to mn: mn_step
-    int width, valid;                      // 0: absent; how many of the eight tokens there are
-};
-
-// Packed latents of the eight tokens: their codes come to LDS as they are, into the place that the wavefront's eight rows will have there;
-// lane i keeps the parameters of token i / groups, group i % groups (at most 8 * 8 pairs).
-struct HalfParams {
-    uint32_t sc, mn;                       // as they lie in memory
-};
-__device__ __forceinline__ uint32_t raw_param(const uint8_t* section, uint32_t i, bool half) {
-    return half ? reinterpret_cast<const uint16_t*>(section)[i] : reinterpret_cast<const uint32_t*>(section)[i];
-}
-__device__ __forceinline__ float raw_value(uint32_t raw, bool half) {
-    return half ? static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(raw))) : __builtin_bit_cast(float, raw);
-}
-template <int DC, int W>
-__device__ __forceinline__ void packed_fetch(HalfParams& x, const TileHalf& t, uint8_t* rows, uint64_t mn_step, int groups, bool half, uint32_t lane) {
-    constexpr int kBytes = 8 * DC * W / 8;
+// Eight latents from their codes, as a Load gives them: product and sum rounded to binary32 one after the other, then to fp16.  HP: a code of 8 bits
+// times a scale of 11 is exact, so that one multiply-add rounds as the two steps do.
+template <int W, bool HP>
+__device__ __forceinline__ u4_t latent_dequantise(u2_t w, float sc, float mn) {
+    typedef float f2_t __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < (kBytes + 1023) / 1024; ++i)
-        if (kBytes >= 1024 || lane * 16 < kBytes) to_lds(t.codes, i * 1024 + lane * 16, rows + i * 1024);
-    const uint32_t at = min(lane, static_cast<uint32_t>(8 * groups - 1));
-    x.sc = raw_param(t.scale, at, half);
-    x.mn = raw_param(t.scale + mn_step, at, half);
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t c = W == 8 ? ((k < 4 ? w.x : w.y) >> ((k & 3) * 8)) & 0xffu : (w.x >> (k * W)) & ((1u << W) - 1u);
+        const float code = static_cast<float>(c);
+        x[k] = HP ? __builtin_fmaf(code, sc, mn) : code * sc + mn;
+    }
+    u4_t y;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2_t{x[2 * k], x[2 * k + 1]}, h2_t));
+    return y;
 }
 
-// Dequantises them in their place (missing tokens: zeros).  All codes are read before the first row is written.
-template <int DC, int W>
-__device__ __forceinline__ void packed_unpack(const HalfParams& x, uint8_t* tile, int token0, int valid, int groups, int lpg_log2, bool half, int lane) {
-    constexpr int kRow = DC * W / 128, kN = (8 * kRow + 63) / 64, kOut = 16 / W;       // pieces of a token's codes, of a lane, and what one makes
-    const uint8_t* rows = tile + token0 * (DC * 2);
-    u4_t code[kN];
+// Dequantises them in their place, a lane eight latents at a time, side by side with its neighbours' (missing tokens: zeros).  All codes are
+// read before the first row is written; the parameters lie where the last one will be.  TIGHT: one step after the other, parameters a step ahead:
+// side by side they take registers that are not there.
+template <int DC, int W, int TW, bool HP, bool TIGHT>
+__device__ __forceinline__ void packed_unpack(uint8_t* tile, int token0, int valid, int groups, int lpg_log2, int lane) {
+    constexpr int kRow = DC / 8, kN = TW * kRow / 64, kParams = TW * DC * 2 * 3 / 4;   // pieces of a row, of a lane
+    static_assert((kN - 1) * 1024 <= kParams, "only the last step writes where the parameters lie");
+    uint8_t* rows = tile + token0 * (DC * 2);
+    const int param0 = lane / kRow * groups + ((lane % kRow) >> lpg_log2);
+    auto param = [&](int i, int section) __attribute__((always_inline)) {
+        return latent_param(rows + kParams + section * (TW * DC / 4), param0 + i * (64 / kRow) * groups, HP);
+    };
+    u2_t code[kN];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) code[i] = *reinterpret_cast<const u4_t*>(rows + i * 1024 + (8 * kRow < 64 ? lane % (8 * kRow) : lane) * 16);
+    for (int i = 0; i < kN; ++i) {
+        const uint8_t* from = rows + (i * 64 + lane) * W;
+        if constexpr (W == 8) code[i] = *reinterpret_cast<const u2_t*>(from);
+        else if constexpr (W == 4) code[i].x = *reinterpret_cast<const uint32_t*>(from);
+        else code[i].x = *reinterpret_cast<const uint16_t*>(from);
+    }
+    float sc[kN], mn[kN];
+#pragma unroll
+    for (int i = 0; i < (TIGHT ? 1 : kN); ++i) {
+        sc[i] = param(i, 0);
+        mn[i] = param(i, 1);
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-        const int p = (i * 64 + lane) % (8 * kRow), token = p / kRow, in = p % kRow;
-        const int of = token * groups + ((in * kOut) >> lpg_log2);
-        const float sc = raw_value(__shfl(x.sc, of), half), mn = raw_value(__shfl(x.mn, of), half);
-        const bool there = token < valid;
-        if (8 * kRow < 64 && lane >= 8 * kRow) continue;
-#pragma unroll
-        for (int o = 0; o < kOut; ++o) {
-            u2_t w;
-            if constexpr (W == 8) w = u2_t{code[i][2 * o], code[i][2 * o + 1]};
-            else if constexpr (W == 4) w = u2_t{code[i][o], 0u};
-            else w = u2_t{code[i][o / 2] >> (16 * (o % 2)), 0u};
-            u4_t y = dequantise_piece<W>(w, sc, mn);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = there ? y[e] : 0u;
-            *reinterpret_cast<u4_t*>(tile + tile_latent<DC>(token0 + token, in * kOut + o)) = y;
+        const int token = (i * 64 + lane) / kRow, in = lane % kRow;
+        u4_t y = latent_dequantise<W, HP>(code[i], sc[i], mn[i]);
+        if (TIGHT && i + 1 < kN) {
+            sc[(i + 1) % kN] = param(i + 1, 0);
+            mn[(i + 1) % kN] = param(i + 1, 1);
         }
+        if (valid < TW) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = token < valid ? y[e] : 0u;
+        }
+        *reinterpret_cast<u4_t*>(tile + tile_latent<DC>(token0 + token, in)) = y;
+        if (TIGHT && i + 1 < kN) asm volatile("" : "+v"(code[(i + 1) % kN].x), "+v"(code[(i + 1) % kN].y)::"memory");
     }
 }
 
-// Attention of a tile of M query rows to a run of tiles of tokens, the four wavefronts of a workgroup together.  A tile of 32 tokens comes
-// to LDS once, as fp16; each of the first M / 16 (at most four) wavefronts has the logits S^T = K Q^T and the softmax of its own rows, leaves
-// their probabilities in LDS, and each wavefront has a quarter of the dimensions of O^T += V^T P^T for all rows: keys are read from LDS
-// by M / 16 wavefronts, values by one.
+struct LatentAttendArgs {
+    LatentView v;
+    LatentGeom g;
+    const _Float16 *qa, *q;
+    const int32_t *row_start, *line;
+    const uint8_t* zeros;
+    float *part_o, *part_ml;
+    int32_t lpg_log2;
+};
+
+// Attention of a tile of M query rows to a run of tiles of tokens, the eight wavefronts of a workgroup together.  A tile of 32 tokens comes to
+// LDS once, as fp16; each of the first M / 16 wavefronts has the logits S^T = K Q^T and the softmax of its own 16 rows and leaves their
+// probabilities in LDS, and each wavefront has an eighth of the dimensions of O^T += V^T P^T for all rows: keys are read from LDS by M / 16
+// wavefronts, values by one.  A turn of the loop, with one barrier, asks for tile t + 3, has the logits and the softmax of tile t + 1 and the
+// values of tile t, half of the wavefronts in this order and half in the other, so that the exponentials of one are beside the products of the
+// other, and brings tile t + 2 into its form.
 template <int DC, int DR, int M>
-__global__ __launch_bounds__(256, 2) void latent_attend_kernel(LatentView v, LatentGeom g, const _Float16* __restrict__ qa,
-                                                                              const _Float16* __restrict__ q, const int32_t* __restrict__ row_start,
-                                                                              const int32_t* __restrict__ line, const uint8_t* __restrict__ zeros,
-                                                                              int32_t lpg_log2, float* __restrict__ part_o, float* __restrict__ part_ml) {
-    constexpr int kTileBytes = kLatentTile * (DC + DR) * 2, kBufs = 2;
-    constexpr int kWaves = M >= 64 ? 4 : M / 16, RB = M / 16 / kWaves;         // wavefronts with rows, blocks of 16 rows of each
-    constexpr int KS = DC / 32, KR = DR / 32, DB = DC / 64, MB = M / 16;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kBufs * kTileBytes];
-    __shared__ __attribute__((aligned(16))) uint8_t probs[M * 64];             // [MB][64 lanes][16 bytes]
-    __shared__ float alphas[M];                                                // what the rows' outputs are rescaled by,
-    __shared__ int32_t moved[4];                                               // if any of the wavefront's rows are
-    __shared__ uint32_t bad_tokens;                                            // tokens of a tile that are not finite
+__global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs args) {
+    // (arguments are fetched where they are used, in the loop only by what is rare: kept in registers all the time they do not fit, and what
+    // does not fit is fetched from vector registers, one by one)
+    auto here = [&]() __attribute__((always_inline)) {
+        auto at = (const __attribute__((address_space(4))) LatentAttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+        asm volatile("" : "+s"(at));
+        return (const LatentAttendArgs*)at;
+    };
+    const int32_t* line = args.line;
+    const uint8_t* zeros = args.zeros;
+    uint8_t* const pool = args.v.p.pool;
+    const float scale_log2e = args.g.scale_log2e;
+    constexpr int kTileBytes = kLatentTile * DC * 2, kRopeBytes = kLatentTile * DR * 2;
+    constexpr int NW = kLatentWaves, kWaves = M / 16;                          // wavefronts, those with rows (16 each)
+    constexpr int KS = DC / 32, KR = DR / 32, DB = DC / 16 / NW, MB = M / 16;  // steps over the dimensions; a wavefront's blocks of 16 of them
+    constexpr int TW = kLatentTile / NW;                                       // tokens that a wavefront brings
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kTileBytes], rope_lds[3 * kRopeBytes];      // of the tiles in turn
+    // of the tiles in turn: probabilities [MB][64 lanes][16 bytes], what the rows' outputs are rescaled by, blocks of rows that are, tokens that
+    // are not finite
+    __shared__ __attribute__((aligned(16))) uint8_t probs_lds[2][M * 64];
+    __shared__ float alphas_lds[2][M];
+    __shared__ uint32_t moved_lds[3];
+    __shared__ uint32_t bad_lds[2];
     const int lane0 = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const LatentLine ll = *reinterpret_cast<const LatentLine*>(line);
-    int at = static_cast<int>(blockIdx.x) * ll.run;
-    const int run_end = at + ll.run;
-    if (threadIdx.x == 0) bad_tokens = 0u;
-    if (threadIdx.x < 4) moved[threadIdx.x] = 0;
+    const int run = line[0];
+    int at = static_cast<int>(blockIdx.x) * run;
+    const int run_end = at + run;
+    const int n_seqs = args.v.p.n_seqs;
     int s = -1, s_end = 0;
     while (at < run_end) {
         // the sequence in whose work place `at` lies: the first that ends behind it
         if (at >= s_end) {
-            int lo = s + 1, n = v.p.n_seqs - lo;
+            int lo = s + 1, n = n_seqs - lo;
             while (n > 64) {
                 const int step = (n + 63) >> 6, i = min(lane0 * step + step - 1, n - 1);
                 const int cnt = __builtin_popcountll(__ballot(line[4 + lo + i] <= at && lane0 * step < n));
@@ -282,36 +341,32 @@ __global__ __launch_bounds__(256, 2) void latent_attend_kernel(LatentView v, Lat
             s = __builtin_amdgcn_readfirstlane(lo + __builtin_ctzll(any));
             s_end = __builtin_amdgcn_readfirstlane(line[4 + s]);
         }
-        const LatentSeq sw = latent_seq(v, g, row_start, s);
-        const int each = attend_places(sw.units, ll.round, ll.cost), local = at - (s_end - each * sw.row_tiles);
+        const LatentAttendArgs* a0 = here();
+        const LatentSeq sw = latent_seq(a0->v, a0->g, a0->row_start, s);
+        const int each = latent_places(sw.units), local = at - (s_end - each * sw.row_tiles);
         const int rt = local / each, place = local - rt * each, places = min(each - place, run_end - at);
-        const int u_begin = max(place - ll.cost, 0), u_end = min(place + places - ll.cost, sw.units);
+        const int u_begin = max(place - kLatentCost, 0), u_end = place + places - kLatentCost;
         at += places;
         if (u_end <= u_begin) continue;
 
         // this wavefront's rows: queries, what they see
-        const int count = min(sw.count, g.max_rows), H = g.H;
-        h8_t qf[RB][KS + KR];
-        int last[RB];
-        float ref[RB], sum[RB];
+        const int count = min(sw.count, a0->g.max_rows), H = a0->g.H;
+        h8_t qf[KS + KR];
+        int last = -1;
+        float ref = -INFINITY, sum = 0.0f;
         if (wave < kWaves) {
             int lane = lane0;
             asm volatile("" : "+v"(lane));
             const int l16 = lane & 15, g4 = lane >> 4;
+            const int j = rt * M + wave * 16 + l16, nth = j / H, h = j - nth * H;
+            const bool ok = j < sw.rows;
+            last = ok ? sw.n - sw.count + nth : -1;
+            const _Float16* lat = a0->qa + (static_cast<int64_t>(s) * a0->g.max_rows * H + (ok ? j : 0)) * DC + 8 * g4;
+            const _Float16* pos = a0->q + (sw.first + (ok ? nth : 0)) * a0->g.q_stride + (ok ? h : 0) * (a0->g.Dk + DR) + a0->g.Dk + 8 * g4;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int j = rt * M + (wave * RB + b) * 16 + l16, nth = j / H, h = j - nth * H;
-                const bool ok = j < sw.rows;
-                last[b] = ok ? sw.n - sw.count + nth : -1;
-                ref[b] = -INFINITY;
-                sum[b] = 0.0f;
-                const _Float16* lat = qa + (static_cast<int64_t>(s) * g.max_rows * H + (ok ? j : 0)) * DC + 8 * g4;
-                const _Float16* pos = q + (sw.first + (ok ? nth : 0)) * g.q_stride + (ok ? h : 0) * (g.Dk + DR) + g.Dk + 8 * g4;
+                for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const h8_t*>(lat + 32 * k);
 #pragma unroll
-                for (int k = 0; k < KS; ++k) qf[b][k] = *reinterpret_cast<const h8_t*>(lat + 32 * k);
-#pragma unroll
-                for (int k = 0; k < KR; ++k) qf[b][KS + k] = *reinterpret_cast<const h8_t*>(pos + 32 * k);
-            }
+                for (int k = 0; k < KR; ++k) qf[KS + k] = *reinterpret_cast<const h8_t*>(pos + 32 * k);
         }
         const int all_see = sw.n - sw.count + rt * M / H;       // tokens up to this one are seen by every row
         const int none_sees = sw.n - sw.count + min(count, (rt * M + M - 1) / H + 1);
@@ -321,122 +376,159 @@ __global__ __launch_bounds__(256, 2) void latent_attend_kernel(LatentView v, Lat
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[b][d] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-        // the pages of 64 halves of tiles (16 tokens each), one per lane
-        const uint64_t* offs = v.p.off + static_cast<int64_t>(s) * v.p.stride;
-        const uint8_t* bits = v.p.bits + static_cast<int64_t>(s) * v.p.stride;
-        uint64_t half_off = 0;
-        uint32_t half_row = 0, half_width = 0;                  // (row: of the first token, of the record's rows of a section)
+        // What this wavefront brings of 64 tiles, a tile per lane: the record of its tokens' page and where their rows lie in it, and of which tiles
+        // either half (16 tokens, one page) is there.
+        const int my_token = wave * TW, my_half = my_token / 16, seq_n = sw.n;
+        uint64_t tile_off = 0, have_low = 0, have_high = 0;
+        uint32_t tile_row = 0, tile_width = 0;
         int batch0 = -1;                                        // first tile of the batch
+        const uint32_t rope16 = static_cast<uint32_t>(a0->v.p.bit_bytes) * 16;      // where position parts begin in fp16 records
         auto look_up = [&](int u) __attribute__((always_inline)) {
             batch0 = u;
             int lane = lane0;
             asm volatile("" : "+v"(lane));
-            const int half = 2 * u + lane;
-            const bool in = (half * 16 < min(sw.n, none_sees)) & (half < 2 * u_end);
-            const int half_page = v.p.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(half), v.p.page_of_tile)) : half;
-            const int page = in ? half_page : 0;
-            const uint64_t off = offs[page];
-            const uint32_t b = bits[page];
-            half_width = (in & latent_present(v, off, b)) ? b : 0u;
-            half_off = off;
-            half_row = static_cast<uint32_t>(v.layer * v.p.T + half * 16 - page * v.p.T);
+            const LatentAttendArgs* a = here();
+            const LatentView v = a->v;
+            const uint64_t* offs = v.p.off + static_cast<int64_t>(s) * v.p.stride;
+            const uint8_t* bits = v.p.bits + static_cast<int64_t>(s) * v.p.stride;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int half = 2 * (u + lane) + i;
+                const bool in = (half * 16 < min(seq_n, none_sees)) & (u + lane < u_end);
+                const int half_page = v.p.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(half), v.p.page_of_tile)) : half;
+                const int page = in ? half_page : 0;
+                const uint64_t off = offs[page];
+                const uint32_t b = bits[page], width = (in & latent_present(v, off, b)) ? b : 0u;
+                if (i == 0) have_low = __ballot(width != 0);
+                else have_high = __ballot(width != 0);
+                if (my_half == i) {
+                    tile_off = off;
+                    tile_width = width;
+                    tile_row = static_cast<uint32_t>(v.layer * v.p.T + half * 16 + my_token % 16 - page * v.p.T);
+                }
+            }
         };
-        auto lane_u64 = [&](uint64_t x, int l) __attribute__((always_inline)) {
-            const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(x), l), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(x >> 32), l);
-            return static_cast<uint64_t>(hi) << 32 | lo;
-        };
-        const uint64_t mn_step = static_cast<uint64_t>(v.p.slabs) * v.p.T * static_cast<uint32_t>(v.p.groups * (v.p.half_params ? 2 : 4));
-        const int my_half = wave >> 1, my_token = wave * 8;    // the eight tokens of a tile that this wavefront brings
-        auto half_of = [&](int u) __attribute__((always_inline)) {
-            TileHalf t;
-            const int l = 2 * (u - batch0) + my_half;
-            const int first = (wave & 1) * 8;
-            t.width = static_cast<int>(__builtin_amdgcn_readlane(half_width, l));
-            const uint8_t* record = v.p.pool + lane_u64(half_off, l);
-            const uint32_t row = __builtin_amdgcn_readlane(half_row, l) + first, b = t.width;
-            t.codes = record + static_cast<uint64_t>(row) * (DC / 8 * b);
-            record += v.p.bit_bytes * b;
-            t.scale = record + static_cast<uint64_t>(row) * static_cast<uint32_t>(v.p.groups * (v.p.half_params ? 2 : 4));
-            t.rope = record + (b == 16 ? 0u : v.p.param_bytes) + static_cast<uint64_t>(row) * (DR * 2);
-            t.valid = t.width ? max(0, min(8, sw.n - (u * kLatentTile + my_token))) : 0;
-            return t;
-        };
-        HalfParams packed = {0u, 0u};
-        int packed_width = 0, packed_valid = 0;
-        // Issues the loads of tile u into buffer `buf`.  fp16 rows and position parts go straight to LDS, rows that are not there come from the
-        // zeros; packed ones are unpacked behind this tile's values.
-        auto fetch = [&](int u, int buf) __attribute__((always_inline)) {
-            const TileHalf t = half_of(u);
-            uint8_t *tile = lds + buf * kTileBytes, *rows = tile + my_token * (DC * 2);
+        // Asks for tile u.  Whole rows and position parts come as they stay, those of tokens that are not there from the zeros.
+        int loads = 0, width1 = 16, valid1 = 0;                 // of the tile that was asked for last: the loads, what this wavefront has of it,
+        int have1 = 0, have2 = 0;                               // which halves are there; the same of the tile before
+        auto fetch = [&](int u, uint8_t* rope) __attribute__((always_inline)) {
             constexpr int kRopeRow = DR / 8, kRow = DC / 8, kSide = 64 / kRow;
+            const int l = u - batch0;
+            have1 = static_cast<int>((have_low >> l & 1) | (have_high >> l & 1) << 1);
+            width1 = static_cast<int>(__builtin_amdgcn_readlane(tile_width, l));
+            valid1 = width1 ? max(0, min(TW, seq_n - (u * kLatentTile + my_token))) : 0;
+            const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(tile_off), l);
+            const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(tile_off >> 32), l);
+            const uint8_t* record = pool + (static_cast<uint64_t>(hi) << 32 | lo);
+            const uint32_t row = __builtin_amdgcn_readlane(tile_row, l);       // (offsets in a record fit in 32 bits)
+            uint8_t* rows = lds + (u & 3) * kTileBytes + my_token * (DC * 2);
+            rope += my_token * (DR * 2);
             uint32_t lane_at = lane0;                           // (offsets of lanes are made here, not kept)
             asm volatile("" : "+v"(lane_at));
-            if (lane_at < 8 * kRopeRow) {
-                const uint32_t tk = lane_at / kRopeRow, slot = lane_at % kRopeRow;
-                const uint32_t sw_t = DR == 64 ? latent_swizzle(my_token + tk) & 7 : ((my_token + tk) >> 1) & 3;
-                const uint8_t* from = static_cast<int>(tk) < t.valid ? t.rope + (tk * (DR * 2) + ((slot ^ sw_t) << 4)) : zeros + slot * 16;
-                to_lds(from, tile + kLatentTile * DC * 2 + my_token * (DR * 2));
-            }
-            packed_width = t.valid ? t.width : 16;
-            packed_valid = t.valid;
-            if (packed_width == 16) {
-#pragma unroll
-                for (int i = 0; i < 8 / kSide; ++i) {
-                    uint8_t* to = rows + i * kSide * (DC * 2);
-                    if constexpr (kSide == 1) {
-                        const uint8_t* from = i < t.valid ? t.codes + i * (DC * 2) : zeros;       // (as many zeros as a row has)
-                        to_lds(from, (lane_at ^ static_cast<uint32_t>(latent_swizzle(my_token + i))) << 4, to);
-                    } else {
-                        const uint32_t tk = i * kSide + lane_at / kRow, slot = lane_at % kRow;
-                        const uint32_t in = (slot ^ static_cast<uint32_t>(latent_swizzle(my_token + tk))) << 4;
-                        const uint8_t* from = static_cast<int>(tk) < t.valid ? t.codes + (tk * (DC * 2) + in) : zeros + in;
-                        to_lds(from, to);
-                    }
+            const uint32_t rope_tk = lane_at / kRopeRow, rope_in = ((lane_at % kRopeRow) ^ rope_swizzle<DR>(my_token + rope_tk)) << 4;
+            // piece `lane` of the wavefront's rows, `i` loads on: its place from the load's first row on, as it comes from memory
+            auto in_rows = [&](int i) __attribute__((always_inline)) {
+                const uint32_t tk = lane_at / kRow;
+                return tk * (DC * 2) + (((lane_at % kRow) ^ static_cast<uint32_t>(latent_swizzle(my_token + i * kSide + tk))) << 4);
+            };
+            static_assert(TW / kSide == 4 || TW / kSide == 2, "four loads of whole rows, or two");
+            constexpr bool kFour = TW / kSide == 4;
+            lds_place(rope);
+            if (valid1 == TW && width1 == 16) {
+                if (lane_at < TW * kRopeRow) to_lds(record + (rope16 + row * (DR * 2)), rope_tk * (DR * 2) + rope_in);
+                const uint8_t* codes = record + row * (DC * 2);
+                lds_place(rows);
+                to_lds(codes, in_rows(0));
+                to_lds<1024>(codes, in_rows(1));
+                if constexpr (kFour) {
+                    to_lds<2048>(codes, in_rows(2));
+                    to_lds<3072>(codes, in_rows(3));
                 }
-            } else if (packed_width == 8) packed_fetch<DC, 8>(packed, t, rows, mn_step, v.p.groups, v.p.half_params, lane_at);
-            else if (packed_width == 4) packed_fetch<DC, 4>(packed, t, rows, mn_step, v.p.groups, v.p.half_params, lane_at);
-            else packed_fetch<DC, 2>(packed, t, rows, mn_step, v.p.groups, v.p.half_params, lane_at);
+                loads = TW / kSide + 1;
+                return;
+            }
+            const LatentAttendArgs* a = here();
+            const uint32_t behind_codes = static_cast<uint32_t>(a->v.p.bit_bytes) * width1;
+            const uint8_t* codes = record + row * (DC / 8 * width1);
+            const uint8_t* ropes = record + (behind_codes + (width1 == 16 ? 0u : static_cast<uint32_t>(a->v.p.param_bytes)) + row * (DR * 2));
+            if (lane_at < TW * kRopeRow)
+                to_lds_from(static_cast<int>(rope_tk) < valid1 ? ropes + (rope_tk * (DR * 2) + rope_in) : zeros + rope_in);
+            if (valid1 == 0) width1 = 16;
+            if (width1 == 16) {
+                auto from = [&](int i) __attribute__((always_inline)) {
+                    return static_cast<int>(i * kSide + lane_at / kRow) < valid1 ? codes + i * 1024 + in_rows(i) : zeros + in_rows(i);
+                };
+                lds_place(rows);
+                to_lds_from(from(0));
+                to_lds_from<1024>(from(1));
+                if constexpr (kFour) {
+                    to_lds_from<2048>(from(2));
+                    to_lds_from<3072>(from(3));
+                }
+                loads = TW / kSide + 1;
+            } else {
+                const uint32_t param_row = a->v.p.groups * (a->v.p.half_params ? 2 : 4), mn_step = a->v.p.slabs * a->v.p.T * param_row;
+                const uint8_t* scales = record + (behind_codes + row * param_row);
+                if (width1 == 8) loads = 1 + packed_fetch<DC, 8, TW>(codes, scales, rows, mn_step, TW * param_row, lane_at);
+                else if (width1 == 4) loads = 1 + packed_fetch<DC, 4, TW>(codes, scales, rows, mn_step, TW * param_row, lane_at);
+                else loads = 1 + packed_fetch<DC, 2, TW>(codes, scales, rows, mn_step, TW * param_row, lane_at);
+            }
         };
-        auto unpack = [&](int buf) __attribute__((always_inline)) {
-            uint8_t* tile = lds + buf * kTileBytes;
+        auto unpack = [&](int u, int width, int valid) __attribute__((always_inline)) {
+            uint8_t* tile = lds + (u & 3) * kTileBytes;
             int lane_at = lane0;
             asm volatile("" : "+v"(lane_at));
-            if (packed_width != 16) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // the codes are there
-            if (packed_width == 8) packed_unpack<DC, 8>(packed, tile, my_token, packed_valid, v.p.groups, lpg_log2, v.p.half_params, lane_at);
-            else if (packed_width == 4) packed_unpack<DC, 4>(packed, tile, my_token, packed_valid, v.p.groups, lpg_log2, v.p.half_params, lane_at);
-            else if (packed_width == 2) packed_unpack<DC, 2>(packed, tile, my_token, packed_valid, v.p.groups, lpg_log2, v.p.half_params, lane_at);
+            const LatentAttendArgs* a = here();
+            const int groups = a->v.p.groups, lpg_log2 = a->lpg_log2;
+            const bool half_params = a->v.p.half_params;
+#define KV_UNPACK(W)                                                                                                       \
+    do {                                                                                                                   \
+        if (half_params) packed_unpack<DC, W, TW, true, (M * DC > 64 * 512)>(tile, my_token, valid, groups, lpg_log2, lane_at);         \
+        else packed_unpack<DC, W, TW, false, (M * DC > 64 * 512)>(tile, my_token, valid, groups, lpg_log2, lane_at);                        \
+    } while (0)
+            if (width == 8) KV_UNPACK(8);
+            else if (width == 4) KV_UNPACK(4);
+            else if (width == 2) KV_UNPACK(2);
+#undef KV_UNPACK
         };
 
         look_up(u_begin);
         __syncthreads();                                        // (the piece before is done with LDS)
-        fetch(u_begin, 0);
-        int buf = 0;
-        for (int u = u_begin; u < u_end; ++u) {
-            // which of the tile's halves are there
-            const int l = 2 * (u - batch0);
-            const bool have0 = __builtin_amdgcn_readlane(half_width, l) != 0, have1 = __builtin_amdgcn_readlane(half_width, l + 1) != 0;
-            const int token0 = u * kLatentTile;
-            const bool masked = token0 + kLatentTile - 1 > all_see || !have0 || !have1;
-            uint8_t* tile = lds + buf * kTileBytes;
-            unpack(buf);
-            arrive<0>();                                        // the tile is there; values of the one before have been used
-            buf = buf + 1 == kBufs ? 0 : buf + 1;
-            if (u + 1 < u_end) {
-                if (u + 1 - batch0 >= 32) look_up(u + 1);
-                fetch(u + 1, buf);
-            }
+        if (threadIdx.x < 2) bad_lds[threadIdx.x] = 0u;
+        if (threadIdx.x < 3) moved_lds[threadIdx.x] = 0u;
+        int third = 0;                                          // u % 3, counted from the first turn
+        bool was_edge = false, was_moved = false;               // of the turn before
+        for (int u = u_begin - 3; u < u_end; ++u) {             // (the first three turns bring tiles, the third has logits)
+            const int token0 = (u + 1) * kLatentTile;           // of the tile whose logits are made
+            const int have = have2;                             // which of its halves are there
+            const bool edge = token0 + kLatentTile - 1 > all_see, masked = edge || have != 3;
+            const int next_third = third == 2 ? 0 : third + 1;
+            arrive();                                           // tile u + 1 and the probabilities of tile u are there, tile u - 1 has been used
+            const int width2 = width1, valid2 = valid1;         // of tile u + 2
+            have2 = have1;
+            loads = 0;
+            auto ask = [&]() __attribute__((always_inline)) {
+                if (u + 3 < u_end) {
+                    if (u + 3 - batch0 >= 64) look_up(u + 3);
+                    fetch(u + 3, rope_lds + third * kRopeBytes);        // (where tile u was)
+                }
+            };
+            const uint32_t moved_word = moved_lds[third];       // (read early: it is needed behind the first loads)
+            const int odd = u & 1;                              // (of tile u; tile u + 1 has the other)
             // (what depends on the lane is worked out here again: kept over the loop it would not fit the registers)
             int lane = lane0;
             asm volatile("" : "+v"(lane));
-            const int l16 = lane & 15, g4 = lane >> 4, thread_at = wave * 64 + lane;
+            const int l16 = lane & 15, g4 = lane >> 4;
             // A latent that is not finite must not reach rows that do not see its token, whose probability of 0 does not hold it off: where
-            // some row does not see all tokens it is replaced, and rows that see it are NaN.
-            uint32_t bad = 0u;
-            if (token0 + kLatentTile - 1 > all_see) {
-                const int t = thread_at >> 3;
+            // some row does not see all tokens it is replaced, and rows that see it are NaN.  -> such tokens of tile u + 1.
+            auto scan = [&]() __attribute__((always_inline)) {
+                if (!edge) return 0u;
+                uint8_t* tile = lds + ((u + 1) & 3) * kTileBytes;
+                constexpr int kPer = 64 * NW / kLatentTile;     // threads per token
+                const int thread_at = wave * 64 + lane, t = thread_at / kPer;
                 bool found = false;
 #pragma unroll 1
-                for (int p = thread_at & 7; p < DC / 8; p += 8) {
+                for (int p = thread_at % kPer; p < DC / 8; p += kPer) {
                     u4_t* x = reinterpret_cast<u4_t*>(tile + tile_latent<DC>(t, p));
                     u4_t y = *x;
                     bool any = false;
@@ -448,130 +540,153 @@ __global__ __launch_bounds__(256, 2) void latent_attend_kernel(LatentView v, Lat
                     if (any) *x = y;
                     found |= any;
                 }
-                if (found) atomicOr(&bad_tokens, 1u << t);
+                if (found) atomicOr(&bad_lds[odd ^ 1], 1u << t);
                 __syncthreads();
-                bad = bad_tokens;
-            }
-            if (wave < kWaves) {
-                lf4_t sc[RB][2];
+                return bad_lds[odd ^ 1];
+            };
+            auto logits = [&](uint32_t bad) __attribute__((always_inline)) {
+                const uint8_t* tile = lds + ((u + 1) & 3) * kTileBytes;
+                const uint8_t* rope = rope_lds + next_third * kRopeBytes;
+                uint8_t* probs = probs_lds[odd ^ 1];
+                if (wave < kWaves) {
+                    lf4_t sc[2] = {lf4_t{0.0f, 0.0f, 0.0f, 0.0f}, lf4_t{0.0f, 0.0f, 0.0f, 0.0f}};
+                    // (of a row's pieces four steps have the same low bits, which are all that the swizzle, the same for both halves, changes)
+                    uint32_t key_at = tile_latent<DC>(l16, g4), rope_key_at = tile_rope<DR>(l16, g4);
+                    asm volatile("" : "+v"(key_at), "+v"(rope_key_at));
+                    // Keys of the next steps are on their way while a step's are multiplied; the fences keep the compiler from fetching them all
+                    // first, for which there are no registers.
+                    constexpr int kAhead = M * (DC + DR) > 128 * 544 ? 1 : 2;
+                    h8_t kf[kAhead + 1][2];
+                    auto key = [&](int k, int i) __attribute__((always_inline)) {
+                        return *reinterpret_cast<const h8_t*>(k < KS ? tile + (key_at ^ ((k & 3) << 6)) + (k >> 2) * 256 + i * (16 * DC * 2)
+                                                                     : rope + (rope_key_at ^ ((k - KS) << 6)) + i * (16 * DR * 2));
+                    };
 #pragma unroll
-                for (int b = 0; b < RB; ++b)
+                    for (int f = 0; f < 2 * kAhead; ++f) kf[f / 2][f % 2] = key(f / 2, f % 2);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) sc[b][i] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                // (of a row's pieces four steps have the same low bits, which are all that the swizzle, the same for both halves, changes)
-                uint32_t key_at = tile_latent<DC>(l16, g4), rope_key_at = tile_rope<DC, DR>(l16, g4);
-                asm volatile("" : "+v"(key_at), "+v"(rope_key_at));
-                // Keys of the next two steps are on their way while these are multiplied; the fences keep the compiler from fetching them all
-                // first, for which there are no registers.
-                h8_t kf[2][4];
-                auto key = [&](int k, int i) __attribute__((always_inline)) {
-                    const uint32_t in = k < KS ? (key_at ^ ((k & 3) << 6)) + (k >> 2) * 256 + i * (16 * DC * 2)
-                                               : (rope_key_at ^ ((k - KS) << 6)) + i * (16 * DR * 2);
-                    return *reinterpret_cast<const h8_t*>(tile + in);
-                };
+                    for (int k = 0; k < KS + KR; ++k) {
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int f = 0; f < 4; ++f) kf[0][f] = key(f / 2, f % 2);
+                        for (int i = 0; i < 2; ++i)
+                            if (k + kAhead < KS + KR) kf[(k + kAhead) % (kAhead + 1)][i] = key(k + kAhead, i);
 #pragma unroll
-                for (int k = 0; k < KS + KR; k += 2) {
+                        for (int i = 0; i < 2; ++i) sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[k % (kAhead + 1)][i], qf[k], sc[i], 0, 0, 0);
+                    }
                     __builtin_amdgcn_sched_barrier(0);
-                    const int set = (k / 2) & 1;
-#pragma unroll
-                    for (int f = 0; f < 4; ++f)
-                        if (k + 2 + f / 2 < KS + KR) kf[set ^ 1][f] = key(k + 2 + f / 2, f % 2);
-#pragma unroll
-                    for (int f = 0; f < 4; ++f)
-                        if (k + f / 2 < KS + KR) {
-#pragma unroll
-                            for (int b = 0; b < RB; ++b)
-                                sc[b][f % 2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[set][f], qf[b][k + f / 2], sc[b][f % 2], 0, 0, 0);
-                        }
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                // sc[b][i][e]: token 16 i + 4 g4 + e against row l16 of block b
-                if (masked) {
-#pragma unroll
-                    for (int b = 0; b < RB; ++b)
+                    // sc[i][e]: token 16 i + 4 g4 + e against row l16
+                    if (masked) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int t = 16 * i + 4 * g4 + e;
-                                if (bad >> t & 1) sc[b][i][e] = NAN;
-                                if (!(i ? have1 : have0) || token0 + t > last[b]) sc[b][i][e] = -INFINITY;
+                                if (bad >> t & 1) sc[i][e] = NAN;
+                                if (!(have >> i & 1) || token0 + t > last) sc[i][e] = -INFINITY;
                             }
-                }
-                float top[RB];
-                bool move = false;
-#pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    float m = fmaxf(fmaxf(sc[b][0][0], sc[b][0][1]), fmaxf(sc[b][0][2], sc[b][0][3]));
-                    m = fmaxf(m, fmaxf(fmaxf(sc[b][1][0], sc[b][1][1]), fmaxf(sc[b][1][2], sc[b][1][3])));
-                    top[b] = m * g.scale_log2e;
-                    move |= top[b] > ref[b] + kLatentSlack;
-                }
-                if (__any(move)) {                              // (rare: the reference has room)
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        float m = fmaxf(top[b], __shfl_xor(top[b], 16));
-                        m = fmaxf(m, __shfl_xor(m, 32));
-                        const float to = m > ref[b] + kLatentSlack ? m - kLatentTop : ref[b];
-                        const float alpha = to == ref[b] ? 1.0f : __builtin_amdgcn_exp2f(ref[b] - to);
-                        ref[b] = to;
-                        sum[b] *= alpha;
-                        if (g4 == 0) alphas[(wave * RB + b) * 16 + l16] = alpha;
                     }
-                    if (lane == 0) moved[wave] = 1;
-                } else if (lane == 0) moved[wave] = 0;
-#pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    const float r = ref[b] == -INFINITY ? 0.0f : ref[b];
+                    float top = fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3]));
+                    top = fmaxf(top, fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3]))) * scale_log2e;
+                    const bool move = __any(top > ref + kLatentSlack);
+                    if (move) {                                     // (rare: the reference has room)
+                        float m = fmaxf(top, __shfl_xor(top, 16));
+                        m = fmaxf(m, __shfl_xor(m, 32));
+                        const float to = m > ref + kLatentSlack ? m - kLatentTop : ref;
+                        const float alpha = to == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+                        ref = to;
+                        sum *= alpha;
+                        if (g4 == 0) alphas_lds[odd ^ 1][wave * 16 + l16] = alpha;
+                        if (lane == 0) atomicOr(&moved_lds[next_third], 1u << wave);
+                    }
+                    const float r = ref == -INFINITY ? 0.0f : ref;
                     h8_t p;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][i][e], g.scale_log2e, -r));
-                            sum[b] += x;
+                            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e], scale_log2e, -r));
+                            sum += x;
                             p[4 * i + e] = static_cast<_Float16>(x);
                         }
-                    *reinterpret_cast<h8_t*>(probs + (wave * RB + b) * 1024 + lane * 16) = p;
+                    *reinterpret_cast<h8_t*>(probs + wave * 1024 + lane * 16) = p;
                 }
-            }
-            __syncthreads();
-            if (bad && thread_at == 0) bad_tokens = 0u;
+            };
+            auto rescale = [&]() __attribute__((always_inline)) {
+                const uint32_t moved = __builtin_amdgcn_readfirstlane(moved_word);
+                if (moved == 0) return;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                if (moved[w]) {
+                for (int b = 0; b < MB; ++b)
+                    if (moved >> b & 1) {
+                        const float a = alphas_lds[odd][b * 16 + l16];
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        const float a = alphas[(w * RB + b) * 16 + l16];
-#pragma unroll
-                        for (int d = 0; d < DB; ++d) o[w * RB + b][d] *= a;
+                        for (int d = 0; d < DB; ++d) o[b][d] *= a;
                     }
+            };
+            auto values = [&]() __attribute__((always_inline)) {
+                const uint8_t *tile = lds + (u & 3) * kTileBytes, *probs = probs_lds[odd];
+                // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
+                uint32_t value_at = tile_latent<DC>(4 * g4 + (l16 >> 2), wave * DB * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
+                asm volatile("" : "+v"(value_at));
+                auto value = [&](int d) __attribute__((always_inline)) {
+                    const uint8_t* from = tile + (value_at ^ (d << 5));
+                    const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
+                    const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 16 * DC * 2));
+                    const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
+                    return h8_t{a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+            };
+            auto weights = [&](int b) __attribute__((always_inline)) { return *reinterpret_cast<const h8_t*>(probs + b * 1024 + lane * 16); };
+            // (the fewer operands are kept)
+            if constexpr (MB > DB) {
+                h8_t vf[DB];
+#pragma unroll
+                for (int d = 0; d < DB; ++d) vf[d] = value(d);
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    const h8_t pf = weights(b);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d], pf, o[b][d], 0, 0, 0);
                 }
-            h8_t pf[MB];
+            } else {
+                h8_t pf[MB];
 #pragma unroll
-            for (int b = 0; b < MB; ++b) pf[b] = *reinterpret_cast<const h8_t*>(probs + b * 1024 + lane * 16);
-            // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
-            uint32_t value_at = tile_latent<DC>(4 * g4 + (l16 >> 2), wave * DB * 2 + ((lane & 3) >> 1)) + (lane & 1) * 8;
-            asm volatile("" : "+v"(value_at));
+                for (int b = 0; b < MB; ++b) pf[b] = weights(b);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                if (M == 128) __builtin_amdgcn_sched_barrier(0);
-                const uint8_t* from = tile + (value_at ^ (d << 5));
-                const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
-                const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 16 * DC * 2));
-                const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
-                const h8_t vf = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+                for (int d = 0; d < DB; ++d) {
+                    const h8_t vf = value(d);
 #pragma unroll
-                for (int b = 0; b < MB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[b], o[b][d], 0, 0, 0);
+                    for (int b = 0; b < MB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[b], o[b][d], 0, 0, 0);
+                }
             }
+            };
+            // (the loads of a tile keep the CU's path to memory busy for some 600 cycles, in which whoever has more waits: half of the wavefronts
+            // ask behind their values)
+            const bool has = u >= u_begin - 1 && u + 1 < u_end, late = wave >= NW / 2;
+            if (!late) ask();
+            if (u >= u_begin) rescale();
+            if (has && !late) logits(scan());
+            if (u >= u_begin) values();
+            if (late) {
+                ask();
+                const uint32_t bad = has ? scan() : 0u;
+                if (M == 128 && has) logits(bad);
+            }
+            // (what was read a turn ago is used again in the next)
+            if (was_edge && threadIdx.x == 0) bad_lds[odd] = 0u;
+            if (was_moved && threadIdx.x == 0) moved_lds[third == 0 ? 2 : third - 1] = 0u;
+            was_edge = has && edge;
+            was_moved = u >= u_begin && __builtin_amdgcn_readfirstlane(moved_word) != 0u;
+            // tile u + 2 is there, tile u + 3 may be on its way
+            if (loads == TW * DC / 512 + 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(TW * DC / 512 + 1) : "memory");
+            else wait_loads(loads);
+            if (width2 != 16 && u + 2 < u_end && u + 2 >= u_begin) unpack(u + 2, width2, valid2);
+            third = next_third;
         }
         int lane = lane0;
         asm volatile("" : "+v"(lane));
         const int l16 = lane & 15, g4 = lane >> 4;
         // the share: o[b][d][e] is latent (wave * DB + d) * 16 + 4 g4 + e of row b * 16 + l16
-        const int64_t slot = (blockIdx.x + static_cast<int64_t>(s) * g.row_tiles + rt) * M;
+        const LatentAttendArgs* a1 = here();
+        float *part_o = a1->part_o, *part_ml = a1->part_ml;
+        const int64_t slot = (blockIdx.x + static_cast<int64_t>(s) * a1->g.row_tiles + rt) * M;
         const int here = min(M, sw.rows - rt * M);
 #pragma unroll
         for (int b = 0; b < MB; ++b)
@@ -581,126 +696,153 @@ __global__ __launch_bounds__(256, 2) void latent_attend_kernel(LatentView v, Lat
                     *reinterpret_cast<lf4_t*>(part_o + (slot + b * 16 + l16) * DC + (wave * DB + d) * 16 + 4 * g4) = o[b][d];
             }
         if (wave < kWaves) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                float l = sum[b] + __shfl_xor(sum[b], 16);
-                l += __shfl_xor(l, 32);
-                const int row = (wave * RB + b) * 16 + l16;
-                if (g4 == 0 && row < here) *reinterpret_cast<float2*>(part_ml + (slot + row) * 2) = float2{ref[b], l};
-            }
+            float l = sum + __shfl_xor(sum, 16);
+            l += __shfl_xor(l, 32);
+            const int row = wave * 16 + l16;
+            if (g4 == 0 && row < here) *reinterpret_cast<float2*>(part_ml + (slot + row) * 2) = float2{ref, l};
         }
     }
 }
 
-// The shares of a row joined and its values made: out[h] = w_v[h]^T (sum of shares / sum of their weights), for ROWS rows of one head in a
-// workgroup.  The joined latents enter the product as the sum of two halves, 22 bits, which costs nothing next to reading shares and w.
-// Grid (H, row blocks), 256 threads.
-template <int DC, int DV, int ROWS>
-__global__ __launch_bounds__(256) void latent_project_kernel(LatentView v, LatentGeom g, const _Float16* __restrict__ w,
-                                                             const int32_t* __restrict__ row_start, const int32_t* __restrict__ line,
-                                                             const float* __restrict__ part_o, const float* __restrict__ part_ml,
-                                                             _Float16* __restrict__ out) {
-    constexpr int kPitch = DC + 8, kSplit = 256 / DV;               // wavefronts that share a column's contraction
-    extern __shared__ float weights[];                              // [4][groups]
-    __shared__ __attribute__((aligned(16))) _Float16 joined[2][ROWS][kPitch];
-    __shared__ lf4_t sums[4][16][16];
-    __shared__ int32_t to[ROWS];
-    const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+// The shares of a query row joined: their sum over the sum of their weights, as the sum of two halves (22 bits, so that the product behind it
+// is not the result's largest error), hi and lo [n_seqs * max_rows][H][DC] each.  Latency bounds it, row, line, weights and shares being loads that
+// wait for each other, and reading the shares.  PER wavefronts share a row, 4 / PER rows are a workgroup's.
+template <int DC, int PER>
+__global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGeom g, const int32_t* __restrict__ row_start,
+                                                          const int32_t* __restrict__ line, const float* __restrict__ part_o,
+                                                          const float* __restrict__ part_ml, _Float16* __restrict__ hi, _Float16* __restrict__ lo) {
+    extern __shared__ float weights[];                              // [4 / PER][groups]
+    __shared__ lf4_t parts[PER > 1 ? PER : 1][PER > 1 ? DC / 4 : 1];
+    const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int h = static_cast<int>(blockIdx.x);
-    const LatentLine ll = *reinterpret_cast<const LatentLine*>(line);
-    float* weight = weights + wave * g.groups;
-    for (int i = wave; i < ROWS; i += 4) {
-        const int64_t nr = static_cast<int64_t>(blockIdx.y) * ROWS + i;
-        const int s = static_cast<int>(nr / g.max_rows), nth = static_cast<int>(nr - static_cast<int64_t>(s) * g.max_rows);
-        const LatentSeq sw = latent_seq(v, g, row_start, s);
-        const bool ok = nth < min(sw.count, g.max_rows);
-        if (lane == 0) to[i] = ok ? sw.first + nth : -1;
-        lf4_t x[DC / 256];
+    const int nth_wave = wave % PER;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * (4 / PER) + wave / PER;
+    const int row = static_cast<int>(at / g.H), h = static_cast<int>(at - static_cast<int64_t>(row) * g.H);
+    const int s = row / g.max_rows, nth = row - s * g.max_rows;
+    float* weight = weights + wave / PER * g.groups;
+    const int run = line[0];
+    const LatentSeq sw = latent_seq(v, g, row_start, s);
+    const bool ok = nth < min(sw.count, g.max_rows);
+    if (!ok) return;                                                // (uniform: where wavefronts share a row, for all of them)
+    lf4_t x[DC / 256];
 #pragma unroll
-        for (int k = 0; k < DC / 256; ++k) x[k] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        float total = 0.0f;
-        if (ok && sw.units > 0) {
-            const int M = 1 << g.tile_log2, j = nth * g.H + h, rt = j >> g.tile_log2, each = attend_places(sw.units, ll.round, ll.cost);
-            const int begin = line[4 + s] - each * (sw.row_tiles - rt) + ll.cost, wg = begin / ll.run;
-            const int used = (begin + sw.units - 1) / ll.run - wg + 1;
-            const int64_t first = (wg + static_cast<int64_t>(s) * g.row_tiles + rt) * M + (j & (M - 1));
-            float ref = -INFINITY;
-            for (int k = lane; k < used; k += 64) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * M) * 2]);
+    for (int k = 0; k < DC / 256; ++k) x[k] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    float total = 0.0f;
+    if (sw.units > 0) {
+        const int M = 1 << g.tile_log2, j = nth * g.H + h, rt = j >> g.tile_log2;
+        const int begin = line[4 + s] - latent_places(sw.units) * (sw.row_tiles - rt) + kLatentCost, wg = begin / run;
+        const int used = (begin + sw.units - 1) / run - wg + 1;
+        const int64_t first = (wg + static_cast<int64_t>(s) * g.row_tiles + rt) * M + (j & (M - 1));
+        // (the wavefronts of a row all work the weights out, each writes and reads the same)
+        float ref = -INFINITY;
+        for (int k = lane; k < used; k += 64) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * M) * 2]);
 #pragma unroll
-            for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
-            for (int k = lane; k < used; k += 64) {
-                const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * M) * 2);
-                const float f = ml.x == -INFINITY ? 0.0f : ml.x == ref ? 1.0f : __builtin_amdgcn_exp2f(ml.x - ref);
-                weight[k] = f;
-                total += f * ml.y;
-            }
-#pragma unroll
-            for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const float* src = part_o + first * DC + lane * 4;
-#pragma unroll 4
-            for (int k = 0; k < used; ++k) {
-                const float f = weight[k];
-#pragma unroll
-                for (int c = 0; c < DC / 256; ++c) x[c] += *reinterpret_cast<const lf4_t*>(src + static_cast<int64_t>(k) * M * DC + c * 256) * f;
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int d = 32; d; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+        for (int k = lane; k < used; k += 64) {
+            const float2 ml = *reinterpret_cast<const float2*>(part_ml + (first + static_cast<int64_t>(k) * M) * 2);
+            const float f = ml.x == -INFINITY ? 0.0f : ml.x == ref ? 1.0f : __builtin_amdgcn_exp2f(ml.x - ref);
+            weight[k] = f;
+            total += f * ml.y;
         }
-        const float inv = total > 0.0f ? 1.0f / total : total;       // a row that sees nothing: zeros; NaN stays
 #pragma unroll
-        for (int c = 0; c < DC / 256; ++c) {
-            lh4_t hi, lo;
+        for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const float* src = part_o + first * DC + lane * 4;
+        for (int k0 = nth_wave; k0 < used; k0 += 8 * PER) {
+            lf4_t y[8][DC / 256];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y = x[c][e] * inv;
-                hi[e] = static_cast<_Float16>(y);
-                lo[e] = static_cast<_Float16>(y - static_cast<float>(hi[e]));
-            }
-            *reinterpret_cast<lh4_t*>(&joined[0][i][lane * 4 + c * 256]) = hi;
-            *reinterpret_cast<lh4_t*>(&joined[1][i][lane * 4 + c * 256]) = lo;
+            for (int k = 0; k < 8; ++k)                              // (behind the last share it is read again, for nothing)
+#pragma unroll
+                for (int c = 0; c < DC / 256; ++c)
+                    y[k][c] = *reinterpret_cast<const lf4_t*>(src + static_cast<int64_t>(min(k0 + k * PER, used - 1)) * M * DC + c * 256);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k0 + k * PER < used) {
+                    const float f = weight[k0 + k * PER];
+#pragma unroll
+                    for (int c = 0; c < DC / 256; ++c) x[c] += y[k][c] * f;
+                }
         }
     }
-    __syncthreads();
-    // 64 columns and a share of the contraction per wavefront: a lane loads four adjacent columns of eight latents, column 4 l16 + n is
-    // row l16 of the n-th product's operand
-    const int col0 = DV == 128 ? (wave & 1) * 64 : 0, split = DV == 128 ? wave >> 1 : wave;
+    if constexpr (PER > 1) {
+#pragma unroll
+        for (int c = 0; c < DC / 256; ++c) parts[nth_wave][lane + c * 64] = x[c];
+        __syncthreads();
+        if (nth_wave) return;
+#pragma unroll
+        for (int k = 1; k < PER; ++k)
+#pragma unroll
+            for (int c = 0; c < DC / 256; ++c) x[c] += parts[k][lane + c * 64];
+    }
+    const float inv = total > 0.0f ? 1.0f / total : total;           // a row that sees nothing: zeros; NaN stays
+#pragma unroll
+    for (int c = 0; c < DC / 256; ++c) {
+        lh4_t a, b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float y = x[c][e] * inv;
+            a[e] = static_cast<_Float16>(y);
+            b[e] = static_cast<_Float16>(y - static_cast<float>(a[e]));
+        }
+        *reinterpret_cast<lh4_t*>(hi + at * DC + lane * 4 + c * 256) = a;
+        *reinterpret_cast<lh4_t*>(lo + at * DC + lane * 4 + c * 256) = b;
+    }
+}
+
+// Values from joined latents: out[h] = w_v[h]^T (hi + lo) for 16 rows of one head and 64 of its columns in a workgroup, whose wavefronts have a
+// quarter of the contraction each.  Bound by reading w: a lane loads four adjacent columns of eight latents, column 4 l16 + n is row l16 of the
+// n-th product's operand.  Grid (H * DV / 64, row blocks), 256 threads.
+template <int DC, int DV>
+__global__ __launch_bounds__(256) void latent_values_kernel(LatentView v, LatentGeom g, const _Float16* __restrict__ w,
+                                                            const int32_t* __restrict__ row_start, const _Float16* __restrict__ hi,
+                                                            const _Float16* __restrict__ lo, _Float16* __restrict__ out) {
+    constexpr int kSteps = DC / 32 / 4;
+    __shared__ lf4_t sums[4][16][17];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int h = static_cast<int>(blockIdx.x) / (DV / 64), col0 = static_cast<int>(blockIdx.x) % (DV / 64) * 64;
+    const int row0 = static_cast<int>(blockIdx.y) * 16, all = v.p.n_seqs * g.max_rows;
     const int64_t w_row = static_cast<int64_t>(g.H) * (g.Dk + DV);
-    const _Float16* w_at = w + static_cast<int64_t>(h) * (g.Dk + DV) + g.Dk + col0 + 4 * l16;
+    const int c0 = wave * (DC / 4) + 8 * g4;
+    const _Float16* w_at = w + static_cast<int64_t>(h) * (g.Dk + DV) + g.Dk + col0 + 4 * l16 + c0 * w_row;
+    const int64_t from = (static_cast<int64_t>(min(row0 + l16, all - 1)) * g.H + h) * DC + c0;
+    u2_t wx[kSteps][8];
+    h8_t a[kSteps], b[kSteps];
+#pragma unroll
+    for (int k = 0; k < kSteps; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) wx[k][e] = *reinterpret_cast<const u2_t*>(w_at + (k * 32 + e) * w_row);
+        a[k] = *reinterpret_cast<const h8_t*>(hi + from + k * 32);
+        b[k] = *reinterpret_cast<const h8_t*>(lo + from + k * 32);
+    }
     lf4_t acc[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) acc[n] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kLen = DC / kSplit;
-    for (int k = split * kLen; k < (split + 1) * kLen; k += 32) {
-        const int c0 = k + 8 * g4;
-        u2_t x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const u2_t*>(w_at + (c0 + e) * w_row);
-        const h8_t hi = *reinterpret_cast<const h8_t*>(&joined[0][l16 % ROWS][c0]), lo = *reinterpret_cast<const h8_t*>(&joined[1][l16 % ROWS][c0]);
+    for (int k = 0; k < kSteps; ++k)
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
             u4_t f;
 #pragma unroll
-            for (int p = 0; p < 4; ++p) f[p] = __builtin_amdgcn_perm(x[2 * p + 1][n / 2], x[2 * p][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
-            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, f), lo, acc[n], 0, 0, 0);
-            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, f), hi, acc[n], 0, 0, 0);
+            for (int p = 0; p < 4; ++p)
+                f[p] = __builtin_amdgcn_perm(wx[k][2 * p + 1][n / 2], wx[k][2 * p][n / 2], n % 2 ? 0x07060302u : 0x05040100u);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, f), b[k], acc[n], 0, 0, 0);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, f), a[k], acc[n], 0, 0, 0);
         }
-    }
     // acc[n][e]: column col0 + 4 (4 g4 + e) + n of row l16
 #pragma unroll
     for (int e = 0; e < 4; ++e) sums[wave][4 * g4 + e][l16] = lf4_t{acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
     __syncthreads();
-    for (int i = threadIdx.x; i < ROWS * (DV / 4); i += 256) {
-        const int row = i / (DV / 4), quad = i % (DV / 4), wv = DV == 128 ? quad / 16 : 0;
-        if (to[row] < 0) continue;
-        lf4_t x = sums[wv][quad % 16][row];
+    const int r = static_cast<int>(threadIdx.x) / 16, quad = static_cast<int>(threadIdx.x) % 16, row = row0 + r;
+    if (row >= all) return;
+    const int s = row / g.max_rows, nth = row - s * g.max_rows;
+    const SeqRows rows = seq_rows(row_start, s, g.n_rows);
+    if (nth >= min(rows.count, g.max_rows)) return;
+    const lf4_t x = (sums[0][quad][r] + sums[1][quad][r]) + (sums[2][quad][r] + sums[3][quad][r]);
+    lh4_t y;
 #pragma unroll
-        for (int k = 1; k < kSplit; ++k) x += sums[wv + k * (4 / kSplit)][quad % 16][row];
-        lh4_t y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = static_cast<_Float16>(x[e]);
-        *reinterpret_cast<lh4_t*>(out + (static_cast<int64_t>(to[row]) * g.H + h) * DV + 4 * quad) = y;
-    }
+    for (int e = 0; e < 4; ++e) y[e] = static_cast<_Float16>(x[e]);
+    *reinterpret_cast<lh4_t*>(out + (static_cast<int64_t>(rows.first + nth) * g.H + h) * DV + col0 + 4 * quad) = y;
 }
 
 }  // namespace kvs

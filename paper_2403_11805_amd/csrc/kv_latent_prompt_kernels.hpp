@@ -147,9 +147,11 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
     const uint8_t* keys = reinterpret_cast<const uint8_t*>(kv) + static_cast<int64_t>(base) * kLatentTile * kv_row + h * ((DK + DV) * 2);
     const uint8_t* rope = reinterpret_cast<const uint8_t*>(ropes) + static_cast<int64_t>(base) * kLatentTile * (DR * 2);
     const uint8_t* have = there + base * 2;
-    auto swz = [](int token, int pieces) __attribute__((always_inline)) {
-        return pieces == 4 ? (token >> 1) & 3 : latent_swizzle(token) & (pieces - 1);
+    // permutations of a row's pieces (see latent_swizzle; a read of keys has one piece of 32 tokens here, one of values four pieces of four)
+    auto key_swz = [](int token, int pieces) __attribute__((always_inline)) {
+        return pieces == 16 ? token & 15 : pieces == 8 ? (token >> 1) & 7 : (token >> 2) & 3;
     };
+    auto value_swz = [](int token, int pieces) __attribute__((always_inline)) { return pieces == 16 ? (token & 3) << 2 : (token & 2) << 1; };
     constexpr int kLoads = (DK + DV) / 64 + 1;                             // of a wavefront for a tile
     auto fetch = [&](int tile, int buf) __attribute__((always_inline)) {
         uint8_t* to = lds + buf * kTileBytes;
@@ -158,16 +160,19 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
 #pragma unroll
         for (int i = 0; i < DK / 64; ++i) {
             const int p = (i * 4 + wave) * 64 + lane, tk = p / kk, slot = p % kk;
-            to_lds(from, static_cast<uint32_t>(tk * kv_row + ((slot ^ swz(tk, kk)) << 4)), to + (i * 4 + wave) * 1024);
+            lds_place(to + (i * 4 + wave) * 1024);
+            to_lds(from, static_cast<uint32_t>(tk * kv_row + ((slot ^ key_swz(tk, kk)) << 4)));
         }
         {
             const int i = DR == 64 ? wave : wave & 1, p = i * 64 + lane, tk = p / kr, slot = p % kr;
-            to_lds(rope + static_cast<int64_t>(tile) * (kLatentTile * DR * 2), static_cast<uint32_t>(tk * (DR * 2) + ((slot ^ swz(tk, kr)) << 4)), to + kRopeAt + i * 1024);
+            lds_place(to + kRopeAt + i * 1024);
+            to_lds(rope + static_cast<int64_t>(tile) * (kLatentTile * DR * 2), static_cast<uint32_t>(tk * (DR * 2) + ((slot ^ key_swz(tk, kr)) << 4)));
         }
 #pragma unroll
         for (int i = 0; i < DV / 64; ++i) {
             const int p = (i * 4 + wave) * 64 + lane, tk = p / kv_, slot = p % kv_;
-            to_lds(from, static_cast<uint32_t>(tk * kv_row + DK * 2 + ((slot ^ swz(tk, kv_)) << 4)), to + kValueAt + (i * 4 + wave) * 1024);
+            lds_place(to + kValueAt + (i * 4 + wave) * 1024);
+            to_lds(from, static_cast<uint32_t>(tk * kv_row + DK * 2 + ((slot ^ value_swz(tk, kv_)) << 4)));
         }
     };
     lf16_t o[VB];
@@ -195,8 +200,8 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         for (int e = 0; e < 16; ++e) sc[e] = 0.0f;
 #pragma unroll
         for (int k = 0; k < KS + KR; ++k) {
-            const uint8_t* p = k < KS ? at + l32 * (DK * 2) + (((2 * k + half) ^ swz(l32, DK / 8)) << 4)
-                                      : at + kRopeAt + l32 * (DR * 2) + (((2 * (k - KS) + half) ^ swz(l32, DR / 8)) << 4);
+            const uint8_t* p = k < KS ? at + l32 * (DK * 2) + (((2 * k + half) ^ key_swz(l32, DK / 8)) << 4)
+                                      : at + kRopeAt + l32 * (DR * 2) + (((2 * (k - KS) + half) ^ key_swz(l32, DR / 8)) << 4);
             sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc, 0, 0, 0);
         }
         // sc[e]: token 8 (e / 4) + 4 half + e % 4 against this lane's row
@@ -249,8 +254,8 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
                 const int tk = 16 * st + 4 * half + ((lane & 15) >> 2), piece = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                const uint8_t* lo_at = at + kValueAt + tk * (DV * 2) + ((piece ^ swz(tk, DV / 8)) << 4) + (lane & 1) * 8;
-                const uint8_t* hi_at = at + kValueAt + (tk + 8) * (DV * 2) + ((piece ^ swz(tk + 8, DV / 8)) << 4) + (lane & 1) * 8;
+                const uint8_t* lo_at = at + kValueAt + tk * (DV * 2) + ((piece ^ value_swz(tk, DV / 8)) << 4) + (lane & 1) * 8;
+                const uint8_t* hi_at = at + kValueAt + (tk + 8) * (DV * 2) + ((piece ^ value_swz(tk + 8, DV / 8)) << 4) + (lane & 1) * 8;
                 const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(lo_at));
                 const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(hi_at));
                 const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
