@@ -324,7 +324,20 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
     const int run_end = at + run;
     const int n_seqs = args.v.p.n_seqs;
     int s = -1, s_end = 0;
+    LatentSeq sw;
+    if (n_seqs <= 64) {
+        // the first piece's sequence: all there is to know of up to 64 comes together, a sequence per lane, in one trip to memory
+        const LatentSeq of_lane = latent_seq(args.v, args.g, args.row_start, lane0);
+        const int end_of_lane = line[4 + min(lane0, n_seqs - 1)];
+        const uint64_t any = __ballot(lane0 < n_seqs && end_of_lane > at);
+        if (!any) return;                                       // behind the end of the line
+        s = __builtin_ctzll(any);
+        s_end = __builtin_amdgcn_readlane(end_of_lane, s);
+        sw = {__builtin_amdgcn_readlane(of_lane.n, s),    __builtin_amdgcn_readlane(of_lane.first, s),     __builtin_amdgcn_readlane(of_lane.count, s),
+              __builtin_amdgcn_readlane(of_lane.rows, s), __builtin_amdgcn_readlane(of_lane.row_tiles, s), __builtin_amdgcn_readlane(of_lane.units, s)};
+    }
     while (at < run_end) {
+        const LatentAttendArgs* a0 = here();
         // the sequence in whose work place `at` lies: the first that ends behind it
         if (at >= s_end) {
             int lo = s + 1, n = n_seqs - lo;
@@ -340,34 +353,15 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
             if (!any) return;                                   // the end of the line
             s = __builtin_amdgcn_readfirstlane(lo + __builtin_ctzll(any));
             s_end = __builtin_amdgcn_readfirstlane(line[4 + s]);
+            sw = latent_seq(a0->v, a0->g, a0->row_start, s);
         }
-        const LatentAttendArgs* a0 = here();
-        const LatentSeq sw = latent_seq(a0->v, a0->g, a0->row_start, s);
         const int each = latent_places(sw.units), local = at - (s_end - each * sw.row_tiles);
         const int rt = local / each, place = local - rt * each, places = min(each - place, run_end - at);
         const int u_begin = max(place - kLatentCost, 0), u_end = place + places - kLatentCost;
         at += places;
         if (u_end <= u_begin) continue;
 
-        // this wavefront's rows: queries, what they see
         const int count = min(sw.count, a0->g.max_rows), H = a0->g.H;
-        h8_t qf[KS + KR];
-        int last = -1;
-        float ref = -INFINITY, sum = 0.0f;
-        if (wave < kWaves) {
-            int lane = lane0;
-            asm volatile("" : "+v"(lane));
-            const int l16 = lane & 15, g4 = lane >> 4;
-            const int j = rt * M + wave * 16 + l16, nth = j / H, h = j - nth * H;
-            const bool ok = j < sw.rows;
-            last = ok ? sw.n - sw.count + nth : -1;
-            const _Float16* lat = a0->qa + (static_cast<int64_t>(s) * a0->g.max_rows * H + (ok ? j : 0)) * DC + 8 * g4;
-            const _Float16* pos = a0->q + (sw.first + (ok ? nth : 0)) * a0->g.q_stride + (ok ? h : 0) * (a0->g.Dk + DR) + a0->g.Dk + 8 * g4;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const h8_t*>(lat + 32 * k);
-#pragma unroll
-                for (int k = 0; k < KR; ++k) qf[KS + k] = *reinterpret_cast<const h8_t*>(pos + 32 * k);
-        }
         const int all_see = sw.n - sw.count + rt * M / H;       // tokens up to this one are seen by every row
         const int none_sees = sw.n - sw.count + min(count, (rt * M + M - 1) / H + 1);
         lf4_t o[MB][DB];
@@ -391,22 +385,28 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
             const LatentView v = a->v;
             const uint64_t* offs = v.p.off + static_cast<int64_t>(s) * v.p.stride;
             const uint8_t* bits = v.p.bits + static_cast<int64_t>(s) * v.p.stride;
+            int page[2];
+            bool in[2];
+            uint64_t off[2];
+            uint32_t b[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int half = 2 * (u + lane) + i;
-                const bool in = (half * 16 < min(seq_n, none_sees)) & (u + lane < u_end);
+                in[i] = (half * 16 < min(seq_n, none_sees)) & (u + lane < u_end);
                 const int half_page = v.p.page_of_tile ? static_cast<int>(__umulhi(static_cast<uint32_t>(half), v.p.page_of_tile)) : half;
-                const int page = in ? half_page : 0;
-                const uint64_t off = offs[page];
-                const uint32_t b = bits[page], width = (in & latent_present(v, off, b)) ? b : 0u;
-                if (i == 0) have_low = __ballot(width != 0);
-                else have_high = __ballot(width != 0);
-                if (my_half == i) {
-                    tile_off = off;
-                    tile_width = width;
-                    tile_row = static_cast<uint32_t>(v.layer * v.p.T + half * 16 + my_token % 16 - page * v.p.T);
-                }
+                page[i] = in[i] ? half_page : 0;
+                off[i] = offs[page[i]];
+                b[i] = bits[page[i]];
             }
+            uint32_t width[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) width[i] = (in[i] & latent_present(v, off[i], b[i])) ? b[i] : 0u;
+            have_low = __ballot(width[0] != 0);
+            have_high = __ballot(width[1] != 0);
+            const bool second = my_half == 1;
+            tile_off = second ? off[1] : off[0];
+            tile_width = second ? width[1] : width[0];
+            tile_row = static_cast<uint32_t>(v.layer * v.p.T + (2 * (u + lane) + my_half) * 16 + my_token % 16 - (second ? page[1] : page[0]) * v.p.T);
         };
         // Asks for tile u.  Whole rows and position parts come as they stay, those of tokens that are not there from the zeros.
         int loads = 0, width1 = 16, valid1 = 0;                 // of the tile that was asked for last: the loads, what this wavefront has of it,
@@ -493,6 +493,24 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
         };
 
         look_up(u_begin);
+        // this wavefront's rows: queries, what they see
+        h8_t qf[KS + KR];
+        int last = -1;
+        float ref = -INFINITY, sum = 0.0f;
+        if (wave < kWaves) {
+            int lane = lane0;
+            asm volatile("" : "+v"(lane));
+            const int l16 = lane & 15, g4 = lane >> 4;
+            const int j = rt * M + wave * 16 + l16, nth = j / H, h = j - nth * H;
+            const bool ok = j < sw.rows;
+            last = ok ? sw.n - sw.count + nth : -1;
+            const _Float16* lat = a0->qa + (static_cast<int64_t>(s) * a0->g.max_rows * H + (ok ? j : 0)) * DC + 8 * g4;
+            const _Float16* pos = a0->q + (sw.first + (ok ? nth : 0)) * a0->g.q_stride + (ok ? h : 0) * (a0->g.Dk + DR) + a0->g.Dk + 8 * g4;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const h8_t*>(lat + 32 * k);
+#pragma unroll
+                for (int k = 0; k < KR; ++k) qf[KS + k] = *reinterpret_cast<const h8_t*>(pos + 32 * k);
+        }
         __syncthreads();                                        // (the piece before is done with LDS)
         if (threadIdx.x < 2) bad_lds[threadIdx.x] = 0u;
         if (threadIdx.x < 3) moved_lds[threadIdx.x] = 0u;
