@@ -110,13 +110,13 @@ struct PromptSpace {
 };
 int64_t prompt_tiles(int32_t n_seqs, int64_t n_tokens) { return n_tokens / kLatentTile + std::min<int64_t>(n_seqs, n_tokens); }
 PromptSpace prompt_space(const kv_latent_shape_t& s, int32_t n_seqs, int64_t n_tokens) {
-    const uint64_t rows = static_cast<uint64_t>(prompt_tiles(n_seqs, n_tokens)) * kLatentTile;
+    const uint64_t rows = (static_cast<uint64_t>(prompt_tiles(n_seqs, n_tokens)) + 1) * kLatentTile;      // (a turn may reach a tile past the last)
     PromptSpace w;
     w.kv = 0;
     w.latents = w.kv + up256(rows * s.n_heads * (s.key_dim + s.value_dim) * 2);
     w.ropes = w.latents + up256(rows * s.latent_dim * 2);
     w.there = w.ropes + up256(rows * s.rope_dim * 2);
-    w.table = w.there + up256(rows / 16);
+    w.table = w.there + up256(rows / 8);
     w.all = w.table + up256(static_cast<uint64_t>(n_seqs) * 8);
     return w;
 }
@@ -311,7 +311,7 @@ int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_
     _Float16* kv = reinterpret_cast<_Float16*>(space + sp.kv);
     _Float16* latents = reinterpret_cast<_Float16*>(space + sp.latents);
     _Float16* ropes = reinterpret_cast<_Float16*>(space + sp.ropes);
-    uint8_t* there = space + sp.there;
+    uint32_t* there = reinterpret_cast<uint32_t*>(space + sp.there);
     PromptTable table;
     table.tile_end = reinterpret_cast<int32_t*>(space + sp.table);
     table.row_end = table.tile_end + n_seqs;

@@ -66,11 +66,11 @@ __device__ __forceinline__ int first_behind(const int32_t* __restrict__ end, int
     return any ? lo + __builtin_ctzll(any) : -1;
 }
 
-// A tile of 32 tokens from their pages: latents in the product's fragment order, position parts row-major, whether each half's page is
-// there; tokens that are not there are zeros.
+// A tile of 32 tokens from their pages: latents in the product's fragment order, position parts row-major, which halves' pages are there
+// (bits 0 and 1); tokens that are not there are zeros.
 template <int DC, int DR>
 __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, PromptGeom g, PromptTable t, int32_t lpg_log2, _Float16* __restrict__ latents,
-                                                            _Float16* __restrict__ ropes, uint8_t* __restrict__ there) {
+                                                            _Float16* __restrict__ ropes, uint32_t* __restrict__ there) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int tile = static_cast<int>(blockIdx.x);
     const int s = __builtin_amdgcn_readfirstlane(first_behind(t.tile_end, v.p.n_seqs, tile, lane));
@@ -82,7 +82,10 @@ __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, Prompt
     const uint64_t off = v.p.off[entry];
     const int b = v.p.bits[entry];
     const bool have = token0 < n && latent_present(v, off, b);
-    if (threadIdx.x % 128 == 0) there[tile * 2 + (wave >> 1)] = have ? 1 : 0;
+    __shared__ uint32_t halves[2];
+    if (threadIdx.x % 128 == 0) halves[wave >> 1] = have ? 1u << (wave >> 1) : 0u;
+    __syncthreads();
+    if (threadIdx.x == 0) there[tile] = halves[0] | halves[1];
     // a lane has one token and every eighth piece, so that sixteen tokens' pieces are written side by side
     const int tk = (wave >> 1) * 16 + (lane & 15), token = token0 + (lane & 15);
     const bool ok = have && token < n;
@@ -104,15 +107,18 @@ __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, Prompt
     }
 }
 
-// Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them.
+// Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them, and takes
+// 64 tokens a turn, two independent products S^T = K Q^T of 32 tokens each.  Keys and values go straight to LDS, the next turn's while this one's
+// are used.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
+constexpr int kPromptTile = 64;
 template <int DK, int DR, int DV>
 __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, PromptGeom g, PromptTable t, const int32_t* __restrict__ row_start,
                                                                const _Float16* __restrict__ q, const _Float16* __restrict__ kv,
-                                                               const _Float16* __restrict__ ropes, const uint8_t* __restrict__ there,
+                                                               const _Float16* __restrict__ ropes, const uint32_t* __restrict__ there,
                                                                _Float16* __restrict__ out) {
-    constexpr int kRopeAt = kLatentTile * DK * 2, kValueAt = kRopeAt + kLatentTile * DR * 2, kTileBytes = kValueAt + kLatentTile * DV * 2;
-    constexpr int KS = DK / 16, KR = DR / 16, VB = DV / 32, kBufs = 3;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kBufs * kTileBytes];
+    constexpr int kRopeAt = kPromptTile * DK * 2, kValueAt = kRopeAt + kPromptTile * DR * 2, kTileBytes = kValueAt + kPromptTile * DV * 2;
+    constexpr int KS = DK / 16, KR = DR / 16, VB = DV / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes];
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     // workgroups are dealt to the eight XCDs in turn: those of a head go to one of them, whose L2 then holds its keys and values
@@ -134,45 +140,63 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
     const bool ok = m < rows.count;
     const int behind = n - rows.count;                                     // the token of row 0
     const int pos = ok ? behind + m : -1;
-    const int min_pos = behind + row0 + wave * 32, max_pos = behind + min(row0 + wave * 32 + 31, rows.count - 1);
+    const bool idle = row0 + wave * 32 >= rows.count;                       // (a wavefront without rows)
+    const int min_pos = idle ? -1 : behind + row0 + wave * 32, max_pos = idle ? -1 : behind + min(row0 + wave * 32 + 31, rows.count - 1);
     const int end_pos = behind + min(row0 + kPromptRows, rows.count) - 1;  // of the workgroup's last row
-    const int n_tiles = end_pos < 0 ? 0 : end_pos / kLatentTile + 1;
+    const int n_tiles = end_pos < 0 ? 0 : end_pos / kPromptTile + 1;
     h8_t qf[KS + KR];
     {
         const _Float16* from = q + (rows.first + (ok ? m : 0)) * g.q_stride + h * (DK + DR) + 8 * half;
 #pragma unroll
         for (int k = 0; k < KS + KR; ++k) qf[k] = *reinterpret_cast<const h8_t*>(from + 16 * k);
     }
-    const int64_t kv_row = static_cast<int64_t>(g.H) * (DK + DV) * 2;
+    const uint32_t kv_row = static_cast<uint32_t>(g.H) * (DK + DV) * 2;
     const uint8_t* keys = reinterpret_cast<const uint8_t*>(kv) + static_cast<int64_t>(base) * kLatentTile * kv_row + h * ((DK + DV) * 2);
     const uint8_t* rope = reinterpret_cast<const uint8_t*>(ropes) + static_cast<int64_t>(base) * kLatentTile * (DR * 2);
-    const uint8_t* have = there + base * 2;
     // permutations of a row's pieces (see latent_swizzle; a read of keys has one piece of 32 tokens here, one of values four pieces of four)
     auto key_swz = [](int token, int pieces) __attribute__((always_inline)) {
         return pieces == 16 ? token & 15 : pieces == 8 ? (token >> 1) & 7 : (token >> 2) & 3;
     };
     auto value_swz = [](int token, int pieces) __attribute__((always_inline)) { return pieces == 16 ? (token & 3) << 2 : (token & 2) << 1; };
-    constexpr int kLoads = (DK + DV) / 64 + 1;                             // of a wavefront for a tile
-    auto fetch = [&](int tile, int buf) __attribute__((always_inline)) {
-        uint8_t* to = lds + buf * kTileBytes;
-        const uint8_t* from = keys + static_cast<int64_t>(tile) * kLatentTile * kv_row;
-        constexpr int kk = DK / 8, kv_ = DV / 8, kr = DR / 8;
+    // Where a lane's piece lies in memory, for the loads of a wavefront's quarter of the tile, one after the other in LDS (1 KB each, which the
+    // load's own offset adds on both sides).
+    constexpr int kk = DK / 8, kv_ = DV / 8, kr = DR / 8, kRopeLoads = DR / 32;
+    uint32_t key_at_[DK / 32], rope_at_[kRopeLoads], value_at_[DV / 32];
 #pragma unroll
-        for (int i = 0; i < DK / 64; ++i) {
-            const int p = (i * 4 + wave) * 64 + lane, tk = p / kk, slot = p % kk;
-            lds_place(to + (i * 4 + wave) * 1024);
-            to_lds(from, static_cast<uint32_t>(tk * kv_row + ((slot ^ key_swz(tk, kk)) << 4)));
-        }
-        {
-            const int i = DR == 64 ? wave : wave & 1, p = i * 64 + lane, tk = p / kr, slot = p % kr;
-            lds_place(to + kRopeAt + i * 1024);
-            to_lds(rope + static_cast<int64_t>(tile) * (kLatentTile * DR * 2), static_cast<uint32_t>(tk * (DR * 2) + ((slot ^ key_swz(tk, kr)) << 4)));
-        }
+    for (int i = 0; i < DK / 32; ++i) {
+        const int p = (wave * (DK / 32) + i) * 64 + lane, tk = p / kk;
+        key_at_[i] = tk * kv_row + ((p % kk ^ key_swz(tk, kk)) << 4) - i * 1024;
+    }
 #pragma unroll
-        for (int i = 0; i < DV / 64; ++i) {
-            const int p = (i * 4 + wave) * 64 + lane, tk = p / kv_, slot = p % kv_;
-            lds_place(to + kValueAt + (i * 4 + wave) * 1024);
-            to_lds(from, static_cast<uint32_t>(tk * kv_row + DK * 2 + ((slot ^ value_swz(tk, kv_)) << 4)));
+    for (int i = 0; i < kRopeLoads; ++i) {
+        const int p = (wave * kRopeLoads + i) * 64 + lane, tk = p / kr;
+        rope_at_[i] = static_cast<uint32_t>(tk * (DR * 2) + ((p % kr ^ key_swz(tk, kr)) << 4) - i * 1024);
+    }
+#pragma unroll
+    for (int i = 0; i < DV / 32; ++i) {
+        const int p = (wave * (DV / 32) + i) * 64 + lane, tk = p / kv_;
+        value_at_[i] = tk * kv_row + DK * 2 + ((p % kv_ ^ value_swz(tk, kv_)) << 4) - i * 1024;
+    }
+    auto fetch = [&](int tile) __attribute__((always_inline)) {
+        uint8_t* to = lds + (tile & 1) * kTileBytes;
+        const uint8_t* from = keys + static_cast<int64_t>(tile) * (kPromptTile * static_cast<int64_t>(kv_row));
+        const uint8_t* rope_at = rope + static_cast<int64_t>(tile) * (kPromptTile * DR * 2) ;
+        lds_place(to + wave * (DK * 32));
+        to_lds(from, key_at_[0]);
+        to_lds<1024>(from, key_at_[1]);
+        if constexpr (DK == 128) {
+            to_lds<2048>(from, key_at_[2]);
+            to_lds<3072>(from, key_at_[3]);
+        }
+        lds_place(to + kRopeAt + wave * (DR * 32));
+        to_lds(rope_at, rope_at_[0]);
+        if constexpr (DR == 64) to_lds<1024>(rope_at, rope_at_[1]);
+        lds_place(to + kValueAt + wave * (DV * 32));
+        to_lds(from, value_at_[0]);
+        to_lds<1024>(from, value_at_[1]);
+        if constexpr (DV == 128) {
+            to_lds<2048>(from, value_at_[2]);
+            to_lds<3072>(from, value_at_[3]);
         }
     };
     lf16_t o[VB];
@@ -181,60 +205,73 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
     float ref = -INFINITY, sum = 0.0f;
-    if (n_tiles > 0) {
-        fetch(0, 0);
-        fetch(min(1, n_tiles - 1), 1);
-    }
-    int buf = 0;
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        const bool have0 = have[2 * tile] != 0, have1 = have[2 * tile + 1] != 0;
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-        const int next2 = buf == 0 ? 2 : buf - 1;
-        fetch(min(tile + 2, n_tiles - 1), next2);
-        const uint8_t* at = lds + buf * kTileBytes;
-        buf = buf == 2 ? 0 : buf + 1;
-        const int token0 = tile * kLatentTile;
-        if (token0 > max_pos) continue;                                    // (uniform; behind all of this wavefront's rows)
-        lf16_t sc;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sc[e] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < KS + KR; ++k) {
-            const uint8_t* p = k < KS ? at + l32 * (DK * 2) + (((2 * k + half) ^ key_swz(l32, DK / 8)) << 4)
-                                      : at + kRopeAt + l32 * (DR * 2) + (((2 * (k - KS) + half) ^ key_swz(l32, DR / 8)) << 4);
-            sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc, 0, 0, 0);
+    if (n_tiles > 0) fetch(0);
+    const uint32_t* have_at = there + base;
+    uint32_t have_next = n_tiles > 0 ? have_at[0] | have_at[1] << 2 : 0u;
+    // A turn: EDGE, if some of its tokens may be behind some of the wavefront's rows.
+    auto turn = [&](int tile, auto EDGE) __attribute__((always_inline)) {
+        constexpr bool edge = decltype(EDGE)::value;
+        const uint32_t have = have_next;                                    // of the four times 16 tokens
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (tile + 1 < n_tiles) {
+            fetch(tile + 1);
+            have_next = have_at[2 * tile + 2] | have_at[2 * tile + 3] << 2;
         }
-        // sc[e]: token 8 (e / 4) + 4 half + e % 4 against this lane's row
-        const bool edge = token0 + kLatentTile - 1 > min_pos;
-        uint32_t bad = 0u;
-        if (edge) {
+        const uint8_t* at = lds + (tile & 1) * kTileBytes;
+        const int token0 = tile * kPromptTile;
+        if (edge && token0 > max_pos) return;                              // (uniform; behind all of this wavefront's rows)
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int tk32 = ln & 31, hf = ln >> 5;
+        lf16_t sc[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[i][e] = 0.0f;
+        const uint32_t key_at = tk32 * (DK * 2) + ((hf ^ key_swz(tk32, kk)) << 4), rope_key_at = tk32 * (DR * 2) + ((hf ^ key_swz(tk32, kr)) << 4);
+#pragma unroll
+        for (int k = 0; k < KS + KR; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint8_t* p = k < KS ? at + (key_at ^ (k << 5)) + i * (32 * DK * 2)
+                                          : at + kRopeAt + (rope_key_at ^ ((k - KS) << 5)) + i * (32 * DR * 2);
+                sc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc[i], 0, 0, 0);
+            }
+        // sc[i][e]: token 32 i + 8 (e / 4) + 4 half + e % 4 against this lane's row
+        uint64_t bad = 0u;
+        if constexpr (edge) {
             // Values that are not finite must not reach rows that do not see their token, whose probability of 0 does not hold them off: they
             // are left out below, and rows that see them are NaN.
             bool found = false;
 #pragma unroll 1
-            for (int p = half; p < DV / 8; p += 2) {
-                const u4_t y = *reinterpret_cast<const u4_t*>(at + kValueAt + l32 * (DV * 2) + (p << 4));
+            for (int p = 0; p < DV / 8; ++p) {
+                const u4_t y = *reinterpret_cast<const u4_t*>(at + kValueAt + ln * (DV * 2) + (p << 4));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) found |= (y[e] & 0x7c00u) == 0x7c00u || (y[e] & 0x7c000000u) == 0x7c000000u;
             }
-            const uint64_t any = __ballot(found);
-            bad = static_cast<uint32_t>(any) | static_cast<uint32_t>(any >> 32);
+            bad = __ballot(found);
         }
-        if (edge || !have0 || !have1) {
+        if (edge || have != 15u) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int tk = 8 * (e / 4) + 4 * half + e % 4;
-                if (bad >> tk & 1) sc[e] = NAN;
-                if (!(e < 8 ? have0 : have1) || token0 + tk > pos) sc[e] = -INFINITY;
-            }
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int tk = 32 * i + 8 * (e / 4) + 4 * hf + e % 4;
+                    if (bad >> tk & 1) sc[i][e] = NAN;
+                    if (!(have >> (2 * i + e / 8) & 1) || token0 + tk > pos) sc[i][e] = -INFINITY;
+                }
         }
-        float m_tile = sc[0];
+        // (the instruction itself: fmaxf() takes two, and one for each operand besides)
+        float top = sc[0][0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) m_tile = fmaxf(m_tile, sc[e]);
-        m_tile *= g.scale_log2e;
-        if (__any(m_tile > ref + kLatentSlack)) {
-            const float m = xhalf_max(m_tile);
-            const float to = m > ref + kLatentSlack ? m - kLatentTop : ref;
+        for (int e = 0; e < 32; e += 2) {
+            const float x = sc[e / 16][e % 16], y = sc[e / 16][e % 16 + 1];
+            asm("v_max3_f32 %0, %0, %1, %2" : "+v"(top) : "v"(x), "v"(y));
+        }
+        top *= g.scale_log2e;
+        if (__any(top > ref + kLatentSlack)) {                              // (rare: the reference has room)
+            const float hi = xhalf_max(top);
+            const float to = hi > ref + kLatentSlack ? hi - kLatentTop : ref;
             const float alpha = to == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
             ref = to;
             sum *= alpha;
@@ -242,25 +279,33 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
             for (int b = 0; b < VB; ++b) o[b] *= alpha;
         }
         const float r = ref == -INFINITY ? 0.0f : ref;
-        h8_t p[2];
+        h8_t p[4];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], g.scale_log2e, -r));
-            sum += x;
-            p[e / 8][e % 8] = static_cast<_Float16>(x);
-        }
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int b = 0; b < VB; ++b)
+            for (int e = 0; e < 16; e += 2) {
+                typedef float f2_t __attribute__((ext_vector_type(2)));
+                typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+                const f2_t x = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e], g.scale_log2e, -r)),
+                                __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e + 1], g.scale_log2e, -r))};
+                const h2_t y = __builtin_convertvector(x, h2_t), ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+                sum = __builtin_amdgcn_fdot2(y, ones, sum, false);          // (of the rounded ones, which the values are weighted with)
+                p[2 * i + e / 8][e % 8] = y[0];
+                p[2 * i + e / 8][e % 8 + 1] = y[1];
+            }
+        // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
+        const int v_tk = 4 * hf + ((ln & 15) >> 2), v_piece = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
+        const uint32_t value_at = kValueAt + v_tk * (DV * 2) + ((v_piece ^ value_swz(v_tk, kv_)) << 4) + (ln & 1) * 8;
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const int tk = 16 * st + 4 * half + ((lane & 15) >> 2), piece = 4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                const uint8_t* lo_at = at + kValueAt + tk * (DV * 2) + ((piece ^ value_swz(tk, DV / 8)) << 4) + (lane & 1) * 8;
-                const uint8_t* hi_at = at + kValueAt + (tk + 8) * (DV * 2) + ((piece ^ value_swz(tk + 8, DV / 8)) << 4) + (lane & 1) * 8;
-                const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(lo_at));
-                const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(hi_at));
+        for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int b = 0; b < VB; ++b) {
+                const uint8_t* from = at + (value_at ^ (b << 6)) + st * (16 * DV * 2);
+                const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
+                const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 8 * DV * 2));
                 const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
                 h8_t vf = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
-                if (bad) {                                                 // (uniform)
+                if constexpr (edge) {
                     u4_t y = __builtin_bit_cast(u4_t, vf);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -271,8 +316,11 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
                 }
                 o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[st], o[b], 0, 0, 0);
             }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                       // (LDS is not left while it is written to)
+    };
+    const int clear = min(n_tiles, (min_pos + 1) / kPromptTile);             // turns whose tokens all of the rows see
+    int tile = 0;
+    for (; tile < clear; ++tile) turn(tile, std::false_type{});
+    for (; tile < n_tiles; ++tile) turn(tile, std::true_type{});
     if (ok) {
         const float all = xhalf_sum(sum), inv = all > 0.0f ? 1.0f / all : all;     // a row that sees nothing: zeros; NaN stays
         _Float16* to = out + (static_cast<int64_t>(rows.first + m) * g.H + h) * DV;
