@@ -177,10 +177,10 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         const int p = (wave * (DV / 32) + i) * 64 + lane, tk = p / kv_;
         value_at_[i] = tk * kv_row + DK * 2 + ((p % kv_ ^ value_swz(tk, kv_)) << 4) - i * 1024;
     }
-    auto fetch = [&](int tile) __attribute__((always_inline)) {
+    auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
         uint8_t* to = lds + (tile & 1) * kTileBytes;
         const uint8_t* from = keys + static_cast<int64_t>(tile) * (kPromptTile * static_cast<int64_t>(kv_row));
-        const uint8_t* rope_at = rope + static_cast<int64_t>(tile) * (kPromptTile * DR * 2) ;
+        const uint8_t* rope_at = rope + static_cast<int64_t>(tile) * (kPromptTile * DR * 2);
         lds_place(to + wave * (DK * 32));
         to_lds(from, key_at_[0]);
         to_lds<1024>(from, key_at_[1]);
@@ -191,7 +191,10 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         lds_place(to + kRopeAt + wave * (DR * 32));
         to_lds(rope_at, rope_at_[0]);
         if constexpr (DR == 64) to_lds<1024>(rope_at, rope_at_[1]);
-        lds_place(to + kValueAt + wave * (DV * 32));
+    };
+    auto fetch_values = [&](int tile) __attribute__((always_inline)) {
+        const uint8_t* from = keys + static_cast<int64_t>(tile) * (kPromptTile * static_cast<int64_t>(kv_row));
+        lds_place(lds + (tile & 1) * kTileBytes + kValueAt + wave * (DV * 32));
         to_lds(from, value_at_[0]);
         to_lds<1024>(from, value_at_[1]);
         if constexpr (DV == 128) {
@@ -205,25 +208,12 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
     float ref = -INFINITY, sum = 0.0f;
-    if (n_tiles > 0) fetch(0);
-    const uint32_t* have_at = there + base;
-    uint32_t have_next = n_tiles > 0 ? have_at[0] | have_at[1] << 2 : 0u;
-    // A turn: EDGE, if some of its tokens may be behind some of the wavefront's rows.
-    auto turn = [&](int tile, auto EDGE) __attribute__((always_inline)) {
-        constexpr bool edge = decltype(EDGE)::value;
-        const uint32_t have = have_next;                                    // of the four times 16 tokens
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (tile + 1 < n_tiles) {
-            fetch(tile + 1);
-            have_next = have_at[2 * tile + 2] | have_at[2 * tile + 3] << 2;
-        }
+    // sc[i][e]: token 32 i + 8 (e / 4) + 4 half + e % 4 against this lane's row
+    auto logits = [&](int tile, lf16_t (&sc)[2]) __attribute__((always_inline)) {
         const uint8_t* at = lds + (tile & 1) * kTileBytes;
-        const int token0 = tile * kPromptTile;
-        if (edge && token0 > max_pos) return;                              // (uniform; behind all of this wavefront's rows)
         int ln = lane;
         asm volatile("" : "+v"(ln));
         const int tk32 = ln & 31, hf = ln >> 5;
-        lf16_t sc[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -237,7 +227,34 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
                                           : at + kRopeAt + (rope_key_at ^ ((k - KS) << 5)) + i * (32 * DR * 2);
                 sc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc[i], 0, 0, 0);
             }
-        // sc[i][e]: token 32 i + 8 (e / 4) + 4 half + e % 4 against this lane's row
+    };
+    const uint32_t* have_at = there + base;
+    auto have_of = [&](int tile) __attribute__((always_inline)) { return tile < n_tiles ? have_at[2 * tile] | have_at[2 * tile + 1] << 2 : 0u; };
+    uint32_t have_next = have_of(0);
+    lf16_t sc0[2], sc1[2];
+    if (n_tiles > 0) {
+        fetch_keys(0);
+        fetch_values(0);
+        if (n_tiles > 1) fetch_keys(1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        logits(0, sc0);
+    }
+    // A turn: the next tile's logits, this one's probabilities and values.  EDGE, if some of its tokens may be behind some of the wavefront's rows.
+    auto turn = [&](int tile, auto EDGE, lf16_t (&sc)[2], lf16_t (&next)[2]) __attribute__((always_inline)) {
+        constexpr bool edge = decltype(EDGE)::value;
+        const uint32_t have = have_next;                                    // of the four times 16 tokens
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (tile + 1 < n_tiles) {
+            if (tile + 2 < n_tiles) fetch_keys(tile + 2);
+            fetch_values(tile + 1);
+        }
+        have_next = have_of(tile + 1);
+        const uint8_t* at = lds + (tile & 1) * kTileBytes;
+        const int token0 = tile * kPromptTile;
+        if (edge && token0 > max_pos) return;                              // (uniform; behind all of this wavefront's rows)
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int hf = ln >> 5;
         uint64_t bad = 0u;
         if constexpr (edge) {
             // Values that are not finite must not reach rows that do not see their token, whose probability of 0 does not hold them off: they
@@ -279,6 +296,7 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
             for (int b = 0; b < VB; ++b) o[b] *= alpha;
         }
         const float r = ref == -INFINITY ? 0.0f : ref;
+        if (!edge || token0 + kPromptTile <= max_pos) logits(tile + 1, next);
         h8_t p[4];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -319,8 +337,15 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
     };
     const int clear = min(n_tiles, (min_pos + 1) / kPromptTile);             // turns whose tokens all of the rows see
     int tile = 0;
-    for (; tile < clear; ++tile) turn(tile, std::false_type{});
-    for (; tile < n_tiles; ++tile) turn(tile, std::true_type{});
+    for (; tile + 1 < clear; tile += 2) {
+        turn(tile, std::false_type{}, sc0, sc1);
+        turn(tile + 1, std::false_type{}, sc1, sc0);
+    }
+    for (; tile < n_tiles; ++tile) {
+        turn(tile, std::true_type{}, sc0, sc1);
+        sc0[0] = sc1[0];
+        sc0[1] = sc1[1];
+    }
     if (ok) {
         const float all = xhalf_sum(sum), inv = all > 0.0f ? 1.0f / all : all;     // a row that sees nothing: zeros; NaN stays
         _Float16* to = out + (static_cast<int64_t>(rows.first + m) * g.H + h) * DV;
