@@ -209,24 +209,37 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         for (int e = 0; e < 16; ++e) o[b][e] = 0.0f;
     float ref = -INFINITY, sum = 0.0f;
     // sc[i][e]: token 32 i + 8 (e / 4) + 4 half + e % 4 against this lane's row
-    auto logits = [&](int tile, lf16_t (&sc)[2]) __attribute__((always_inline)) {
-        const uint8_t* at = lds + (tile & 1) * kTileBytes;
-        int ln = lane;
-        asm volatile("" : "+v"(ln));
-        const int tk32 = ln & 31, hf = ln >> 5;
+    auto key_read = [&](const uint8_t* at, int ln, int k, int i) __attribute__((always_inline)) {
+        const int tk = ln & 31, hf = ln >> 5;
+        const uint32_t key_at = tk * (DK * 2) + ((hf ^ key_swz(tk, kk)) << 4), rope_key_at = tk * (DR * 2) + ((hf ^ key_swz(tk, kr)) << 4);
+        const uint8_t* p = k < KS ? at + (key_at ^ (k << 5)) + i * (32 * DK * 2) : at + kRopeAt + (rope_key_at ^ ((k - KS) << 5)) + i * (32 * DR * 2);
+        return *reinterpret_cast<const h8_t*>(p);
+    };
+    // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
+    auto value_read = [&](const uint8_t* at, int ln, int st, int b) __attribute__((always_inline)) {
+        const int tk = 4 * (ln >> 5) + ((ln & 15) >> 2), piece = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
+        const uint32_t value_at = kValueAt + tk * (DV * 2) + ((piece ^ value_swz(tk, kv_)) << 4) + (ln & 1) * 8;
+        const uint8_t* from = at + (value_at ^ (b << 6)) + st * (16 * DV * 2);
+        const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
+        const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 8 * DV * 2));
+        const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
+        return h8_t{a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+    };
+    auto zero = [&](lf16_t (&sc)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[i][e] = 0.0f;
-        const uint32_t key_at = tk32 * (DK * 2) + ((hf ^ key_swz(tk32, kk)) << 4), rope_key_at = tk32 * (DR * 2) + ((hf ^ key_swz(tk32, kr)) << 4);
+    };
+    auto logits = [&](int tile, lf16_t (&sc)[2]) __attribute__((always_inline)) {
+        const uint8_t* at = lds + (tile & 1) * kTileBytes;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        zero(sc);
 #pragma unroll
         for (int k = 0; k < KS + KR; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint8_t* p = k < KS ? at + (key_at ^ (k << 5)) + i * (32 * DK * 2)
-                                          : at + kRopeAt + (rope_key_at ^ ((k - KS) << 5)) + i * (32 * DR * 2);
-                sc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*reinterpret_cast<const h8_t*>(p), qf[k], sc[i], 0, 0, 0);
-            }
+            for (int i = 0; i < 2; ++i) sc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_read(at, ln, k, i), qf[k], sc[i], 0, 0, 0);
     };
     const uint32_t* have_at = there + base;
     auto have_of = [&](int tile) __attribute__((always_inline)) { return tile < n_tiles ? have_at[2 * tile] | have_at[2 * tile + 1] << 2 : 0u; };
@@ -296,44 +309,68 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
             for (int b = 0; b < VB; ++b) o[b] *= alpha;
         }
         const float r = ref == -INFINITY ? 0.0f : ref;
-        if (!edge || token0 + kPromptTile <= max_pos) logits(tile + 1, next);
         h8_t p[4];
+        auto weigh = [&](int pair) __attribute__((always_inline)) {
+            typedef float f2_t __attribute__((ext_vector_type(2)));
+            typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+            const int i = pair / 8, e = pair % 8 * 2;
+            const f2_t x = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e], g.scale_log2e, -r)),
+                            __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e + 1], g.scale_log2e, -r))};
+            const h2_t y = __builtin_convertvector(x, h2_t), ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+            sum = __builtin_amdgcn_fdot2(y, ones, sum, false);              // (of the rounded ones, which the values are weighted with)
+            p[2 * i + e / 8][e % 8] = y[0];
+            p[2 * i + e / 8][e % 8 + 1] = y[1];
+        };
+        constexpr int kSteps = KS + KR, kFrags = 4 * VB, kAheadKeys = 2, kAheadValues = 4;
+        if constexpr (!edge) {
+            // In this order: reads of LDS ahead of the products that they are for, probabilities between the products.
+            const uint8_t* next_at = lds + (tile + 1 & 1) * kTileBytes;
+            h8_t kf[kSteps][2], vf[kFrags];
+            auto read_keys = [&](int k) __attribute__((always_inline)) {
+                kf[k][0] = key_read(next_at, ln, k, 0);
+                kf[k][1] = key_read(next_at, ln, k, 1);
+            };
+            zero(next);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int k = 0; k < kAheadKeys; ++k) read_keys(k);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                typedef float f2_t __attribute__((ext_vector_type(2)));
-                typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
-                const f2_t x = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e], g.scale_log2e, -r)),
-                                __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][e + 1], g.scale_log2e, -r))};
-                const h2_t y = __builtin_convertvector(x, h2_t), ones = {static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
-                sum = __builtin_amdgcn_fdot2(y, ones, sum, false);          // (of the rounded ones, which the values are weighted with)
-                p[2 * i + e / 8][e % 8] = y[0];
-                p[2 * i + e / 8][e % 8 + 1] = y[1];
-            }
-        // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
-        const int v_tk = 4 * hf + ((ln & 15) >> 2), v_piece = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
-        const uint32_t value_at = kValueAt + v_tk * (DV * 2) + ((v_piece ^ value_swz(v_tk, kv_)) << 4) + (ln & 1) * 8;
+            for (int k = 0; k < kSteps; ++k) {
+                if (k + kAheadKeys < kSteps)
+                    read_keys(k + kAheadKeys);
+                else
 #pragma unroll
-        for (int st = 0; st < 4; ++st)
-#pragma unroll
-            for (int b = 0; b < VB; ++b) {
-                const uint8_t* from = at + (value_at ^ (b << 6)) + st * (16 * DV * 2);
-                const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
-                const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 8 * DV * 2));
-                const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
-                h8_t vf = {a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
-                if constexpr (edge) {
-                    u4_t y = __builtin_bit_cast(u4_t, vf);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
-                        if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
+                    for (int f = 0; f < kAheadValues / kAheadKeys; ++f) {
+                        const int at_f = (k + kAheadKeys - kSteps) * (kAheadValues / kAheadKeys) + f;
+                        vf[at_f] = value_read(at, ln, at_f / VB, at_f % VB);
                     }
-                    vf = __builtin_bit_cast(h8_t, y);
-                }
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, p[st], o[b], 0, 0, 0);
+                next[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k][0], qf[k], next[0], 0, 0, 0);
+                next[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k][1], qf[k], next[1], 0, 0, 0);
+#pragma unroll
+                for (int pair = k * 16 / kSteps; pair < (k + 1) * 16 / kSteps; ++pair) weigh(pair);
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+                if (f + kAheadValues < kFrags) vf[f + kAheadValues] = value_read(at, ln, (f + kAheadValues) / VB, (f + kAheadValues) % VB);
+                o[f % VB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[f], p[f / VB], o[f % VB], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            if (token0 + kPromptTile <= max_pos) logits(tile + 1, next);
+#pragma unroll
+            for (int pair = 0; pair < 16; ++pair) weigh(pair);
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+                u4_t y = __builtin_bit_cast(u4_t, value_read(at, ln, f / VB, f % VB));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if ((y[e] & 0x7c00u) == 0x7c00u) y[e] &= 0xffff0000u;
+                    if ((y[e] & 0x7c000000u) == 0x7c000000u) y[e] &= 0xffffu;
+                }
+                o[f % VB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8_t, y), p[f / VB], o[f % VB], 0, 0, 0);
+            }
+        }
     };
     const int clear = min(n_tiles, (min_pos + 1) / kPromptTile);             // turns whose tokens all of the rows see
     int tile = 0;
