@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, Prompt
 // Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them, and takes
 // 64 tokens a turn, two independent products S^T = K Q^T of 32 tokens each.  Keys and values go straight to LDS, the next turn's while this one's
 // are used.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
-constexpr int kPromptTile = 64;
+constexpr int kPromptTile = 64, kPromptHeads = 4;
 template <int DK, int DR, int DV>
 __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, PromptGeom g, PromptTable t, const int32_t* __restrict__ row_start,
                                                                const _Float16* __restrict__ q, const _Float16* __restrict__ kv,
@@ -121,16 +121,12 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kTileBytes];
     const int lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    // workgroups are dealt to the eight XCDs in turn: those of a head go to one of them, whose L2 then holds its keys and values
-    int h, rt;
-    if (g.H % 8 == 0) {
-        const int id = static_cast<int>(blockIdx.x) >> 3;
-        h = id / g.row_tiles * 8 + (static_cast<int>(blockIdx.x) & 7);
-        rt = g.row_tiles - 1 - id % g.row_tiles;
-    } else {
-        h = static_cast<int>(blockIdx.x) / g.row_tiles;
-        rt = g.row_tiles - 1 - static_cast<int>(blockIdx.x) % g.row_tiles;
-    }
+    // Workgroups are dealt to the eight XCDs in turn: those of a head go to one of them, whose L2 then holds its keys and values.  Four heads at a
+    // time, the longest rows first: with the heads one after the other the last one's longest rows would run when all else is done.
+    const int n_xcd = g.H % 8 == 0 ? 8 : 1, per_xcd = g.H / n_xcd;
+    const int id = static_cast<int>(blockIdx.x) / n_xcd, four = id / (g.row_tiles * kPromptHeads) * kPromptHeads;
+    const int heads = min(kPromptHeads, per_xcd - four), in_four = id - four * g.row_tiles;
+    const int h = (four + in_four % heads) * n_xcd + static_cast<int>(blockIdx.x) % n_xcd, rt = g.row_tiles - 1 - in_four / heads;
     const int s = __builtin_amdgcn_readfirstlane(first_behind(t.row_end, v.p.n_seqs, rt, lane));
     if (s < 0) return;
     const int rt_in = rt - (s ? t.row_end[s - 1] : 0), base = s ? t.tile_end[s - 1] : 0;
