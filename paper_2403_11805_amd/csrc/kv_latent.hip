@@ -304,7 +304,10 @@ int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_
     g.q_stride = q_stride;
     g.scale_log2e = static_cast<float>(latent_scale(*shape));
     const int64_t groups = static_cast<int64_t>(g.row_tiles) * g.H;
-    if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows * n_heads too large for one call");
+    const int32_t cols = g.H * (shape->key_dim + shape->value_dim), token_tiles = (g.cap_tiles + kProjectTiles - 1) / kProjectTiles;
+    const int32_t col_tiles = (cols + kProjectCols - 1) / kProjectCols;
+    const int64_t project_groups = (col_tiles + 7) / 8 * 8 * static_cast<int64_t>(token_tiles);
+    if (groups > most_groups(256) || project_groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows * n_heads or n_tokens * n_heads too large for one call");
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
     uint8_t* space = static_cast<uint8_t*>(workspace);
@@ -329,8 +332,16 @@ int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_
     }
 #undef KV_LAUNCH
     if (int rc = launch_status("latent_gather_kernel launch")) return rc;
-    if (int rc = own_product(stream, static_cast<int64_t>(g.cap_tiles) * kLatentTile, static_cast<int64_t>(g.H) * (shape->key_dim + shape->value_dim),
-                             shape->latent_dim, latents, w, kv, "keys and values"))
+    if (g.cap_tiles > kProjectFewTiles) {
+        const dim3 project(static_cast<uint32_t>(project_groups));
+#define KV_LAUNCH(D)                                                                                                               \
+    hipLaunchKernelGGL((latent_project_kernel<D>), project, dim3(256), 0, st, table, n_seqs, cols, col_tiles, token_tiles, \
+                       latents, static_cast<const _Float16*>(w), kv)
+        if (shape->latent_dim == 512) KV_LAUNCH(512);
+        else KV_LAUNCH(256);
+#undef KV_LAUNCH
+        if (int rc = launch_status("latent_project_kernel launch")) return rc;
+    } else if (int rc = own_product(stream, static_cast<int64_t>(g.cap_tiles) * kLatentTile, cols, shape->latent_dim, latents, w, kv, "keys and values"))
         return rc;
     const dim3 attend(static_cast<uint32_t>(groups));
 #define KV_LAUNCH(K, R, V)                                                                                                                        \

@@ -177,23 +177,21 @@ __device__ __forceinline__ void wait_loads(int n) {
 // Waits for the other wavefronts; LDS is not touched across it.
 __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Loads from memory to LDS, without registers in between: lane i's 16 bytes (to_lds_dwords: 4) to 16 i (4 i) behind the place that lds_place() has
-// named last plus OFFSET, from a base for all lanes, an offset of the lane, and OFFSET again; or (to_lds_from) from an address of the lane.  The
-// compiler would wait for all such loads in front of every read of LDS that they might write to, and a tile ahead would never be one; so they
-// are written out, and wait_loads() waits for them.  The place stands in a register that the loads behind it hold for some 200 cycles each: it is
-// named once for all rows of a wavefront.
-__device__ __forceinline__ void lds_place(uint8_t* to) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)to)));
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(at) : "memory");
+// Loads from memory to LDS, without registers in between: lane i's 16 bytes (to_lds_dwords: 4) to 16 i (4 i) behind a place plus OFFSET, from a
+// base for all lanes, an offset of the lane, and OFFSET again; or (to_lds_from) from an address of the lane.  The compiler would wait for all such
+// loads in front of every read of LDS that they might write to, and a tile ahead would never be one; so they are written out, and wait_loads()
+// waits for them.  The place is in m0 (a register that the compiler knows as the instruction's operand); it must be there one state before.
+__device__ __forceinline__ uint32_t lds_place(uint8_t* to) {
+    return __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)to)));
 }
-template <int OFFSET = 0> __device__ __forceinline__ void to_lds(const uint8_t* base, uint32_t at) {
-    asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(at), "s"(base), "n"(OFFSET) : "memory");
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds(uint32_t place, const uint8_t* base, uint32_t at) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(at), "s"(base), "n"(OFFSET), "{m0}"(place) : "memory");
 }
-template <int OFFSET = 0> __device__ __forceinline__ void to_lds_dwords(const uint8_t* base, uint32_t at) {
-    asm volatile("global_load_lds_dword %0, %1 offset:%2" ::"v"(at), "s"(base - OFFSET), "n"(OFFSET) : "memory");
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds_dwords(uint32_t place, const uint8_t* base, uint32_t at) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1 offset:%2" ::"v"(at), "s"(base - OFFSET), "n"(OFFSET), "{m0}"(place) : "memory");
 }
-template <int OFFSET = 0> __device__ __forceinline__ void to_lds_from(const uint8_t* from) {
-    asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from - OFFSET), "n"(OFFSET) : "memory");
+template <int OFFSET = 0> __device__ __forceinline__ void to_lds_from(uint32_t place, const uint8_t* from) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off offset:%1" ::"v"(from - OFFSET), "n"(OFFSET), "{m0}"(place) : "memory");
 }
 
 // Packed latents of a wavefront's TW tokens: codes and parameters come to LDS as they are, into the place that its rows will have there (codes in
@@ -203,13 +201,13 @@ __device__ __forceinline__ int packed_fetch(const uint8_t* codes, const uint8_t*
                                             uint32_t lane) {
     constexpr int kBytes = TW * DC * W / 8, kParams = TW * DC * 2 * 3 / 4;
     static_assert(kBytes <= kParams, "codes and parameters do not overlap");
-    lds_place(rows);
-    if (kBytes >= 1024 || lane * 16 < kBytes) to_lds(codes, lane * 16);
-    if constexpr (kBytes > 1024) to_lds<1024>(codes, lane * 16);
+    const uint32_t place = lds_place(rows);
+    if (kBytes >= 1024 || lane * 16 < kBytes) to_lds(place, codes, lane * 16);
+    if constexpr (kBytes > 1024) to_lds<1024>(place, codes, lane * 16);
     static_assert(kBytes <= 2048, "two loads of codes");
     if (lane * 4 < param_bytes) {
-        to_lds_dwords<kParams>(scales, lane * 4);
-        to_lds_dwords<kParams + TW * DC / 4>(scales + mn_step, lane * 4);
+        to_lds_dwords<kParams>(place, scales, lane * 4);
+        to_lds_dwords<kParams + TW * DC / 4>(place, scales + mn_step, lane * 4);
     }
     return (kBytes + 1023) / 1024 + 2;
 }
@@ -433,16 +431,15 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
             };
             static_assert(TW / kSide == 4 || TW / kSide == 2, "four loads of whole rows, or two");
             constexpr bool kFour = TW / kSide == 4;
-            lds_place(rope);
+            const uint32_t rope_place = lds_place(rope), place = lds_place(rows);
             if (valid1 == TW && width1 == 16) {
-                if (lane_at < TW * kRopeRow) to_lds(record + (rope16 + row * (DR * 2)), rope_tk * (DR * 2) + rope_in);
+                if (lane_at < TW * kRopeRow) to_lds(rope_place, record + (rope16 + row * (DR * 2)), rope_tk * (DR * 2) + rope_in);
                 const uint8_t* codes = record + row * (DC * 2);
-                lds_place(rows);
-                to_lds(codes, in_rows(0));
-                to_lds<1024>(codes, in_rows(1));
+                to_lds(place, codes, in_rows(0));
+                to_lds<1024>(place, codes, in_rows(1));
                 if constexpr (kFour) {
-                    to_lds<2048>(codes, in_rows(2));
-                    to_lds<3072>(codes, in_rows(3));
+                    to_lds<2048>(place, codes, in_rows(2));
+                    to_lds<3072>(place, codes, in_rows(3));
                 }
                 loads = TW / kSide + 1;
                 return;
@@ -452,18 +449,17 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
             const uint8_t* codes = record + row * (DC / 8 * width1);
             const uint8_t* ropes = record + (behind_codes + (width1 == 16 ? 0u : static_cast<uint32_t>(a->v.p.param_bytes)) + row * (DR * 2));
             if (lane_at < TW * kRopeRow)
-                to_lds_from(static_cast<int>(rope_tk) < valid1 ? ropes + (rope_tk * (DR * 2) + rope_in) : zeros + rope_in);
+                to_lds_from(rope_place, static_cast<int>(rope_tk) < valid1 ? ropes + (rope_tk * (DR * 2) + rope_in) : zeros + rope_in);
             if (valid1 == 0) width1 = 16;
             if (width1 == 16) {
                 auto from = [&](int i) __attribute__((always_inline)) {
                     return static_cast<int>(i * kSide + lane_at / kRow) < valid1 ? codes + i * 1024 + in_rows(i) : zeros + in_rows(i);
                 };
-                lds_place(rows);
-                to_lds_from(from(0));
-                to_lds_from<1024>(from(1));
+                to_lds_from(place, from(0));
+                to_lds_from<1024>(place, from(1));
                 if constexpr (kFour) {
-                    to_lds_from<2048>(from(2));
-                    to_lds_from<3072>(from(3));
+                    to_lds_from<2048>(place, from(2));
+                    to_lds_from<3072>(place, from(3));
                 }
                 loads = TW / kSide + 1;
             } else {

@@ -107,6 +107,119 @@ __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, Prompt
     }
 }
 
+// permutations of the 16-byte pieces of a row of values in LDS (see latent_swizzle; a read has four pieces of each of four rows)
+__device__ __forceinline__ int value_swizzle(int token, int pieces) { return pieces >= 16 ? (token & 3) << 2 : (token & 2) << 1; }
+
+// The operand of 16 rows x 32 columns from row-major LDS, eight rows in each half of the wavefront: rows 0..7 and 8..15, or (HALVES = 4: the order
+// in which a product S^T leaves its probabilities) 0..3 and 8..11, 4..7 and 12..15.  A lane hands in four columns of one of its group's four rows
+// and receives its column of all four.  columns_at(): the lane's place in the first four rows of its half.
+template <int ROW_BYTES, int HALVES> __device__ __forceinline__ uint32_t columns_at(int lane) {
+    const int row = HALVES * (lane >> 5) + ((lane & 15) >> 2), piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    return row * ROW_BYTES + ((piece ^ value_swizzle(row, ROW_BYTES / 16)) << 4) + (lane & 1) * 8;
+}
+template <int ROW_BYTES, int HALVES> __device__ __forceinline__ h8_t read_columns(const uint8_t* from) {
+    const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
+    const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + (12 - HALVES) * ROW_BYTES));
+    const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
+    return h8_t{a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+}
+
+// Keys and values of all heads from the latents: a workgroup makes 128 tokens (four gathered tiles) x 256 columns, a wavefront 64 columns of them.
+// 32 of the latents' dimensions a stage, both operands straight to LDS, two stages ahead; two workgroups to a CU, so that one's results are
+// written while the other multiplies (with 256 tokens in 512 threads, one to a CU, 4096 tokens x 32768 columns took 1.25 times as long).
+constexpr int kProjectTiles = 4, kProjectCols = 256;
+template <int DC>
+__global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, int32_t n_seqs, int32_t N, int32_t col_tiles, int32_t token_tiles,
+                                                             const _Float16* __restrict__ latents, const _Float16* __restrict__ w,
+                                                             _Float16* __restrict__ kv) {
+    constexpr int kStages = 3, kSteps = DC / 32, kTokens = kProjectTiles * 2048, kWeights = 32 * kProjectCols * 2, kStageBytes = kTokens + kWeights;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStageBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    // workgroups are dealt to the eight XCDs in turn: one of them takes all tokens of its columns, one column tile after the other
+    const int per_xcd = (col_tiles + 7) / 8, id = static_cast<int>(blockIdx.x) >> 3;
+    const int ct = (static_cast<int>(blockIdx.x) & 7) * per_xcd + id / token_tiles, tile0 = id % token_tiles * kProjectTiles;
+    const int tiles = t.tile_end[n_seqs - 1];
+    if (ct >= col_tiles || tile0 >= tiles) return;
+    const int n0 = ct * kProjectCols;
+    const uint8_t* token_from = reinterpret_cast<const uint8_t*>(latents) + static_cast<int64_t>(min(tile0 + wave, tiles - 1)) * (kLatentTile * DC * 2);
+    const uint8_t* weight_from = reinterpret_cast<const uint8_t*>(w) + n0 * 2;
+    uint32_t weight_at[4];                                                  // (columns past the last repeat it)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = wave * 8 + 2 * i + (lane >> 5), piece = min((lane & 31) ^ value_swizzle(row, kProjectCols / 8), (N - n0) / 8 - 1);
+        weight_at[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(N) * 2u + piece * 16;
+    }
+    auto fetch = [&](int step) __attribute__((always_inline)) {
+        uint8_t* to = lds + step % kStages * kStageBytes;
+        const uint32_t tokens = lds_place(to + wave * 2048), weights = lds_place(to + kTokens + wave * 4096);
+        const uint8_t* from = token_from + step * 2048;
+        to_lds(tokens, from, lane * 16);
+        to_lds<1024>(tokens, from, lane * 16);
+        const uint8_t* rows = weight_from + static_cast<int64_t>(step) * 32 * N * 2;
+        to_lds(weights, rows, weight_at[0]);
+        to_lds<1024>(weights, rows - 1024, weight_at[1]);                   // (the lanes' offsets are not negative: a row may be shorter than 512 bytes)
+        to_lds<2048>(weights, rows - 2048, weight_at[2]);
+        to_lds<3072>(weights, rows - 3072, weight_at[3]);
+    };
+    lf16_t acc[2][4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[b][m][e] = 0.0f;
+    const uint32_t cols_at = columns_at<kProjectCols * 2, 8>(lane);
+    static_assert(kSteps >= kStages, "stages ahead");
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) fetch(i);
+#pragma unroll
+    for (int step = 0; step < kSteps; ++step) {
+        // a wavefront's own six loads of this stage are done, and then everybody's; the stage that is fetched was used a step ago
+        if (step + 1 < kSteps) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (step + kStages - 1 < kSteps) fetch(step + kStages - 1);
+        const uint8_t* at = lds + step % kStages * kStageBytes;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            h8_t wf[2], cf[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                wf[b] = read_columns<kProjectCols * 2, 8>(at + kTokens + (cols_at ^ ((2 * wave + b) << 6)) + k * (16 * kProjectCols * 2));
+#pragma unroll
+            for (int m = 0; m < 4; ++m) cf[m] = *reinterpret_cast<const h8_t*>(at + m * 2048 + k * 1024 + lane * 16);
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) acc[b][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wf[b], cf[m], acc[b][m], 0, 0, 0);
+        }
+    }
+    // acc[b][m][e]: column 32 b + 8 (e / 4) + 4 half + e % 4 of token lane % 32; after an exchange of the halves a lane has eight columns
+    const int half = lane >> 5;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const int tile = tile0 + m;
+        if (tile >= tiles) break;
+        _Float16* to = kv + (static_cast<int64_t>(tile) * kLatentTile + (lane & 31)) * N;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                lh4_t x, y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = static_cast<_Float16>(acc[b][m][4 * j + e]);
+                    y[e] = static_cast<_Float16>(acc[b][m][4 * j + 4 + e]);
+                }
+                const u2_t p = __builtin_bit_cast(u2_t, x), q = __builtin_bit_cast(u2_t, y);
+                const auto r0 = __builtin_amdgcn_permlane32_swap(p[0], q[0], false, false);
+                const auto r1 = __builtin_amdgcn_permlane32_swap(p[1], q[1], false, false);
+                const u4_t z = {r0[0], r1[0], r0[1], r1[1]};
+                const int n = n0 + wave * 64 + 32 * b + 8 * (j + half);
+                if (n < N) *reinterpret_cast<u4_t*>(to + n) = z;
+            }
+    }
+}
+
 // Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them, and takes
 // 64 tokens a turn, two independent products S^T = K Q^T of 32 tokens each.  Keys and values go straight to LDS, the next turn's while this one's
 // are used.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
@@ -149,11 +262,10 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
     const uint32_t kv_row = static_cast<uint32_t>(g.H) * (DK + DV) * 2;
     const uint8_t* keys = reinterpret_cast<const uint8_t*>(kv) + static_cast<int64_t>(base) * kLatentTile * kv_row + h * ((DK + DV) * 2);
     const uint8_t* rope = reinterpret_cast<const uint8_t*>(ropes) + static_cast<int64_t>(base) * kLatentTile * (DR * 2);
-    // permutations of a row's pieces (see latent_swizzle; a read of keys has one piece of 32 tokens here, one of values four pieces of four)
+    // permutation of the pieces of a row of keys (a read has one piece of 32 tokens)
     auto key_swz = [](int token, int pieces) __attribute__((always_inline)) {
         return pieces == 16 ? token & 15 : pieces == 8 ? (token >> 1) & 7 : (token >> 2) & 3;
     };
-    auto value_swz = [](int token, int pieces) __attribute__((always_inline)) { return pieces == 16 ? (token & 3) << 2 : (token & 2) << 1; };
     // Where a lane's piece lies in memory, for the loads of a wavefront's quarter of the tile, one after the other in LDS (1 KB each, which the
     // load's own offset adds on both sides).
     constexpr int kk = DK / 8, kv_ = DV / 8, kr = DR / 8, kRopeLoads = DR / 32;
@@ -171,31 +283,31 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
 #pragma unroll
     for (int i = 0; i < DV / 32; ++i) {
         const int p = (wave * (DV / 32) + i) * 64 + lane, tk = p / kv_;
-        value_at_[i] = tk * kv_row + DK * 2 + ((p % kv_ ^ value_swz(tk, kv_)) << 4) - i * 1024;
+        value_at_[i] = tk * kv_row + DK * 2 + ((p % kv_ ^ value_swizzle(tk, kv_)) << 4) - i * 1024;
     }
     auto fetch_keys = [&](int tile) __attribute__((always_inline)) {
         uint8_t* to = lds + (tile & 1) * kTileBytes;
         const uint8_t* from = keys + static_cast<int64_t>(tile) * (kPromptTile * static_cast<int64_t>(kv_row));
         const uint8_t* rope_at = rope + static_cast<int64_t>(tile) * (kPromptTile * DR * 2);
-        lds_place(to + wave * (DK * 32));
-        to_lds(from, key_at_[0]);
-        to_lds<1024>(from, key_at_[1]);
+        const uint32_t place = lds_place(to + wave * (DK * 32));
+        to_lds(place, from, key_at_[0]);
+        to_lds<1024>(place, from, key_at_[1]);
         if constexpr (DK == 128) {
-            to_lds<2048>(from, key_at_[2]);
-            to_lds<3072>(from, key_at_[3]);
+            to_lds<2048>(place, from, key_at_[2]);
+            to_lds<3072>(place, from, key_at_[3]);
         }
-        lds_place(to + kRopeAt + wave * (DR * 32));
-        to_lds(rope_at, rope_at_[0]);
-        if constexpr (DR == 64) to_lds<1024>(rope_at, rope_at_[1]);
+        const uint32_t place1 = lds_place(to + kRopeAt + wave * (DR * 32));
+        to_lds(place1, rope_at, rope_at_[0]);
+        if constexpr (DR == 64) to_lds<1024>(place1, rope_at, rope_at_[1]);
     };
     auto fetch_values = [&](int tile) __attribute__((always_inline)) {
         const uint8_t* from = keys + static_cast<int64_t>(tile) * (kPromptTile * static_cast<int64_t>(kv_row));
-        lds_place(lds + (tile & 1) * kTileBytes + kValueAt + wave * (DV * 32));
-        to_lds(from, value_at_[0]);
-        to_lds<1024>(from, value_at_[1]);
+        const uint32_t place2 = lds_place(lds + (tile & 1) * kTileBytes + kValueAt + wave * (DV * 32));
+        to_lds(place2, from, value_at_[0]);
+        to_lds<1024>(place2, from, value_at_[1]);
         if constexpr (DV == 128) {
-            to_lds<2048>(from, value_at_[2]);
-            to_lds<3072>(from, value_at_[3]);
+            to_lds<2048>(place2, from, value_at_[2]);
+            to_lds<3072>(place2, from, value_at_[3]);
         }
     };
     lf16_t o[VB];
@@ -211,15 +323,8 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         const uint8_t* p = k < KS ? at + (key_at ^ (k << 5)) + i * (32 * DK * 2) : at + kRopeAt + (rope_key_at ^ ((k - KS) << 5)) + i * (32 * DR * 2);
         return *reinterpret_cast<const h8_t*>(p);
     };
-    // a lane hands in four dimensions of one of its group's four tokens and receives its dimension of all four
     auto value_read = [&](const uint8_t* at, int ln, int st, int b) __attribute__((always_inline)) {
-        const int tk = 4 * (ln >> 5) + ((ln & 15) >> 2), piece = 2 * ((ln >> 4) & 1) + ((ln & 3) >> 1);
-        const uint32_t value_at = kValueAt + tk * (DV * 2) + ((piece ^ value_swz(tk, kv_)) << 4) + (ln & 1) * 8;
-        const uint8_t* from = at + (value_at ^ (b << 6)) + st * (16 * DV * 2);
-        const ls4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from));
-        const ls4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) ls4_t*)(from + 8 * DV * 2));
-        const lh4_t a = __builtin_bit_cast(lh4_t, lo), c = __builtin_bit_cast(lh4_t, hi);
-        return h8_t{a[0], a[1], a[2], a[3], c[0], c[1], c[2], c[3]};
+        return read_columns<DV * 2, 4>(at + kValueAt + (columns_at<DV * 2, 4>(ln) ^ (b << 6)) + st * (16 * DV * 2));
     };
     auto zero = [&](lf16_t (&sc)[2]) __attribute__((always_inline)) {
 #pragma unroll

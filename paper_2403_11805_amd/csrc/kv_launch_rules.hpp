@@ -91,6 +91,9 @@ constexpr AttendDivision attend_division(int32_t in_steps, int32_t in_two_steps,
     return {1, kPieceCost, (in_line + groups - 1) / groups};
 }
 
+// Latent prompts: room for up to so many tiles of 32 tokens takes the product that streams the weights (up to 64 rows).
+constexpr int32_t kProjectFewTiles = 2;
+
 // Latent attention: tiles of 32 tokens (places in the line of work) that a workgroup takes, of `units` tiles of tokens in `pairs` (sequence, row
 // tile) pairs: at least so many that `groups` workgroups do, and so many that writing and reading the shares, M rows of a share per workgroup,
 // costs no more than dividing the work gains.
