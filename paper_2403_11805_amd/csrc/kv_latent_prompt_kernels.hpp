@@ -135,9 +135,10 @@ __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, i
     constexpr int kStages = 3, kSteps = DC / 32, kTokens = kProjectTiles * 2048, kWeights = 32 * kProjectCols * 2, kStageBytes = kTokens + kWeights;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kStages * kStageBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    // workgroups are dealt to the eight XCDs in turn: one of them takes all tokens of its columns, one column tile after the other
+    // Workgroups are dealt to the eight XCDs in turn: one of them has an eighth of the columns, which it takes through eight token tiles at a time.
     const int per_xcd = (col_tiles + 7) / 8, id = static_cast<int>(blockIdx.x) >> 3;
-    const int ct = (static_cast<int>(blockIdx.x) & 7) * per_xcd + id / token_tiles, tile0 = id % token_tiles * kProjectTiles;
+    const int eight = id / (per_xcd * 8) * 8, in_eight = id - eight * per_xcd, wide = min(8, token_tiles - eight);
+    const int ct = (static_cast<int>(blockIdx.x) & 7) * per_xcd + in_eight / wide, tile0 = (eight + in_eight % wide) * kProjectTiles;
     const int tiles = t.tile_end[n_seqs - 1];
     if (ct >= col_tiles || tile0 >= tiles) return;
     const int n0 = ct * kProjectCols;
@@ -193,30 +194,30 @@ __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, i
                 for (int b = 0; b < 2; ++b) acc[b][m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(wf[b], cf[m], acc[b][m], 0, 0, 0);
         }
     }
-    // acc[b][m][e]: column 32 b + 8 (e / 4) + 4 half + e % 4 of token lane % 32; after an exchange of the halves a lane has eight columns
-    const int half = lane >> 5;
+    // acc[b][m][e]: column 32 b + 8 (e / 4) + 4 half + e % 4 of token lane % 32.  Through LDS, so that whole rows are written (pieces of 16 bytes
+    // change places by the token: a wavefront writes one piece of 32 tokens).
+    const int half = lane >> 5, l32 = lane & 31;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const int tile = tile0 + m;
-        if (tile >= tiles) break;
-        _Float16* to = kv + (static_cast<int64_t>(tile) * kLatentTile + (lane & 31)) * N;
+    for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-                lh4_t x, y;
+            for (int j = 0; j < 4; ++j) {
+                lh4_t x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = static_cast<_Float16>(acc[b][m][4 * j + e]);
-                    y[e] = static_cast<_Float16>(acc[b][m][4 * j + 4 + e]);
-                }
-                const u2_t p = __builtin_bit_cast(u2_t, x), q = __builtin_bit_cast(u2_t, y);
-                const auto r0 = __builtin_amdgcn_permlane32_swap(p[0], q[0], false, false);
-                const auto r1 = __builtin_amdgcn_permlane32_swap(p[1], q[1], false, false);
-                const u4_t z = {r0[0], r1[0], r0[1], r1[1]};
-                const int n = n0 + wave * 64 + 32 * b + 8 * (j + half);
-                if (n < N) *reinterpret_cast<u4_t*>(to + n) = z;
+                for (int e = 0; e < 4; ++e) x[e] = static_cast<_Float16>(acc[b][m][4 * j + e]);
+                const int piece = wave * 8 + 4 * b + j;
+                *reinterpret_cast<lh4_t*>(lds + (32 * m + l32) * (kProjectCols * 2) + ((piece ^ l32) << 4) + half * 8) = x;
             }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+        const int token = 8 * i + 2 * wave + half;
+        if (tile0 + token / kLatentTile < tiles && n0 + l32 * 8 < N) {
+            const u4_t x = *reinterpret_cast<const u4_t*>(lds + token * (kProjectCols * 2) + ((l32 ^ (token & 31)) << 4));
+            *reinterpret_cast<u4_t*>(kv + (static_cast<int64_t>(tile0) * kLatentTile + token) * N + n0 + l32 * 8) = x;
+        }
     }
 }
 
