@@ -5,6 +5,8 @@
 // parts [T][Dr] in fp16.  That is one slab per layer of the record format of the per-head caches, with the position parts behind it.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_pages_kernels.hpp"
 
 namespace kvs {
@@ -50,6 +52,14 @@ __device__ __forceinline__ RowPlace row_place(const LatentView& v, const int32_t
     return {off, latent_present(v, off, b) ? b : 0, token - page * v.p.T};
 }
 
+// Whether rows r .. last lie in one page, r's (whose place is `at` and whose sequence s).
+__device__ __forceinline__ bool rows_in_page(const LatentView& v, const int32_t* __restrict__ row_start, int n_rows, int last, int r, int s,
+                                             const RowPlace& at) {
+    if (at.b == 0) return false;
+    const SeqRows rows = seq_rows(row_start, s, n_rows);
+    return last < rows.first + rows.count && at.in_page + (last - r) < v.p.T;
+}
+
 // A wavefront has kSide rows side by side (two where a row is half a wavefront wide), UNITS times.
 template <int DC> struct LatentLanes {
     static constexpr int kPieces = DC / 8, kSide = 64 / kPieces;
@@ -74,7 +84,33 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentView v, const 
         raw[u] = *reinterpret_cast<const u4_t*>(c + row * c_stride + piece * 8);
         if (has_rope) rope[u] = *reinterpret_cast<const u4_t*>(r + row * r_stride + piece * 8);
     }
+    auto store = [&](int u, const RowPlace& at) __attribute__((always_inline)) {
+        uint8_t* record = v.p.pool + at.off;
+        const SlabAt slab = slab_at<DC>(v.p, at.b, v.layer);
+        const int p = at.in_page * L::kPieces + piece;
+        if (at.b == 16) stream_store<true>(raw[u], reinterpret_cast<u4_t*>(record + slab.codes) + p);
+        else if (v.p.half_params) {
+            if (at.b == 8) compress_piece<8, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+            else if (at.b == 4) compress_piece<4, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+            else compress_piece<2, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+        } else {
+            if (at.b == 8) compress_piece<8, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+            else if (at.b == 4) compress_piece<4, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+            else compress_piece<2, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
+        }
+        if (has_rope) stream_store<true>(rope[u], reinterpret_cast<u4_t*>(record + rope_at(v, at.b)) + at.in_page * (v.Dr / 8) + piece);
+    };
     int s = -1;
+    if constexpr (UNITS > 1) {
+        const RowPlace at = row_place(v, row_start, n_rows, r0, s, lane);
+        const int last = min(r0 + UNITS * L::kSide, n_rows) - 1;
+        if (rows_in_page(v, row_start, n_rows, last, r0, s, at)) {          // (most: one look at the tables)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u)
+                if (r0 + u * L::kSide + side <= last) store(u, {at.off, at.b, at.in_page + u * L::kSide + side});
+            return;
+        }
+    }
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         RowPlace at = {0, 0, 0};
@@ -85,22 +121,7 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentView v, const 
             const RowPlace one = row_place(v, row_start, n_rows, row, s, lane);
             if (side == i) at = one;
         }
-        if (at.b != 0) {
-            uint8_t* record = v.p.pool + at.off;
-            const SlabAt slab = slab_at<DC>(v.p, at.b, v.layer);
-            const int p = at.in_page * L::kPieces + piece;
-            if (at.b == 16) stream_store<true>(raw[u], reinterpret_cast<u4_t*>(record + slab.codes) + p);
-            else if (v.p.half_params) {
-                if (at.b == 8) compress_piece<8, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-                else if (at.b == 4) compress_piece<4, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-                else compress_piece<2, true>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-            } else {
-                if (at.b == 8) compress_piece<8, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-                else if (at.b == 4) compress_piece<4, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-                else compress_piece<2, false>(raw[u], record + slab.codes, record + slab.scale, record + slab.mn, p, lpg_log2, lane);
-            }
-            if (has_rope) stream_store<true>(rope[u], reinterpret_cast<u4_t*>(record + rope_at(v, at.b)) + at.in_page * (v.Dr / 8) + piece);
-        }
+        if (at.b != 0) store(u, at);
     }
 }
 
@@ -133,6 +154,35 @@ __global__ __launch_bounds__(256) void latent_read_kernel(LatentView v, _Float16
     const int r0 = static_cast<int>(first);
     const bool has_rope = piece < v.Dr / 8;
     int s = -1;
+    if constexpr (UNITS > 1) {
+        const RowPlace at = row_place(v, row_start, n_rows, r0, s, lane);
+        const int last = min(r0 + UNITS * L::kSide, n_rows) - 1;
+        if (rows_in_page(v, row_start, n_rows, last, r0, s, at)) {          // (most: one look at the tables, and all rows asked for at once)
+            const uint8_t* record = v.p.pool + at.off;
+            const SlabAt slab = slab_at<DC>(v.p, at.b, v.layer);
+            auto move = [&](auto WIDTH) __attribute__((always_inline)) {
+                u4_t rope[UNITS], x[UNITS];
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    const int in_page = at.in_page + min(u * L::kSide + side, last - r0);
+                    if (has_rope) rope[u] = stream_load<true>(reinterpret_cast<const u4_t*>(record + rope_at(v, at.b)) + in_page * (v.Dr / 8) + piece);
+                    x[u] = read_piece<DC>(v, record, slab, decltype(WIDTH)::value, in_page * L::kPieces + piece, lpg_log2);
+                }
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    const int row = r0 + u * L::kSide + side;
+                    if (row > last) break;
+                    *reinterpret_cast<u4_t*>(c + row * c_stride + piece * 8) = x[u];
+                    if (has_rope) *reinterpret_cast<u4_t*>(r + row * r_stride + piece * 8) = rope[u];
+                }
+            };
+            if (at.b == 16) move(std::integral_constant<int, 16>{});
+            else if (at.b == 8) move(std::integral_constant<int, 8>{});
+            else if (at.b == 4) move(std::integral_constant<int, 4>{});
+            else move(std::integral_constant<int, 2>{});
+            return;
+        }
+    }
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
         RowPlace at = {0, 0, 0};
