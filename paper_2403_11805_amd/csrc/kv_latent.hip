@@ -163,17 +163,17 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
     if (n_rows == 0) return KV_OK;
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
-    const int units = n_rows >= 4 * 2048 ? 4 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
+    const int units = n_rows >= 4 * 2048 ? 2 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
     const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(n_rows) + rows - 1) / rows));
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define KV_LAUNCH(D, UNITS)                                                                                                \
     hipLaunchKernelGGL((latent_read_kernel<D, UNITS>), grid, dim3(256), 0, st, view, static_cast<_Float16*>(c), c_stride, \
                        static_cast<_Float16*>(r), r_stride, n_rows, lpg, row_start)
     if (shape->latent_dim == 512) {
-        if (units == 4) KV_LAUNCH(512, 4);
+        if (units == 2) KV_LAUNCH(512, 2);
         else KV_LAUNCH(512, 1);
     } else {
-        if (units == 4) KV_LAUNCH(256, 4);
+        if (units == 2) KV_LAUNCH(256, 2);
         else KV_LAUNCH(256, 1);
     }
 #undef KV_LAUNCH
