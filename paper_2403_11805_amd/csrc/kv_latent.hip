@@ -140,7 +140,9 @@ int32_t kv_latent_append_tokens(const kv_latent_shape_t* shape, const kv_pages_t
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
     const int units = n_rows >= 4 * 2048 ? 4 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
-    const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(n_rows) + rows - 1) / rows));
+    const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
+    if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);
+    const dim3 grid(static_cast<uint32_t>(groups));
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define KV_LAUNCH(D, UNITS)                                                                                                        \
     hipLaunchKernelGGL((latent_append_kernel<D, UNITS>), grid, dim3(256), 0, st, view, static_cast<const _Float16*>(c), c_stride, \
@@ -164,7 +166,9 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
     const int units = n_rows >= 4 * 2048 ? 2 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
-    const dim3 grid(static_cast<uint32_t>((static_cast<int64_t>(n_rows) + rows - 1) / rows));
+    const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
+    if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);
+    const dim3 grid(static_cast<uint32_t>(groups));
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define KV_LAUNCH(D, UNITS)                                                                                                \
     hipLaunchKernelGGL((latent_read_kernel<D, UNITS>), grid, dim3(256), 0, st, view, static_cast<_Float16*>(c), c_stride, \
