@@ -62,9 +62,6 @@ inline uint64_t latent_record_bytes(const kv_latent_shape_t& s, int bits) {
     return rows * (static_cast<uint64_t>(s.latent_dim) * bits / 8u + 2u * s.rope_dim) + (bits == 16 ? 0 : latent_param_bytes(s));
 }
 
-// C[M][N] = A[M][K] * B[K][N] in fp16 on the library's own product (M rows of A in fragment order, M a multiple of 32), enqueued on `stream`.
-int own_product(void* stream, int64_t M, int64_t N, int64_t K, const void* A, const void* B, void* C, const char* what);
-
 inline bool aligned(const void* p, uintptr_t a) {
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }

@@ -124,7 +124,7 @@ int check_prompts(const kv_latent_shape_t* shape, int32_t n_seqs, int64_t n_toke
     if (n_tokens < 1) return fail(KV_EINVAL, "n_tokens %lld is less than 1", static_cast<long long>(n_tokens));
     if (n_tokens > (1 << 26)) return fail(KV_ESHAPE, "n_tokens %lld exceeds 67108864", static_cast<long long>(n_tokens));
     const int64_t rows = prompt_tiles(n_seqs, n_tokens) * kLatentTile, cols = static_cast<int64_t>(shape->n_heads) * (shape->key_dim + shape->value_dim);
-    if (((rows + 95) / 96) * ((cols + 255) / 256 + 7) > most_groups(256)) return fail(KV_ESHAPE, "n_tokens * n_heads too large for one call");
+    if (((rows + 127) / 128) * ((cols + 255) / 256 + 7) > most_groups(256)) return fail(KV_ESHAPE, "n_tokens * n_heads too large for one call");
     return KV_OK;
 }
 
@@ -139,7 +139,9 @@ int32_t kv_latent_append_tokens(const kv_latent_shape_t* shape, const kv_pages_t
     if (n_rows == 0) return KV_OK;
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
-    const int units = n_rows >= 4 * 2048 ? 4 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
+    // Rows of a wavefront: one look at the tables for four rows against four wavefronts at once.  32768 rows of four sequences in pages of every width
+    // 13.5 us with four, 18.6 with one; 8192 rows 7.9 and 7.6; 64 rows of as many sequences 5.4 and 3.1.
+    const int units = n_rows >= 16384 ? 4 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
     const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
     if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);
     const dim3 grid(static_cast<uint32_t>(groups));
@@ -165,7 +167,9 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
     if (n_rows == 0) return KV_OK;
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
-    const int units = n_rows >= 4 * 2048 ? 2 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
+    // As in appending; a row's loads and its results stand in registers, so two (24 ragged contexts of up to 16384 tokens: 107 us with two, 111 with four,
+    // 120 with one; 8192 rows 6.8 with two, 7.6 with one; 2048 rows 4.4 and 4.2).
+    const int units = n_rows >= 8192 ? 2 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
     const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
     if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);
     const dim3 grid(static_cast<uint32_t>(groups));
@@ -254,16 +258,11 @@ int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t
     const int64_t heads_rows = static_cast<int64_t>(all_rows) * shape->n_heads;
     _Float16 *hi = reinterpret_cast<_Float16*>(space + sp.joined), *lo = hi + heads_rows * dc;
     const uint32_t lds = static_cast<uint32_t>(g.groups) * 4;
-#define KV_LAUNCH(D, PER)                                                                                                              \
-    hipLaunchKernelGGL((latent_join_kernel<D, PER>), dim3(static_cast<uint32_t>((heads_rows * PER + 3) / 4)), dim3(256), lds * (4 / PER), st, \
-                       view, g, row_start, line, part_o, part_ml, hi, lo)
-    if (join_shares_rows(heads_rows)) {
-        if (dc == 512) KV_LAUNCH(512, 4);
-        else KV_LAUNCH(256, 4);
-    } else {
-        if (dc == 512) KV_LAUNCH(512, 1);
-        else KV_LAUNCH(256, 1);
-    }
+#define KV_LAUNCH(D)                                                                                                                    \
+    hipLaunchKernelGGL((latent_join_kernel<D>), dim3(static_cast<uint32_t>(heads_rows)), dim3(256), lds, st, view, g, row_start, line, part_o, \
+                       part_ml, hi, lo)
+    if (dc == 512) KV_LAUNCH(512);
+    else KV_LAUNCH(256);
 #undef KV_LAUNCH
     if (int rc = launch_status("latent_join_kernel launch")) return rc;
     const dim3 values(static_cast<uint32_t>(shape->n_heads * (shape->value_dim / 64)), static_cast<uint32_t>((all_rows + 15) / 16));
@@ -311,7 +310,7 @@ int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_
     const int32_t cols = g.H * (shape->key_dim + shape->value_dim), token_tiles = (g.cap_tiles + kProjectTiles - 1) / kProjectTiles;
     const int32_t col_tiles = (cols + kProjectCols - 1) / kProjectCols;
     const int64_t project_groups = (col_tiles + 7) / 8 * 8 * static_cast<int64_t>(token_tiles);
-    if (groups > most_groups(256) || project_groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows * n_heads or n_tokens * n_heads too large for one call");
+    if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows * n_heads too large for one call");
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
     uint8_t* space = static_cast<uint8_t*>(workspace);
@@ -336,17 +335,14 @@ int32_t kv_latent_attend_prompts(const kv_latent_shape_t* shape, const kv_pages_
     }
 #undef KV_LAUNCH
     if (int rc = launch_status("latent_gather_kernel launch")) return rc;
-    if (g.cap_tiles > kProjectFewTiles) {
-        const dim3 project(static_cast<uint32_t>(project_groups));
-#define KV_LAUNCH(D)                                                                                                               \
-    hipLaunchKernelGGL((latent_project_kernel<D>), project, dim3(256), 0, st, table, n_seqs, cols, col_tiles, token_tiles, \
-                       latents, static_cast<const _Float16*>(w), kv)
-        if (shape->latent_dim == 512) KV_LAUNCH(512);
-        else KV_LAUNCH(256);
+    const dim3 project(static_cast<uint32_t>(project_groups));
+#define KV_LAUNCH(D)                                                                                                                         \
+    hipLaunchKernelGGL((latent_project_kernel<D>), project, dim3(256), 0, st, table, n_seqs, cols, col_tiles, token_tiles, latents,          \
+                       static_cast<const _Float16*>(w), kv)
+    if (shape->latent_dim == 512) KV_LAUNCH(512);
+    else KV_LAUNCH(256);
 #undef KV_LAUNCH
-        if (int rc = launch_status("latent_project_kernel launch")) return rc;
-    } else if (int rc = own_product(stream, static_cast<int64_t>(g.cap_tiles) * kLatentTile, cols, shape->latent_dim, latents, w, kv, "keys and values"))
-        return rc;
+    if (int rc = launch_status("latent_project_kernel launch")) return rc;
     const dim3 attend(static_cast<uint32_t>(groups));
 #define KV_LAUNCH(K, R, V)                                                                                                                        \
     hipLaunchKernelGGL((latent_prompt_kernel<K, R, V>), attend, dim3(256), 0, st, view, g, table, row_start, static_cast<const _Float16*>(q), kv, \

@@ -720,24 +720,24 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
 
 // The shares of a query row joined: their sum over the sum of their weights, as the sum of two halves (22 bits, so that the product behind it
 // is not the result's largest error), hi and lo [n_seqs * max_rows][H][DC] each.  Latency bounds it, row, line, weights and shares being loads that
-// wait for each other, and reading the shares.  PER wavefronts share a row, 4 / PER rows are a workgroup's.
-template <int DC, int PER>
+// wait for each other, and reading the shares.  A workgroup's four wavefronts share a row (768 rows of 24 sequences 6.5 us, with a wavefront to a
+// row 7.7; 512 rows of 8 longer ones 8.9 and 12.5; 2048 rows of 32768 tokens 15.4 and 16.7; 2560 rows of up to 3001 tokens 9.6 and 9.3).
+template <int DC>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGeom g, const int32_t* __restrict__ row_start,
                                                           const int32_t* __restrict__ line, const float* __restrict__ part_o,
                                                           const float* __restrict__ part_ml, _Float16* __restrict__ hi, _Float16* __restrict__ lo) {
-    extern __shared__ float weights[];                              // [4 / PER][groups]
-    __shared__ lf4_t parts[PER > 1 ? PER : 1][PER > 1 ? DC / 4 : 1];
+    constexpr int PER = 4;
+    extern __shared__ float weight[];                               // [groups]
+    __shared__ lf4_t parts[PER][DC / 4];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int nth_wave = wave % PER;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * (4 / PER) + wave / PER;
+    const int64_t at = static_cast<int64_t>(blockIdx.x);
     const int row = static_cast<int>(at / g.H), h = static_cast<int>(at - static_cast<int64_t>(row) * g.H);
     const int s = row / g.max_rows, nth = row - s * g.max_rows;
-    float* weight = weights + wave / PER * g.groups;
     const int run = line[0];
     const LatentSeq sw = latent_seq(v, g, row_start, s);
     const bool ok = nth < min(sw.count, g.max_rows);
-    if (!ok) return;                                                // (uniform: where wavefronts share a row, for all of them)
+    if (!ok) return;                                                // (uniform)
     lf4_t x[DC / 256];
 #pragma unroll
     for (int k = 0; k < DC / 256; ++k) x[k] = lf4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -747,7 +747,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGe
         const int begin = line[4 + s] - latent_places(sw.units) * (sw.row_tiles - rt) + kLatentCost, wg = begin / run;
         const int used = (begin + sw.units - 1) / run - wg + 1;
         const int64_t first = (wg + static_cast<int64_t>(s) * g.row_tiles + rt) * M + (j & (M - 1));
-        // (the wavefronts of a row all work the weights out, each writes and reads the same)
+        // (the wavefronts all work the weights out, each writes and reads the same)
         float ref = -INFINITY;
         for (int k = lane; k < used; k += 64) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * M) * 2]);
 #pragma unroll
@@ -762,7 +762,7 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGe
         for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const float* src = part_o + first * DC + lane * 4;
-        for (int k0 = nth_wave; k0 < used; k0 += 8 * PER) {
+        for (int k0 = wave; k0 < used; k0 += 8 * PER) {
             lf4_t y[8][DC / 256];
 #pragma unroll
             for (int k = 0; k < 8; ++k)                              // (behind the last share it is read again, for nothing)
@@ -778,16 +778,14 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGe
                 }
         }
     }
-    if constexpr (PER > 1) {
 #pragma unroll
-        for (int c = 0; c < DC / 256; ++c) parts[nth_wave][lane + c * 64] = x[c];
-        __syncthreads();
-        if (nth_wave) return;
+    for (int c = 0; c < DC / 256; ++c) parts[wave][lane + c * 64] = x[c];
+    __syncthreads();
+    if (wave) return;
 #pragma unroll
-        for (int k = 1; k < PER; ++k)
+    for (int k = 1; k < PER; ++k)
 #pragma unroll
-            for (int c = 0; c < DC / 256; ++c) x[c] += parts[k][lane + c * 64];
-    }
+        for (int c = 0; c < DC / 256; ++c) x[c] += parts[k][lane + c * 64];
     const float inv = total > 0.0f ? 1.0f / total : total;           // a row that sees nothing: zeros; NaN stays
 #pragma unroll
     for (int c = 0; c < DC / 256; ++c) {

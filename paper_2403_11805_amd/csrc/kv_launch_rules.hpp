@@ -91,9 +91,6 @@ constexpr AttendDivision attend_division(int32_t in_steps, int32_t in_two_steps,
     return {1, kPieceCost, (in_line + groups - 1) / groups};
 }
 
-// Latent prompts: room for up to so many tiles of 32 tokens takes the product that streams the weights (up to 64 rows).
-constexpr int32_t kProjectFewTiles = 2;
-
 // Latent attention: tiles of 32 tokens (places in the line of work) that a workgroup takes, of `units` tiles of tokens in `pairs` (sequence, row
 // tile) pairs: at least so many that `groups` workgroups do, and so many that writing and reading the shares, M rows of a share per workgroup,
 // costs no more than dividing the work gains.
@@ -106,9 +103,6 @@ constexpr int32_t latent_run(int32_t units, int32_t pairs, int32_t groups, int32
     run = run > enough ? run : enough;
     return static_cast<int32_t>(run > 1 ? run : 1);
 }
-
-// Latent attention, joining: whether the wavefronts of a workgroup share a row, of `rows` rows of all heads.
-inline bool join_shares_rows(int64_t rows) { return rows < 1024; }
 
 // Eviction: workgroups that share a pair's moves, `rows` at a time each: some 2048 in all, at least four a pair.  512 pairs of 1170 moves
 // 130 us with 1024 or 2048, 145 with 4096; 12 pairs of up to 5700 moves 27 us with 4096, 28 with 2048, 31 with 1024.

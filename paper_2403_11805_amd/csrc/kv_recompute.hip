@@ -330,7 +330,7 @@ int own_gemm(hipStream_t st, FixedTile fixed, int64_t M, int64_t K, const void* 
         else hipLaunchKernelGGL(gemm_stream_kernel<2>, grid, dim3(256), 0, st, g);
     } else {
         const int64_t blocks = (static_cast<int64_t>(h.col_tiles) * h.splits + 7) / 8 * 8 * h.row_tiles;
-        if (blocks > 0xffffffffLL / 256) return fail(KV_ESHAPE, "GEMM (%s): grid exceeds 2^32 threads", what);
+        if (blocks > 0x7fffffffLL) return fail(KV_ESHAPE, "GEMM (%s): grid exceeds 2^31 workgroups", what);
         const dim3 grid(static_cast<uint32_t>(blocks));
 #define KV_TILE(MB)                                                                                       \
     do {                                                                                                  \
@@ -476,11 +476,6 @@ int tune_gemm(kv_recompute* rc, const GemmJob* jobs, int n_jobs, int which, hipS
 }
 
 }  // namespace
-
-int kvs::own_product(void* stream, int64_t M, int64_t N, int64_t K, const void* A, const void* B, void* C, const char* what) {
-    const GemmGroup one = {1, {N}, {B}, {C}};
-    return own_gemm(static_cast<hipStream_t>(stream), FixedTile{}, M, K, A, one, nullptr, Out::kF16, Room{nullptr, 0}, nullptr, what);
-}
 
 extern "C" {
 

@@ -259,7 +259,7 @@ def test_prompts_of_any_number_of_heads(heads, dims):
 
 @pytest.mark.parametrize("room", [70, 129, 500, 5000])
 def test_room_for_more_tokens_than_there_are(room):
-    """What is made of the tokens does not depend on the room for others (nor on which product makes it: above 64 tokens another one)."""
+    """What is made of the tokens does not depend on the room for others."""
     p = Latent((1, 4, 512, 64, 128, 128, 64, 16, 64), [30, 33], MIXED, 41)
     start, n = rows([30, 4])
     q, w = p.queries(n), p.weights()
