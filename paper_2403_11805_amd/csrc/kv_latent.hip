@@ -60,6 +60,8 @@ int check_moved_rows(const kv_latent_shape_t* shape, const kv_pages_t* pages, in
 
 double latent_scale(const kv_latent_shape_t& s) { return 1.4426950408889634 / std::sqrt(static_cast<double>(s.key_dim + s.rope_dim)); }
 
+// Query rows of a tile: the fewest that hold a sequence's, since the products and the probabilities of rows that are not there take their time: 64
+// rows of 8 contexts 25.9 us, in tiles of 128 38.7; 40 rows of one 8.7 and 10.7; 32 rows of 24 contexts 38.8, in tiles of 64 41.1.
 int32_t tile_rows_log2(int64_t rows) { return rows <= 16 ? 4 : rows <= 32 ? 5 : rows <= 64 ? 6 : 7; }
 
 LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_rows) {
@@ -72,6 +74,7 @@ LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_r
     g.tile_log2 = tile_rows_log2(rows);
     g.row_tiles = static_cast<int32_t>((rows + (1 << g.tile_log2) - 1) >> g.tile_log2);
     const int64_t pairs = static_cast<int64_t>(n_seqs) * g.row_tiles, units = pairs * ((s.n_tokens + kLatentTile - 1) / kLatentTile);
+    // (one workgroup to a CU: its tiles fill LDS at latent_dim 512)
     g.groups = static_cast<int32_t>(std::min<int64_t>(256, units + pairs * kLatentCost));
     g.scale_log2e = static_cast<float>(latent_scale(s));
     return g;

@@ -72,7 +72,7 @@ __device__ __forceinline__ void latent_make_line(const LatentView& v, const Late
         units += __builtin_amdgcn_readlane(latent_prefix_sum(w.units * w.row_tiles), 63);
         pairs += __builtin_amdgcn_readlane(latent_prefix_sum(w.units ? w.row_tiles : 0), 63);
     }
-    if (lane == 0) line[0] = latent_run(units, pairs, g.groups, 1 << g.tile_log2);
+    if (lane == 0) line[0] = latent_run(units, pairs, g.groups);
     int before = 0;
     for (int s0 = 0; s0 < v.p.n_seqs; s0 += 64) {
         const LatentSeq w = latent_seq(v, g, row_start, s0 + lane);
@@ -289,8 +289,13 @@ struct LatentAttendArgs {
 // LDS once, as fp16; each of the first M / 16 wavefronts has the logits S^T = K Q^T and the softmax of its own 16 rows and leaves their
 // probabilities in LDS, and each wavefront has an eighth of the dimensions of O^T += V^T P^T for all rows: keys are read from LDS by M / 16
 // wavefronts, values by one.  A turn of the loop, with one barrier, asks for tile t + 3, has the logits and the softmax of tile t + 1 and the
-// values of tile t, half of the wavefronts in this order and half in the other, so that the exponentials of one are beside the products of the
-// other, and brings tile t + 2 into its form.
+// values of tile t, and brings tile t + 2 into its form.  (With half of the wavefronts in another order, values before logits, 128 rows took 5 % longer.)
+//
+// 128 rows: 16 sequences of 32768 tokens in fp16, 604 MB read once, 186 us when the chip is cool, 221 after a few milliseconds of it: 3.2 and 2.7
+// TB/s, 0.8 and 0.66 PFLOP/s.  The same loop with the loads alone takes 132 us, with the products alone 141 to 165 (LDS gives 64 rows of keys 16
+// times, of values 8 times), with neither 31: what is over the products is the start of a workgroup (8 to 12 us until its first tile is there)
+// and the shares that it writes.  16 to 64 rows: the chain of a turn bounds it, load to tile, tile to logits, logits to weights, weights to values,
+// with a barrier: 24 packed contexts of up to 8000 tokens and 32 rows 38 us.
 template <int DC, int DR, int M>
 __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs args) {
     // (arguments are fetched where they are used, in the loop only by what is rare: kept in registers all the time they do not fit, and what
@@ -671,18 +676,11 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
                 }
             }
             };
-            // (the loads of a tile keep the CU's path to memory busy for some 600 cycles, in which whoever has more waits: half of the wavefronts
-            // ask behind their values)
-            const bool has = u >= u_begin - 1 && u + 1 < u_end, late = wave >= NW / 2;
-            if (!late) ask();
+            const bool has = u >= u_begin - 1 && u + 1 < u_end;
+            ask();
             if (u >= u_begin) rescale();
-            if (has && !late) logits(scan());
+            if (has) logits(scan());
             if (u >= u_begin) values();
-            if (late) {
-                ask();
-                const uint32_t bad = has ? scan() : 0u;
-                if (M == 128 && has) logits(bad);
-            }
             // (what was read a turn ago is used again in the next)
             if (was_edge && threadIdx.x == 0) bad_lds[odd] = 0u;
             if (was_moved && threadIdx.x == 0) moved_lds[third == 0 ? 2 : third - 1] = 0u;

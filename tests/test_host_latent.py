@@ -138,7 +138,7 @@ def rules(tmp_path_factory):
         pytest.skip("needs g++")
     at = tmp_path_factory.mktemp("latent_rules")
     source = at / "driver.cpp"
-    source.write_text('#include "kv_launch_rules.hpp"\nextern "C" int latent_run(int u, int p, int g, int m) { return kvs::latent_run(u, p, g, m); }\n')
+    source.write_text('#include "kv_launch_rules.hpp"\nextern "C" int latent_run(int u, int p, int g) { return kvs::latent_run(u, p, g); }\n')
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2403_11805_amd", "csrc"),
                     str(source), "-o", str(at / "rules.so")], check=True)
     return ctypes.CDLL(str(at / "rules.so"))
@@ -150,6 +150,5 @@ def test_runs_of_the_line_of_work(rules):
     for pairs in (1, 2, 3, 16, 24, 100, 4096, 65535):
         for tiles in (0, 1, 2, 7, 32, 1024):
             for groups in (1, 5, 256):
-                for rows in (16, 32, 64, 128):
-                    run = rules.latent_run(pairs * tiles, pairs, groups, rows)
-                    assert run >= 1 and run * groups >= pairs * (tiles + cost)
+                run = rules.latent_run(pairs * tiles, pairs, groups)
+                assert run >= 1 and run * groups >= pairs * (tiles + cost)
