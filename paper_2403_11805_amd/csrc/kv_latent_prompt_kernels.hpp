@@ -67,7 +67,7 @@ __device__ __forceinline__ int first_behind(const int32_t* __restrict__ end, int
 }
 
 // A tile of 32 tokens from their pages: latents in the product's fragment order, position parts row-major, which halves' pages are there
-// (bits 0 and 1); tokens that are not there are zeros.
+// (bits 0 and 1); tokens that are not there are zeros.  Bound by HBM where there are many: 40000 tokens of 8, 4 and 2 bits 25 to 27 us.
 template <int DC, int DR>
 __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, PromptGeom g, PromptTable t, int32_t lpg_log2, _Float16* __restrict__ latents,
                                                             _Float16* __restrict__ ropes, uint32_t* __restrict__ there) {
@@ -125,8 +125,10 @@ template <int ROW_BYTES, int HALVES> __device__ __forceinline__ h8_t read_column
 }
 
 // Keys and values of all heads from the latents: a workgroup makes 128 tokens (four gathered tiles) x 256 columns, a wavefront 64 columns of them.
-// 32 of the latents' dimensions a stage, both operands straight to LDS, two stages ahead; two workgroups to a CU, so that one's results are
-// written while the other multiplies (with 256 tokens in 512 threads, one to a CU, 4096 tokens x 32768 columns took 1.25 times as long).
+// 32 of the latents' dimensions a stage, both operands straight to LDS, two stages ahead: the tokens as they were gathered are an operand as it
+// lies, rows of weights are transposed by the reads.  Two workgroups to a CU, so that one's results are written while the other multiplies: with 256
+// tokens in 512 threads, one to a CU, 40000 tokens x 8192 columns took 1.26 times as long.  4096 tokens x 32768 columns 140 to 155 us, 0.9 PFLOP/s;
+// 292 with results written from registers in pieces of 32 bytes and each column tile taken through all tokens.
 constexpr int kProjectTiles = 4, kProjectCols = 256;
 template <int DC>
 __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, int32_t n_seqs, int32_t N, int32_t col_tiles, int32_t token_tiles,
@@ -223,7 +225,10 @@ __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, i
 
 // Causal attention of the new rows to the expanded keys and values: a workgroup has 128 rows of one head, a wavefront 32 of them, and takes
 // 64 tokens a turn, two independent products S^T = K Q^T of 32 tokens each.  Keys and values go straight to LDS, the next turn's while this one's
-// are used.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
+// are used; a turn makes the next one's logits beside its own probabilities.  Probabilities are rounded to fp16, and their sum is that of the
+// rounded ones, so that it has no part in the result's error.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
+// Two workgroups to a CU, 242 of 256 registers.  Bound by the chip's power: one prompt of 4096 tokens and 128 heads, 0.69 TFLOP, takes 1.5 M cycles, in 45 %
+// of which the matrix pipe is busy, and 770 to 890 us at the clock that is left (1.65 to 1.85 GHz).  LDS gives a wavefront 56 KB a turn, a quarter of its rate.
 constexpr int kPromptTile = 64, kPromptHeads = 4;
 template <int DK, int DR, int DV>
 __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, PromptGeom g, PromptTable t, const int32_t* __restrict__ row_start,
