@@ -444,7 +444,7 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
                 to_lds<1024>(place, codes, in_rows(1));
                 if constexpr (kFour) {
                     to_lds<2048>(place, codes, in_rows(2));
-                    to_lds<3072>(place, codes, in_rows(3));
+                    to_lds<3 * 1024>(place, codes, in_rows(3));
                 }
                 loads = TW / kSide + 1;
                 return;
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
                 to_lds_from<1024>(place, from(1));
                 if constexpr (kFour) {
                     to_lds_from<2048>(place, from(2));
-                    to_lds_from<3072>(place, from(3));
+                    to_lds_from<3 * 1024>(place, from(3));
                 }
                 loads = TW / kSide + 1;
             } else {

@@ -48,7 +48,7 @@ __global__ __launch_bounds__(64) void latent_table_kernel(LatentView v, PromptGe
             t.row_end[s] = row_to;
         }
         tiles = min(__builtin_amdgcn_readlane(end, 63), g.cap_tiles + 1);
-        row_tiles = __builtin_amdgcn_readlane(row_to, 63);
+        row_tiles = min(__builtin_amdgcn_readlane(row_to, 63), 1 << 29);      // (more than any grid: lists that do not ascend must not overflow)
     }
 }
 
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, i
         to_lds(weights, rows, weight_at[0]);
         to_lds<1024>(weights, rows - 1024, weight_at[1]);                   // (the lanes' offsets are not negative: a row may be shorter than 512 bytes)
         to_lds<2048>(weights, rows - 2048, weight_at[2]);
-        to_lds<3072>(weights, rows - 3072, weight_at[3]);
+        to_lds<3 * 1024>(weights, rows - 3 * 1024, weight_at[3]);
     };
     lf16_t acc[2][4];
 #pragma unroll
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         to_lds<1024>(place, from, key_at_[1]);
         if constexpr (DK == 128) {
             to_lds<2048>(place, from, key_at_[2]);
-            to_lds<3072>(place, from, key_at_[3]);
+            to_lds<3 * 1024>(place, from, key_at_[3]);
         }
         const uint32_t place1 = lds_place(to + kRopeAt + wave * (DR * 32));
         to_lds(place1, rope_at, rope_at_[0]);
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, Pro
         to_lds<1024>(place2, from, value_at_[1]);
         if constexpr (DV == 128) {
             to_lds<2048>(place2, from, value_at_[2]);
-            to_lds<3072>(place2, from, value_at_[3]);
+            to_lds<3 * 1024>(place2, from, value_at_[3]);
         }
     };
     lf16_t o[VB];
