@@ -257,6 +257,36 @@ def test_prompts_of_any_number_of_heads(heads, dims):
     check_attend(p, 0, p.queries(n), p.weights(), start, expanded=True)
 
 
+@pytest.mark.parametrize("expanded", [False, True])
+def test_the_most_heads_and_rows(expanded):
+    """1024 heads and 16 new rows of one sequence: 16384 query rows on one latent a token."""
+    p = Latent((1, 1024, 256, 32, 64, 64, 48, 16, 64), [37, 20], (16, 8), 45)
+    start, n = rows([16, 1])
+    check_attend(p, 0, p.queries(n), p.weights(), start, 16, expanded)
+
+
+@pytest.mark.parametrize("expanded", [False, True])
+def test_lists_of_rows_that_do_not_ascend_reach_no_other_memory(expanded):
+    """A list out of order, below zero and past n_rows: what comes out is not said, but pool and the room around the output stay as they are."""
+    p = Latent((1, 4, 256, 32, 64, 64, 64, 16, 64), [50, 64, 20, 33], MIXED, 47)
+    n = 6
+    q, w = put(p.queries(n)), put(p.weights())
+    for wild in ([6, 4, 5, 0, 6], [0, 1 << 30, -5, 3, 2], [-(1 << 31), (1 << 31) - 1, 0, (1 << 31) - 1, 0], [5, 5, 5, 5, 5]):
+        start = put(np.array(wild, dtype=np.int32))
+        pages, pool = p.device()
+        room = torch.full((n + 64, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+        out = room[32:32 + n]
+        if expanded:
+            kvs.kv_latent_attend_prompts(pages, 0, q, w, space(p, n_tokens=300), out, 300, row_start=start)
+        else:
+            kvs.kv_latent_attend_tokens(pages, 0, q, w, space(p, 4), out, row_start=start, max_rows=4)
+        c, r = torch.full((n, 256), 3.0, dtype=torch.float16, device="cuda"), torch.full((n, 32), 3.0, dtype=torch.float16, device="cuda")
+        kvs.kv_latent_read_tokens(pages, 0, c, r, start)
+        torch.cuda.synchronize()
+        assert np.array_equal(pool.cpu().numpy(), p.pool)
+        assert torch.all(room[:32] == 7) and torch.all(room[32 + n:] == 7)
+
+
 @pytest.mark.parametrize("room", [70, 129, 500, 5000])
 def test_room_for_more_tokens_than_there_are(room):
     """What is made of the tokens does not depend on the room for others."""
