@@ -61,8 +61,13 @@ int check_moved_rows(const kv_latent_shape_t* shape, const kv_pages_t* pages, in
 double latent_scale(const kv_latent_shape_t& s) { return 1.4426950408889634 / std::sqrt(static_cast<double>(s.key_dim + s.rope_dim)); }
 
 // Query rows of a tile: the fewest that hold a sequence's, since the products and the probabilities of rows that are not there take their time: 64
-// rows of 8 contexts 25.9 us, in tiles of 128 38.7; 40 rows of one 8.7 and 10.7; 32 rows of 24 contexts 38.8, in tiles of 64 41.1.
-int32_t tile_rows_log2(int64_t rows) { return rows <= 16 ? 4 : rows <= 32 ? 5 : rows <= 64 ? 6 : 7; }
+// rows of 8 contexts 25.9 us, in tiles of 128 38.7; 40 rows of one 8.7 and 10.7; 32 rows of 24 contexts 38.8, in tiles of 64 41.1.  Of more
+// rows than 128, three tiles of 64 take as long as two of 128 less a tenth (a tile of 64 six tenths of one of 128): 160 rows of 16 contexts 27.3 us
+// and 31.5, 128 rows of 16 long ones 266 in tiles of 64 and 222 in one of 128.
+int32_t tile_rows_log2(int64_t rows) {
+    if (rows <= 64) return rows <= 16 ? 4 : rows <= 32 ? 5 : 6;
+    return 3 * ((rows + 63) / 64) < 5 * ((rows + 127) / 128) ? 6 : 7;
+}
 
 LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_rows) {
     LatentGeom g = {};

@@ -257,6 +257,15 @@ def test_prompts_of_any_number_of_heads(heads, dims):
     check_attend(p, 0, p.queries(n), p.weights(), start, expanded=True)
 
 
+@pytest.mark.parametrize("heads", [15, 16, 17, 31, 33, 63, 65, 127, 129, 160, 191, 193, 257, 321])
+def test_tiles_of_query_rows(heads):
+    """Numbers of query rows around every size of a tile, one row a head, and as many again for a second sequence's two rows."""
+    p = Latent((1, heads, 256, 32, 64, 64, 96, 16, 64), [90, 75], (16, 4), 49)
+    check_attend(p, 0, p.queries(2), p.weights())
+    start, n = rows([1, 2])
+    check_attend(p, 0, p.queries(n), p.weights(), start, 2)
+
+
 @pytest.mark.parametrize("expanded", [False, True])
 def test_the_most_heads_and_rows(expanded):
     """1024 heads and 16 new rows of one sequence: 16384 query rows on one latent a token."""
