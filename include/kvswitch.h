@@ -719,7 +719,7 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
  * kv_latent_attend_tokens takes the absorbed form, for few new rows: q[h] w_k[h]^T is rounded to fp16 and has to be in its range, the cache is
  * read once for all heads, and the sum of weights times latents goes through w_v[h].
  *   max_rows 1 .. 16: no sequence has more new rows (of one that has, the first max_rows are computed and the others' output is left as it
- *            was).
+ *            was).  A workspace for more rows or more sequences serves fewer.
  * kv_latent_attend_prompts takes the expanded form, for any number of new rows: keys and values of all heads are made in the workspace, rounded
  * to fp16 and to be in its range.
  *   n_tokens 1 .. 67108864: at least as many as the sequences that have new rows have tokens together.  Where they have more, sequences from the

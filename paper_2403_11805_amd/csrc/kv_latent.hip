@@ -101,6 +101,15 @@ LatentSpace latent_space(const kv_latent_shape_t& s, int32_t n_seqs, const Laten
     w.all = w.zeros + kZeroBytes;
     return w;
 }
+// What a caller provides for steps of up to max_rows rows.  A step's own space grows with its rows but for one place: with three tiles of 64 (129 to
+// 192 query rows) shares are half as high as in the tile of 128 that 65 to 128 rows take, so that their space may be the smaller one.  There the need
+// is that of the most rows that one tile holds, and a workspace for the longest of a program's steps serves all of them.
+uint64_t latent_need(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_rows) {
+    const uint64_t need = latent_space(s, n_seqs, latent_geom(s, n_seqs, max_rows)).all;
+    const int32_t in_one_tile = 128 / s.n_heads;
+    if (in_one_tile == 0 || max_rows <= in_one_tile || tile_rows_log2(static_cast<int64_t>(s.n_heads) * max_rows) == 7) return need;
+    return std::max(need, latent_space(s, n_seqs, latent_geom(s, n_seqs, in_one_tile)).all);
+}
 
 // The places of the line are counted in 31 bits; rows have workgroups of their own in the launches around the attention.
 int check_latent_attend(const kv_latent_shape_t* shape, int32_t n_seqs, int32_t max_rows) {
@@ -198,7 +207,7 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
 
 uint64_t kv_latent_attend_workspace_bytes(const kv_latent_shape_t* shape, int32_t n_seqs, int32_t max_rows) {
     if (check_latent_shape(shape) || check_seqs(n_seqs) || check_latent_attend(shape, n_seqs, max_rows)) return 0;
-    return latent_space(*shape, n_seqs, latent_geom(*shape, n_seqs, max_rows)).all;
+    return latent_need(*shape, n_seqs, max_rows);
 }
 
 int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t* pages, int32_t layer, const void* q, int64_t q_stride,
@@ -216,9 +225,10 @@ int32_t kv_latent_attend_tokens(const kv_latent_shape_t* shape, const kv_pages_t
     g.n_rows = n_rows;
     g.q_stride = q_stride;
     const LatentSpace sp = latent_space(*shape, n_seqs, g);
-    if (workspace_bytes < sp.all)
+    const uint64_t need = latent_need(*shape, n_seqs, max_rows);
+    if (workspace_bytes < need)
         return fail(KV_ENOMEM, "workspace of %llu bytes, %llu needed", static_cast<unsigned long long>(workspace_bytes),
-                    static_cast<unsigned long long>(sp.all));
+                    static_cast<unsigned long long>(need));
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
     uint8_t* space = static_cast<uint8_t*>(workspace);

@@ -380,3 +380,19 @@ def test_latent_pages_are_on_the_current_device_and_fixed():
     for bad in ((q[:, :, :64], w, ws, out), (q, w[:, :, :64], ws, out), (q, w, ws[:64], out), (q, w, ws.cpu(), out), (q, w, ws, out.float())):
         with pytest.raises((ValueError, TypeError, kvs.KvError)):
             kvs.kv_latent_attend_tokens(pages, 0, *bad)
+
+
+@pytest.mark.parametrize("heads,most", [(16, 9), (40, 4), (64, 3)])
+def test_one_workspace_for_the_longest_and_all_shorter_steps(heads, most):
+    """Drafts of one to `most` rows, whose query rows pass from one tile to three lower ones, in the workspace of the longest."""
+    p = Latent((1, heads, 256, 32, 64, 64, 1024, 16, 64), [1000, 17, 640], MIXED, 41)
+    pages, _ = p.device()
+    w, shared = put(p.weights()), space(p, max_rows=most)
+    for m in range(1, most + 1):
+        start, n = rows([m, 1, max(m - 1, 0)])
+        q, start = put(p.queries(n)), put(start)
+        out = torch.zeros((2, n, heads, 64), dtype=torch.float16, device="cuda")
+        kvs.kv_latent_attend_tokens(pages, 0, q, w, shared, out[0], row_start=start, max_rows=m)
+        kvs.kv_latent_attend_tokens(pages, 0, q, w, space(p, max_rows=m), out[1], row_start=start, max_rows=m)
+        torch.cuda.synchronize()
+        assert same(out[0], out[1]) and bool(out.any())
