@@ -78,9 +78,7 @@ LatentGeom latent_geom(const kv_latent_shape_t& s, int32_t n_seqs, int32_t max_r
     g.Dv = s.value_dim;
     g.tile_log2 = tile_rows_log2(rows);
     g.row_tiles = static_cast<int32_t>((rows + (1 << g.tile_log2) - 1) >> g.tile_log2);
-    const int64_t pairs = static_cast<int64_t>(n_seqs) * g.row_tiles, units = pairs * ((s.n_tokens + kLatentTile - 1) / kLatentTile);
-    // (one workgroup to a CU: its tiles fill LDS at latent_dim 512)
-    g.groups = static_cast<int32_t>(std::min<int64_t>(256, units + pairs * kLatentCost));
+    g.groups = latent_groups(static_cast<int64_t>(n_seqs) * g.row_tiles, s.n_tokens);
     g.scale_log2e = static_cast<float>(latent_scale(s));
     return g;
 }

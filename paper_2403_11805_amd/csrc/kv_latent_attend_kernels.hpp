@@ -35,7 +35,6 @@ struct LatentGeom {
 // How the work is divided.  The token tiles of all sequences and row tiles stand in one line, row tile by row tile, sequence by sequence, with
 // kLatentCost places in front of each row tile's for what beginning and ending takes, and every workgroup takes a run of it (latent_run).
 // line: the run's length, then, from line[4] on, where each sequence's places end.
-__device__ __forceinline__ int latent_places(int units) { return units ? units + kLatentCost : 0; }
 struct LatentSeq {
     int n, first, count, rows, row_tiles, units;     // tokens; new rows; query rows, tiles of them; tiles of tokens
 };
@@ -358,10 +357,9 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
             s_end = __builtin_amdgcn_readfirstlane(line[4 + s]);
             sw = latent_seq(a0->v, a0->g, a0->row_start, s);
         }
-        const int each = latent_places(sw.units), local = at - (s_end - each * sw.row_tiles);
-        const int rt = local / each, place = local - rt * each, places = min(each - place, run_end - at);
-        const int u_begin = max(place - kLatentCost, 0), u_end = place + places - kLatentCost;
-        at += places;
+        const LatentPiece piece = latent_piece(at, run_end, s_end, sw.units, sw.row_tiles);
+        const int rt = piece.row_tile, u_begin = piece.begin, u_end = piece.end;
+        at += piece.places;
         if (u_end <= u_begin) continue;
 
         const int count = min(sw.count, a0->g.max_rows), H = a0->g.H;
@@ -698,7 +696,7 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
         // the share: o[b][d][e] is latent (wave * DB + d) * 16 + 4 g4 + e of row b * 16 + l16
         const LatentAttendArgs* a1 = here();
         float *part_o = a1->part_o, *part_ml = a1->part_ml;
-        const int64_t slot = (blockIdx.x + static_cast<int64_t>(s) * a1->g.row_tiles + rt) * M;
+        const int64_t slot = latent_slot(static_cast<int32_t>(blockIdx.x), s, rt, a1->g.row_tiles) * M;
         const int here = min(M, sw.rows - rt * M);
 #pragma unroll
         for (int b = 0; b < MB; ++b)
@@ -742,9 +740,9 @@ __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGe
     float total = 0.0f;
     if (sw.units > 0) {
         const int M = 1 << g.tile_log2, j = nth * g.H + h, rt = j >> g.tile_log2;
-        const int begin = line[4 + s] - latent_places(sw.units) * (sw.row_tiles - rt) + kLatentCost, wg = begin / run;
-        const int used = (begin + sw.units - 1) / run - wg + 1;
-        const int64_t first = (wg + static_cast<int64_t>(s) * g.row_tiles + rt) * M + (j & (M - 1));
+        const LatentShares shares = latent_shares(line[4 + s], sw.units, rt, sw.row_tiles, run);
+        const int used = shares.count;
+        const int64_t first = latent_slot(shares.first, s, rt, g.row_tiles) * M + (j & (M - 1));
         // (the wavefronts all work the weights out, each writes and reads the same)
         float ref = -INFINITY;
         for (int k = lane; k < used; k += 64) ref = fmaxf(ref, part_ml[(first + static_cast<int64_t>(k) * M) * 2]);

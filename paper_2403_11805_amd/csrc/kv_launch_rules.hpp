@@ -101,6 +101,35 @@ constexpr int32_t latent_run(int32_t units, int32_t pairs, int32_t groups) {
     return static_cast<int32_t>(run > 1 ? run : 1);
 }
 
+// Its workgroups: one to a CU (its tiles fill LDS at latent_dim 512), no more than there can be places.
+inline int32_t latent_groups(int64_t pairs, int64_t tokens) {
+    return static_cast<int32_t>(std::min<int64_t>(256, pairs * ((tokens + 31) / 32 + kLatentCost)));
+}
+
+// Places of a row tile of `units` tiles of tokens in the line, and what a workgroup at place `at` of it has there up to run_end: tiles of tokens
+// [begin, end) of one row tile (none if only what is in front of them falls to it).  s_end: where the sequence's places end.
+constexpr int32_t latent_places(int32_t units) { return units ? units + kLatentCost : 0; }
+struct LatentPiece {
+    int32_t row_tile, begin, end, places;
+};
+constexpr LatentPiece latent_piece(int32_t at, int32_t run_end, int32_t s_end, int32_t units, int32_t row_tiles) {
+    const int32_t each = latent_places(units), local = at - (s_end - each * row_tiles);
+    const int32_t row_tile = local / each, place = local - row_tile * each, left = each - place, places = left < run_end - at ? left : run_end - at;
+    return {row_tile, place > kLatentCost ? place - kLatentCost : 0, place + places - kLatentCost, places};
+}
+// Where a workgroup leaves its share of a row tile, one of groups + n_seqs * most_row_tiles places: from one share to the next along the line the
+// workgroup grows, or the row tile, or both.  And the workgroups that have shares of one, from `first` on.
+constexpr int64_t latent_slot(int32_t workgroup, int32_t s, int32_t row_tile, int32_t most_row_tiles) {
+    return workgroup + static_cast<int64_t>(s) * most_row_tiles + row_tile;
+}
+struct LatentShares {
+    int32_t first, count;
+};
+constexpr LatentShares latent_shares(int32_t s_end, int32_t units, int32_t row_tile, int32_t row_tiles, int32_t run) {
+    const int32_t begin = s_end - latent_places(units) * (row_tiles - row_tile) + kLatentCost, first = begin / run;
+    return {first, (begin + units - 1) / run - first + 1};
+}
+
 // Eviction: workgroups that share a pair's moves, `rows` at a time each: some 2048 in all, at least four a pair.  512 pairs of 1170 moves
 // 130 us with 1024 or 2048, 145 with 4096; 12 pairs of up to 5700 moves 27 us with 4096, 28 with 2048, 31 with 1024.
 inline int64_t evict_blocks(int64_t pairs, int64_t list, int64_t rows) {
