@@ -707,7 +707,8 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
 
 /* Attention of the new rows to one layer's pages as they are packed,
  *   out[h] = softmax((q[h] . (c w_k[h], r)) / sqrt(key_dim + rope_dim), tokens up to the row's own, absent pages left out) (c w_v[h]),
- * with c as kv_latent_read_tokens gives it.  Logits, softmax and sums are fp32.  A row that sees no token, or none whose logit is more than
+ * with c as kv_latent_read_tokens gives it.  Logits, softmax and sums are fp32; the weights are rounded to fp16 where the
+ * values are summed with them, half a step of each.  A row that sees no token, or none whose logit is more than
  * -inf, gives zeros; one with a logit that is NaN or +inf is NaN.  What lies behind a sequence's end may be anything, and so may the rows of
  * tokens that a row does not see; a row that sees a token whose latent is not finite is not finite itself.
  *   q    dev fp16 [n_rows][n_heads][key_dim + rope_dim], position part last, q_stride elements from row to row (a multiple of 8);

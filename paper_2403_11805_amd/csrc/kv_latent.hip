@@ -154,8 +154,9 @@ int32_t kv_latent_append_tokens(const kv_latent_shape_t* shape, const kv_pages_t
     if (n_rows == 0) return KV_OK;
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
-    // Rows of a wavefront: one look at the tables for four rows against four wavefronts at once.  32768 rows of four sequences in pages of every width
-    // 13.5 us with four, 18.6 with one; 8192 rows 7.9 and 7.6; 64 rows of as many sequences 5.4 and 3.1.
+    // Rows of a wavefront: one look at the tables for four rows against four wavefronts at once.  32768 rows of four sequences in pages of every width,
+    // inputs and pages from memory, 16.8 us with four, 20.7 with one; 16384 rows 11.0 and 12.5; 8192 rows 8.2 and 7.7; 64 rows of as many sequences
+    // 6.8 and 3.6.
     const int units = n_rows >= 16384 ? 4 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
     const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
     if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);
@@ -182,8 +183,8 @@ int32_t kv_latent_read_tokens(const kv_latent_shape_t* shape, const kv_pages_t* 
     if (n_rows == 0) return KV_OK;
     const LatentView view = latent_view(*shape, *pages, layer);
     const int lpg = log2_of(shape->group / 8);
-    // As in appending; a row's loads and its results stand in registers, so two (24 ragged contexts of up to 16384 tokens: 107 us with two, 111 with four,
-    // 120 with one; 8192 rows 6.8 with two, 7.6 with one; 2048 rows 4.4 and 4.2).
+    // As in appending; a row's loads and its results stand in registers, so two (24 ragged contexts of up to 16384 tokens: 112 us with two, 118 with four,
+    // 126 with one; 8192 rows 7.4 with two, 8.2 with one; 2048 rows 5.2 and 4.6).
     const int units = n_rows >= 8192 ? 2 : 1, rows = units * (shape->latent_dim == 512 ? 1 : 2) * 4;
     const int64_t groups = (static_cast<int64_t>(n_rows) + rows - 1) / rows;
     if (groups > most_groups(256)) return fail(KV_ESHAPE, "n_rows %d too many for one call", n_rows);

@@ -84,7 +84,8 @@ __device__ __forceinline__ void latent_make_line(const LatentView& v, const Late
 // q' of the new rows, fp16 [n_seqs * max_rows][H][DC] (row nth of sequence s at s * max_rows + nth): a product per head of w's columns
 // [h][0, Dk) with the rows, whose contraction runs along both operands' memory, so that neither passes through LDS.  (Rounding q' to fp16
 // changes a logit by 2^-12 of the products it sums at random, as rounding a query does.)
-// Bound by reading w, half of it.  A wavefront has 32 latents and ROWS * 16 rows of one head.
+// 3.1 to 7.4 us: reading half of w, and the loop over Dk, whose 32 dimensions a turn wait for their own loads.  A wavefront has 32 latents and
+// ROWS * 16 rows of one head.
 // Grid (1 + H * DC / 128, row blocks), 256 threads: the first column makes the line and the zeros.
 template <int DC, int ROWS>
 __global__ __launch_bounds__(256) void latent_absorb_kernel(LatentView v, LatentGeom g, const _Float16* __restrict__ q, const _Float16* __restrict__ w,
@@ -290,11 +291,15 @@ struct LatentAttendArgs {
 // wavefronts, values by one.  A turn of the loop, with one barrier, asks for tile t + 3, has the logits and the softmax of tile t + 1 and the
 // values of tile t, and brings tile t + 2 into its form.  (With half of the wavefronts in another order, values before logits, 128 rows took 5 % longer.)
 //
-// 128 rows: 16 sequences of 32768 tokens in fp16, 604 MB read once, 186 us when the chip is cool, 221 after a few milliseconds of it: 3.2 and 2.7
-// TB/s, 0.8 and 0.66 PFLOP/s.  The same loop with the loads alone takes 132 us, with the products alone 141 to 165 (LDS gives 64 rows of keys 16
-// times, of values 8 times), with neither 31: what is over the products is the start of a workgroup (8 to 12 us until its first tile is there)
-// and the shares that it writes.  16 to 64 rows: the chain of a turn bounds it, load to tile, tile to logits, logits to weights, weights to values,
-// with a barrier: 24 packed contexts of up to 8000 tokens and 32 rows 38 us.
+// The weights of O are halves (11 bits; a turn's matrix instructions would be half as many again with the 22 bits of two), their sum is of the
+// unrounded ones, so that each weight is off by half a step on its own.
+//
+// 128 rows: 16 sequences of 32768 tokens in fp16, 604 MB read once, 187 us when the chip is cool, 199 to 218 after a few milliseconds of it: 3.2 to 2.8
+// TB/s, 0.78 to 0.67 PFLOP/s.  The same loop with the loads alone takes 132 us, with the products alone 141 to 165 (LDS gives 64 rows of keys 16
+// times, of values 8 times), with neither 31.  16 to 64 rows: 24 packed contexts of up to 8000 tokens and 32 rows 39 us in 12 turns.
+// A turn's time is a chain, logits to weights to values with a barrier, and at present a trip to memory besides: the compiler waits for the query rows
+// where they are first used, between the products of the logits in every turn (vmcnt 17 to 0 at 512 + 64), and so for the tile that this wavefront
+// has just asked for.  Only wavefronts without rows are three tiles ahead.  How much of a turn that is has not been measured.
 template <int DC, int DR, int M>
 __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs args) {
     // (arguments are fetched where they are used, in the loop only by what is rare: kept in registers all the time they do not fit, and what
@@ -715,9 +720,10 @@ __global__ __launch_bounds__(512, 2) void latent_attend_kernel(LatentAttendArgs 
 }
 
 // The shares of a query row joined: their sum over the sum of their weights, as the sum of two halves (22 bits, so that the product behind it
-// is not the result's largest error), hi and lo [n_seqs * max_rows][H][DC] each.  Latency bounds it, row, line, weights and shares being loads that
-// wait for each other, and reading the shares.  A workgroup's four wavefronts share a row (768 rows of 24 sequences 6.5 us, with a wavefront to a
-// row 7.7; 512 rows of 8 longer ones 8.9 and 12.5; 2048 rows of 32768 tokens 15.4 and 16.7; 2560 rows of up to 3001 tokens 9.6 and 9.3).
+// is not the result's largest error), hi and lo [n_seqs * max_rows][H][DC] each.  Latency bounds it, row, line, references, weights and shares being
+// loads that wait for each other (the shares' addresses are known before the weights are, and they are asked for after), and reading the shares.  A
+// workgroup's four wavefronts share a row (768 rows of 24 sequences 6.5 us, with a wavefront to a row 7.7; 512 rows of 8 longer ones 8.9 and 12.5; 2048
+// rows of 32768 tokens 15.4 and 16.7; 2560 rows of up to 3001 tokens 9.6 and 9.3).
 template <int DC>
 __global__ __launch_bounds__(256) void latent_join_kernel(LatentView v, LatentGeom g, const int32_t* __restrict__ row_start,
                                                           const int32_t* __restrict__ line, const float* __restrict__ part_o,

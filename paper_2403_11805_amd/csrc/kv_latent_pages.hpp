@@ -65,8 +65,11 @@ template <int DC> struct LatentLanes {
     static constexpr int kPieces = DC / 8, kSide = 64 / kPieces;
 };
 
-// Append: rows of new tokens into their pages.  Each row is read once and written once, 16 bytes a lane.  Bound by HBM where there are many (105000
-// rows of 1152 bytes to fp16 pages 37 us, 6.6 TB/s), by the chain from row to sequence to length to page where there are few (64 rows 3.0 us).
+// Append: rows of new tokens into their pages.  Each row is read once and written once, 16 bytes a lane.  Bound by HBM where there are many and
+// their pages are fp16 (105000 rows of 1152 bytes 47.5 us, 5.1 TB/s, where a large copy reaches 4.9; 37 us while the rows still lie in the chip's last
+// cache), by the chain from row to sequence to length to page where there are few (64 rows 3.0 us).  Into pages of 8, 4 and 2 bits 69000 rows take 34 us;
+// with four rows a wavefront the kernel is 91 to 97 KB of code, three widths, two types of parameters, four rows and two ways each, more than the
+// instruction cache of 64 KB, and what that costs beside the arithmetic is not measured.
 template <int DC, int UNITS>
 __global__ __launch_bounds__(256) void latent_append_kernel(LatentView v, const _Float16* __restrict__ c, int64_t c_stride,
                                                             const _Float16* __restrict__ r, int64_t r_stride, int32_t n_rows,
@@ -143,7 +146,9 @@ __device__ __forceinline__ u4_t read_piece(const LatentView& v, const uint8_t* r
 }
 
 // Read: the rows of a step from their pages, as fp16; rows that have no place, or one in an absent page, are left as they are.  24 contexts of up to
-// 16384 tokens in pages of every width 107 us, 3.4 TB/s: bound by the rows in flight, which their registers limit.
+// 16384 tokens in pages of every width, parameters in binary16, 112 us, 3.2 TB/s.  Bound by trips to memory that wait for each other: a parameter's
+// type is looked at where it is read, and a binary16 one is waited for there (latent_param), so that two rows of packed latents take four such trips
+// besides those of the tables, each with whatever else the wavefront has asked for.
 template <int DC, int UNITS>
 __global__ __launch_bounds__(256) void latent_read_kernel(LatentView v, _Float16* __restrict__ c, int64_t c_stride, _Float16* __restrict__ r,
                                                           int64_t r_stride, int32_t n_rows, int32_t lpg_log2,
@@ -159,7 +164,7 @@ __global__ __launch_bounds__(256) void latent_read_kernel(LatentView v, _Float16
     if constexpr (UNITS > 1) {
         const RowPlace at = row_place(v, row_start, n_rows, r0, s, lane);
         const int last = min(r0 + UNITS * L::kSide, n_rows) - 1;
-        if (rows_in_page(v, row_start, n_rows, last, r0, s, at)) {          // (most: one look at the tables, and all rows asked for at once)
+        if (rows_in_page(v, row_start, n_rows, last, r0, s, at)) {          // (most: one look at the tables; rows of fp16 are asked for all at once)
             const uint8_t* record = v.p.pool + at.off;
             const SlabAt slab = slab_at<DC>(v.p, at.b, v.layer);
             auto move = [&](auto WIDTH) __attribute__((always_inline)) {

@@ -1,6 +1,6 @@
 // Latent attention in the expanded form, for many new rows at once: keys and values of every head are made from the latents,
 //     k[h] = (c w_k[h], r),   v[h] = c w_v[h],
-// by one product over all tokens (kv_gemm_kernels.hpp), and the new rows attend to them, 2 H (Dk + Dr + Dv) operations a (row, token).
+// by one product over all tokens (latent_project_kernel), and the new rows attend to them, 2 H (Dk + Dr + Dv) operations a (row, token).
 //
 // Room for the tokens: each sequence that has new rows gets whole tiles of 32 tokens, one sequence after the other, as far as the room
 // reaches; a sequence that does not fit in gets none, and its rows are not computed.
@@ -67,7 +67,9 @@ __device__ __forceinline__ int first_behind(const int32_t* __restrict__ end, int
 }
 
 // A tile of 32 tokens from their pages: latents in the product's fragment order, position parts row-major, which halves' pages are there
-// (bits 0 and 1); tokens that are not there are zeros.  Bound by HBM where there are many: 40000 tokens of 8, 4 and 2 bits 25 to 27 us.
+// (bits 0 and 1); tokens that are not there are zeros.  40000 tokens of 8, 4 and 2 bits 27 us,
+// 66 MB, 2.5 TB/s: not bound by HBM but by a lane's pieces, each of which waits for its own loads (the branches on width and parameter type in
+// read_piece stand inside the loop) before the next is asked for.
 template <int DC, int DR>
 __global__ __launch_bounds__(256) void latent_gather_kernel(LatentView v, PromptGeom g, PromptTable t, int32_t lpg_log2, _Float16* __restrict__ latents,
                                                             _Float16* __restrict__ ropes, uint32_t* __restrict__ there) {
@@ -127,8 +129,10 @@ template <int ROW_BYTES, int HALVES> __device__ __forceinline__ h8_t read_column
 // Keys and values of all heads from the latents: a workgroup makes 128 tokens (four gathered tiles) x 256 columns, a wavefront 64 columns of them.
 // 32 of the latents' dimensions a stage, both operands straight to LDS, two stages ahead: the tokens as they were gathered are an operand as it
 // lies, rows of weights are transposed by the reads.  Two workgroups to a CU, so that one's results are written while the other multiplies: with 256
-// tokens in 512 threads, one to a CU, 40000 tokens x 8192 columns took 1.26 times as long.  4096 tokens x 32768 columns 140 to 155 us, 0.9 PFLOP/s;
-// 292 with results written from registers in pieces of 32 bytes and each column tile taken through all tokens.
+// tokens in 512 threads, one to a CU, 40000 tokens x 8192 columns took 1.26 times as long.  4096 tokens x 32768 columns 148 to 155 us, 0.9 PFLOP/s;
+// 292 with results written from registers in pieces of 32 bytes and each column tile taken through all tokens.  Whole column tiles go to an XCD, so
+// that few heads leave some without work: 256 columns (one head of 128 + 128) are made by one XCD of eight, 1024 by four, 2304 by five that have
+// two tiles each but one; the measurements are of 32768 columns, where all have the same.
 constexpr int kProjectTiles = 4, kProjectCols = 256;
 template <int DC>
 __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, int32_t n_seqs, int32_t N, int32_t col_tiles, int32_t token_tiles,
@@ -227,8 +231,13 @@ __global__ __launch_bounds__(256, 2) void latent_project_kernel(PromptTable t, i
 // 64 tokens a turn, two independent products S^T = K Q^T of 32 tokens each.  Keys and values go straight to LDS, the next turn's while this one's
 // are used; a turn makes the next one's logits beside its own probabilities.  Probabilities are rounded to fp16, and their sum is that of the
 // rounded ones, so that it has no part in the result's error.  (The last turn of a sequence may reach 32 tokens past its room; nobody sees them.)
-// Two workgroups to a CU, 242 of 256 registers.  Bound by the chip's power: one prompt of 4096 tokens and 128 heads, 0.69 TFLOP, takes 1.5 M cycles, in 45 %
-// of which the matrix pipe is busy, and 770 to 890 us at the clock that is left (1.65 to 1.85 GHz).  LDS gives a wavefront 56 KB a turn, a quarter of its rate.
+// Two workgroups to a CU, 242 of 256 registers.  One prompt of 4096 tokens and 128 heads, 0.69 TFLOP, takes 1.36 to 1.43 M cycles, in 47 to 49 % of
+// which the matrix pipe is busy, and 780 to 880 us at 1.56 to 1.76 GHz, the clock that the chip's power leaves (744 at best, when it is cool).  LDS gives a
+// wavefront 56 KB a turn, a quarter of its rate.  Not all of the idle cycles are explained: the compiler waits for the query rows where they are first
+// used, which is inside the walk, so that the first of every two turns waits between its products (vmcnt 11 to 0) for the keys and values that it has
+// just asked for; what that costs is not measured.
+// Tokens are not divided: H * (row tiles) workgroups walk a context each from its beginning, and few rows of few heads behind a long one leave most
+// CUs idle.
 constexpr int kPromptTile = 64, kPromptHeads = 4;
 template <int DK, int DR, int DV>
 __global__ __launch_bounds__(256, 2) void latent_prompt_kernel(LatentView v, PromptGeom g, PromptTable t, const int32_t* __restrict__ row_start,

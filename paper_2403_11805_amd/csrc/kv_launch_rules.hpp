@@ -92,8 +92,9 @@ constexpr AttendDivision attend_division(int32_t in_steps, int32_t in_two_steps,
 }
 
 // Latent attention: tiles of 32 tokens (places in the line of work) that a workgroup takes, of `units` tiles of tokens in `pairs` (sequence, row
-// tile) pairs, so that `groups` workgroups do.  (Longer runs save shares to write and to join, and lose more: 16 contexts of up to 3001 tokens,
-// 160 rows, 32.7 + 10.5 us against 37.6 + 9.3 in runs half as long again.)
+// tile) pairs, so that `groups` workgroups do.  (Longer runs save shares to write and to join, and lose more; attention + join in us, in
+// runs as they are and half as long again: 16 contexts of up to 3001 tokens and 160 rows 27.5 + 9.2 and 32.7 + 8.8, 24 of up to 8000 and 32 rows
+// 38.5 + 6.4 and 49.1 + 5.7, 8 of up to 8192 and 64 rows 26.1 + 8.5 and 29.8 + 7.3.)
 constexpr int kLatentCost = 4;
 constexpr int32_t latent_run(int32_t units, int32_t pairs, int32_t groups) {
     const int64_t places = static_cast<int64_t>(units) + static_cast<int64_t>(pairs) * kLatentCost;
